@@ -92,8 +92,9 @@ def _generator(seed):
 
 def _tokens(case, g):
     """Word ids with the skew of natural text (the r-th word has weight 1 / r^1.1); padding is -1."""
-    w = torch.arange(1, case["V"] + 1, device="cuda", dtype=torch.float32).pow(-1.1)
-    t = torch.multinomial(w, case["n"], replacement=True, generator=g)
+    up_to = torch.arange(1, case["V"] + 1, dtype=torch.float64).pow(-1.1).cumsum(dim=0)
+    u = torch.rand(case["n"], device="cuda", generator=g, dtype=torch.float64) * float(up_to[-1])
+    t = torch.searchsorted(up_to.cuda(), u).clamp(max=case["V"] - 1)
     if case["pad"]:
         t = torch.where(torch.rand(case["n"], device="cuda", generator=g) < case["pad"], torch.full_like(t, -1), t)
     return t.to(getattr(torch, case["tokens"]))
