@@ -242,8 +242,72 @@ int same_lda_selftest(int64_t* failures);
 /* Wait for everything enqueued on the handle's stream. */
 int same_lda_synchronize(same_lda_t* h);
 
-/* Text of the last failure of this handle (of the last failed same_lda_init when h is NULL).
- * The pointer stays valid until the next failing call.                                          */
+/* ---- Word tables as an embedding, in training and in serving --------------------------------------------------
+ * Operators on a table with one row per word: the word-topic matrix phi ([V][K], word-major: copy it out with
+ * same_lda_get) or any other embedding table.  They take no handle: the stream is an argument, its device must be
+ * the current one, all pointers are DEVICE pointers, every call only enqueues kernels and allocates nothing, so calls may
+ * be captured into a graph and may overlap on different streams (each with a workspace of its own).  The text of a
+ * failure is that of same_lda_last_error(NULL) on the same thread.  Operands must not overlap, unless said otherwise. */
+#define SAME_LDA_FLOAT   0   /* binary32                                                                           */
+#define SAME_LDA_BFLOAT  1   /* bfloat16                                                                           */
+#define SAME_LDA_HALF    2   /* binary16                                                                           */
+#define SAME_LDA_MICRO   3   /* microscaled four-bit floating point, see below                                     */
+#define SAME_LDA_WIDTH_MAX (1 << 20)   /* elements of a row (of the output of a product: 2^31 - 1)                 */
+
+/* A matrix of `rows` rows of `width` elements; the elements of a row are contiguous, rows are `stride` elements
+ * apart (at least width).
+ * SAME_LDA_MICRO: a row is cut into blocks of 32 elements.  An element is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6,
+ * the code 0 .. 7 in the low three bits of a half byte (the even element in the low half), the sign above them.
+ * A block has a scale byte s: its elements count 2^(s-127) times (s = 255: all are NaN).  Rows are filled up with
+ * zero blocks to a multiple of 128 elements and follow each other without gaps: 64 bytes of codes (data, aligned to
+ * 16) and 4 of scales (aligned to 4) per 128 elements; stride is not used.                                        */
+typedef struct {
+    void*    data;
+    uint8_t* scales;      /* SAME_LDA_MICRO only */
+    int64_t  rows;        /* below 2^31          */
+    int64_t  stride;
+    int32_t  width;
+    int32_t  type;
+} same_lda_rows;
+
+/* out[i] = scale * table[tokens[i]] for i < out->rows: the product in binary32, rounded once to the output's type.
+ *   tokens       [out->rows] int32 or int64 (token_bytes = 4 or 8); an id outside [0, table->rows) stands for no word
+ *                (padding): its row is zeros.  Null: row i of the table, for all of them (out->rows == table->rows): the
+ *                way to read a microscaled matrix back.
+ *   table        any type; out: any but SAME_LDA_MICRO                                                            */
+int same_lda_embed(const same_lda_rows* table, const void* tokens, int32_t token_bytes, float scale,
+                   const same_lda_rows* out, void* hip_stream);
+
+/* The gradient of that lookup with respect to the table:
+ *   table_grad[w] = scale * sum of grad[i] over the tokens i with tokens[i] = w         (accumulate = 0)
+ *   table_grad[w] += the same, for the words that have a token; others are not touched  (accumulate != 0)
+ * The tokens are sorted by word and every row is one sum in binary32 in an order that depends on the tokens alone, so equal
+ * calls give equal bits; the sum is rounded once to the type of table_grad.  Tokens that stand for no word add nothing:
+ * their rows of grad are not read.
+ *   workspace    as many bytes as same_lda_embed_grad_workspace says for the same matrices (it reads their shapes), aligned
+ *                to 16; its contents are scratch, in use until the call's kernels have ended                          */
+int same_lda_embed_grad_workspace(const same_lda_rows* grad, const same_lda_rows* table_grad, size_t* bytes);
+int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale,
+                        int32_t accumulate, const same_lda_rows* table_grad, void* workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
+/* Bytes of the codes and of the scales of a microscaled matrix. */
+int same_lda_micro_size(int64_t rows, int32_t width, size_t* code_bytes, size_t* scale_bytes);
+
+/* x in microscaled form.  For a block whose largest magnitude is top: s - 127 = floor(log2 top) - 2, at least -127 (zeros:
+ * s = 0); an element is x / 2^(s-127) rounded to the nearest of the sizes, ties to the even code, above 6 to 6.  A block
+ * that holds an infinity or a NaN becomes NaN as a whole (s = 255, codes 0).                                       */
+int same_lda_micro_quantize(const same_lda_rows* x, const same_lda_rows* micro_out, void* hip_stream);
+
+/* out[i][j] = scale * sum_k a[i][k] * b[j][k], both microscaled and of one width, in binary32, rounded once to the output's
+ * type: with rows of topic weights and the rows of phi, the predictive weight of every word (same_lda_sddmm is the
+ * same product at the nonzeros only, of unrounded matrices).
+ *   out          [a->rows][b->rows]                                                                               */
+int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out,
+                           void* hip_stream);
+
+/* Text of the last failure of this handle (when h is NULL: of the last failed call without a handle, same_lda_init
+ * among them, on the calling thread).  The pointer stays valid until the next failing call.                        */
 const char* same_lda_last_error(const same_lda_t* h);
 
 #ifdef __cplusplus

@@ -24,6 +24,7 @@ _DTYPES = {THETA: np.float32, PHI: np.float32, NDK: np.uint32, NWK: np.uint32, N
 EXPORTS = ["same_lda_init", "same_lda_sweep", "same_lda_sweep_poisson", "same_lda_sweep_sampled", "same_lda_loglik", "same_lda_free",
            "same_lda_set_batch", "same_lda_stage_batch", "same_lda_commit_batch", "same_lda_debug_draw_poisson", "same_lda_sddmm",
            "same_lda_vb_exp_elog_beta", "same_lda_vb_estep",
+           "same_lda_embed", "same_lda_embed_grad_workspace", "same_lda_embed_grad", "same_lda_micro_size", "same_lda_micro_quantize", "same_lda_micro_product",
            "same_lda_get", "same_lda_set", "same_lda_get_pass", "same_lda_set_pass", "same_lda_task_count",
            "same_lda_debug_draw", "same_lda_debug_draw_noalloc", "same_lda_debug_chunk_limit", "same_lda_set_timing", "same_lda_get_timing", "same_lda_selftest",
            "same_lda_synchronize",
@@ -39,6 +40,10 @@ class SameLdaError(RuntimeError):
 class _Csc(Structure):
     _fields_ = [("D", c_int32), ("V", c_int32), ("nnz", c_int64), ("colptr", c_void_p),
                 ("rowidx", c_void_p), ("val", c_void_p), ("on_device", c_int32)]
+
+
+class _Rows(Structure):
+    _fields_ = [("data", c_void_p), ("scales", c_void_p), ("rows", c_int64), ("stride", c_int64), ("width", c_int32), ("type", c_int32)]
 
 
 _lib = None
@@ -81,6 +86,12 @@ def load(path: str | None = None) -> ctypes.CDLL:
         L.same_lda_sddmm.argtypes = [c_void_p, c_void_p, c_int32]
         L.same_lda_vb_exp_elog_beta.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
         L.same_lda_vb_estep.argtypes = [c_void_p, c_void_p, c_void_p, c_float, c_int32, c_void_p, c_void_p]
+        L.same_lda_embed.argtypes = [POINTER(_Rows), c_void_p, c_int32, c_float, POINTER(_Rows), c_void_p]
+        L.same_lda_embed_grad_workspace.argtypes = [POINTER(_Rows), POINTER(_Rows), POINTER(c_size_t)]
+        L.same_lda_embed_grad.argtypes = [POINTER(_Rows), c_void_p, c_int32, c_float, c_int32, POINTER(_Rows), c_void_p, c_size_t, c_void_p]
+        L.same_lda_micro_size.argtypes = [c_int64, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
+        L.same_lda_micro_quantize.argtypes = [POINTER(_Rows), POINTER(_Rows), c_void_p]
+        L.same_lda_micro_product.argtypes = [POINTER(_Rows), POINTER(_Rows), c_float, POINTER(_Rows), c_void_p]
         L.same_lda_set_timing.argtypes = [c_void_p, c_int32]
         L.same_lda_get_timing.argtypes = [c_void_p, POINTER(c_double), POINTER(c_int64)]
         L.same_lda_selftest.argtypes = [POINTER(c_int64)]
@@ -195,7 +206,20 @@ class SameLDA:
         return {THETA: (self.D, self.K), PHI: (self.V, self.K), NDK: (self.D, self.K),
                 NWK: (self.V, self.K), NK: (self.K,)}[which]
 
-    def get(self, which) -> np.ndarray:
+    def get(self, which, out=None):
+        """A state matrix as a numpy array; ``out``: a contiguous torch tensor of its shape and type (float32 for THETA and
+        PHI, int32 for NDK and NWK, int64 for NK) that is filled instead, on the host or the device."""
+        if out is not None:
+            import torch
+            dtype = {np.float32: torch.float32, np.uint32: torch.int32, np.uint64: torch.int64}[_DTYPES[which]]
+            if tuple(out.shape) != self._shape(which) or out.dtype != dtype or not out.is_contiguous():
+                raise ValueError(f"out must be a contiguous {dtype} tensor of shape {self._shape(which)}")
+            nbytes = out.numel() * out.element_size()
+            on_device = out.device.type == "cuda"
+            if on_device:
+                torch.cuda.current_stream(out.device).synchronize()     # what is still being done to out ends first
+            self._check(self._lib.same_lda_get(self._h, which, out.data_ptr() if nbytes else None, nbytes, 1 if on_device else 0))
+            return out
         out = np.empty(self._shape(which), dtype=_DTYPES[which])
         self._check(self._lib.same_lda_get(self._h, which, out.ctypes.data if out.size else None, out.nbytes, 0))
         return out
@@ -303,3 +327,187 @@ class SameLDA:
             self.close()
         except Exception:
             pass
+
+
+# ---- Word tables as an embedding.  These functions take torch tensors on one GPU, run on torch's current stream of that
+# GPU and return at once; what a call allocates (outputs, scratch) comes from torch's allocator.
+
+_types = None
+
+
+def _type_of(dtype) -> int:
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    t = _types.get(dtype)
+    if t is None:
+        raise TypeError(f"{dtype} is not one of float32, bfloat16 and float16")
+    return t
+
+
+MICRO = 3
+
+
+class MicroMatrix:
+    """A matrix in microscaled four-bit floating point: ``codes`` [rows, 64 * g] and ``scales`` [rows, 4 * g], contiguous
+    uint8 tensors on one GPU with g = ceil(width / 128), in the layout that include/same_lda.h describes."""
+
+    __slots__ = ("codes", "scales", "width", "rows")
+
+    def __init__(self, codes, scales, width):
+        import torch
+        width = int(width)
+        groups = -(-width // 128)
+        rows = codes.shape[0]
+        if (width < 1 or codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(codes.shape) != (rows, 64 * groups)
+                or tuple(scales.shape) != (rows, 4 * groups) or not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device):
+            raise ValueError(f"rows of {width} elements need contiguous uint8 codes [rows, {64 * groups}] and scales [rows, {4 * groups}] on one device")
+        self.codes, self.scales, self.width, self.rows = codes, scales, width, rows
+
+    @property
+    def shape(self):
+        return (self.rows, self.width)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def __getitem__(self, rows):
+        """A range of rows (a slice without a step), not copied."""
+        if not isinstance(rows, slice) or rows.step not in (None, 1):
+            raise TypeError("a microscaled matrix is sliced by ranges of rows")
+        return MicroMatrix(self.codes[rows], self.scales[rows], self.width)
+
+
+def _rows(x) -> _Rows:
+    if isinstance(x, MicroMatrix):
+        return _Rows(x.codes.data_ptr() or None, x.scales.data_ptr() or None, x.rows, x.width, x.width, MICRO)
+    if x.dim() != 2:
+        raise ValueError(f"a matrix has two dimensions, not {x.dim()}")
+    rows, width = x.shape
+    stride, inner = x.stride()
+    if inner != 1 and width > 1 or stride < width and rows > 1:
+        raise ValueError("the elements of a row must be contiguous and rows must not overlap")
+    return _Rows(x.data_ptr() or None, None, rows, stride if rows > 1 else width, width, _type_of(x.dtype))
+
+
+class _On:
+    """The GPU that the operands live on as the current one, and torch's stream there."""
+
+    __slots__ = ("device", "before", "stream")
+
+    def __init__(self, *operands):
+        self.device = operands[0].device
+        for x in operands:
+            if x.device != self.device or x.device.type != "cuda":
+                raise ValueError(f"all operands must be on one GPU (got {[str(y.device) for y in operands]})")
+
+    def __enter__(self):
+        import torch
+        self.before = torch.cuda.current_device()
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.device)
+        return torch.cuda.current_stream(self.device).cuda_stream or None
+
+    def __exit__(self, *_):
+        if self.before != self.device.index:
+            import torch
+            torch.cuda.set_device(self.before)
+
+
+def _done(rc):
+    if rc != 0:
+        raise SameLdaError(rc, load().same_lda_last_error(None).decode())
+
+
+def _token_ids(tokens):
+    import torch
+    if tokens.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"tokens are int32 or int64, not {tokens.dtype}")
+    return tokens.contiguous()
+
+
+def _output(out, shape, dtype, device):
+    import torch
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype}")
+    return out
+
+
+def embed(table, tokens, scale=1.0, dtype=None, out=None):
+    """scale * table[tokens]: the rows of `table` (a matrix, or a MicroMatrix) for int32 or int64 `tokens` of any shape, in
+    `dtype` (default: the table's, float32 for a MicroMatrix).  An id outside the table (padding) gives zeros.  `out`: a tensor of
+    shape tokens.shape + (width,) whose leading dimensions can be viewed as one."""
+    ids = _token_ids(tokens)
+    with _On(table, ids, *(() if out is None else (out,))) as stream:
+        if dtype is None and out is None:
+            import torch
+            dtype = torch.float32 if isinstance(table, MicroMatrix) else table.dtype
+        out = _output(out, (*tokens.shape, table.shape[1]), dtype, ids.device)
+        flat = out if out.dim() == 2 else out.view(-1, out.shape[-1])
+        if ids.numel():
+            _done(load().same_lda_embed(byref(_rows(table)), ids.data_ptr(), ids.element_size(), scale, byref(_rows(flat)), stream))
+    return out
+
+
+def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumulate=False):
+    """The gradient of ``embed(table, tokens, scale)`` with respect to a table of `rows` rows, from that of its result: `grad`
+    of shape tokens.shape + (width,).  `dtype` (default: grad's) is the result's type.  `out`: where it is written, or added to with
+    ``accumulate=True``; `rows` is then out's.  Equal calls give equal bits."""
+    import torch
+    ids = _token_ids(tokens)
+    if tuple(grad.shape[:-1]) != tuple(tokens.shape):
+        raise ValueError(f"grad has shape {tuple(grad.shape)}, tokens {tuple(tokens.shape)}")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    if rows is None:
+        if out is None:
+            raise ValueError("rows or out must say how many rows the table has")
+        rows = out.shape[0]
+    with _On(grad, ids, *(() if out is None else (out,))) as stream:
+        out = _output(out, (int(rows), grad.shape[-1]), grad.dtype if dtype is None and out is None else dtype, ids.device)
+        flat = grad if grad.dim() == 2 else grad.reshape(-1, grad.shape[-1])
+        g, o = _rows(flat), _rows(out)
+        n = c_size_t()
+        L = load()
+        _done(L.same_lda_embed_grad_workspace(byref(g), byref(o), byref(n)))
+        space = torch.empty(n.value, dtype=torch.uint8, device=ids.device)
+        _done(L.same_lda_embed_grad(byref(g), ids.data_ptr() or None, ids.element_size(), scale, 1 if accumulate else 0, byref(o), space.data_ptr() or None, n.value, stream))
+    return out
+
+
+def micro_quantize(x, out=None) -> MicroMatrix:
+    """A matrix in microscaled four-bit floating point."""
+    import torch
+    with _On(x, *(() if out is None else (out,))) as stream:
+        r = _rows(x)
+        if out is None:
+            groups = -(-r.width // 128)
+            out = MicroMatrix(torch.empty(r.rows, 64 * groups, dtype=torch.uint8, device=x.device),
+                              torch.empty(r.rows, 4 * groups, dtype=torch.uint8, device=x.device), r.width)
+        _done(load().same_lda_micro_quantize(byref(r), byref(_rows(out)), stream))
+    return out
+
+
+def micro_dequantize(q, dtype=None, out=None):
+    """The numbers that a MicroMatrix stands for, in `dtype` (default: float32)."""
+    import torch
+    with _On(q, *(() if out is None else (out,))) as stream:
+        out = _output(out, q.shape, torch.float32 if dtype is None and out is None else dtype, q.device)
+        _done(load().same_lda_embed(byref(_rows(q)), None, 8, 1.0, byref(_rows(out)), stream))
+    return out
+
+
+def micro_product(a, b, scale=1.0, dtype=None, out=None):
+    """scale * a @ b.T in `dtype` (default: float32) for a MicroMatrix `b`; `a` is a MicroMatrix, or a matrix that is rounded to
+    one first."""
+    import torch
+    if not isinstance(a, MicroMatrix):
+        a = micro_quantize(a)
+    with _On(a, b, *(() if out is None else (out,))) as stream:
+        out = _output(out, (a.rows, b.rows), torch.float32 if dtype is None and out is None else dtype, a.device)
+        _done(load().same_lda_micro_product(byref(_rows(a)), byref(_rows(b)), scale, byref(_rows(out)), stream))
+    return out

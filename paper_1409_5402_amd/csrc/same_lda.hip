@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "draw_kernel.h"
+#include "errors.h"
 #include "gamma_kernels.h"
 #include "poisson_kernel.h"
 #include "sddmm_kernel.h"
@@ -1415,3 +1416,13 @@ const char* same_lda_last_error(const same_lda_t* h)
 }
 
 }  // extern "C"
+
+int same::fail_without_handle(int code, const char* fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return fail(nullptr, code, "%s", buf);
+}

@@ -1,0 +1,309 @@
+// Host side of the word-table operators: argument checks and launches.  No handle, no device memory of its own, nothing
+// that waits: every call only enqueues kernels, so all of them can be captured into a graph.
+#include "../../include/same_lda.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "embed_kernels.h"
+#include "errors.h"
+#include "micro_kernels.h"
+
+namespace {
+
+using same::fail_without_handle;
+
+int element_bytes(int32_t type) { return type == SAME_LDA_FLOAT ? 4 : 2; }
+bool is_float_type(int32_t type) { return type == SAME_LDA_FLOAT || type == SAME_LDA_BFLOAT || type == SAME_LDA_HALF; }
+
+// Shape, type and alignment of one operand.  `micro`: whether it is in four bits (-1: either).
+int check_rows(const char* call, const char* name, const same_lda_rows* m, int micro, int32_t width_max = SAME_LDA_WIDTH_MAX)
+{
+    if (!m) return fail_without_handle(SAME_LDA_EINVAL, "%s: %s is null", call, name);
+    if (m->type != SAME_LDA_MICRO && !is_float_type(m->type)) return fail_without_handle(SAME_LDA_EINVAL, "%s: %s has the unknown type %d", call, name, m->type);
+    if (micro >= 0 && (m->type == SAME_LDA_MICRO) != (micro == 1))
+        return fail_without_handle(SAME_LDA_EINVAL, "%s: %s %s be microscaled", call, name, micro ? "must" : "must not");
+    if (m->rows < 0 || m->rows >= (int64_t)1 << 31) return fail_without_handle(SAME_LDA_EINVAL, "%s: %s has %lld rows, not in [0, 2^31)", call, name, (long long)m->rows);
+    if (m->width < 1 || m->width > width_max)
+        return fail_without_handle(SAME_LDA_EINVAL, "%s: rows of %s hold %d elements, not in [1, %d]", call, name, m->width, width_max);
+    if (m->type != SAME_LDA_MICRO && m->rows > 1 && m->stride < m->width)
+        return fail_without_handle(SAME_LDA_EINVAL, "%s: the stride %lld of %s is less than its width %d", call, (long long)m->stride, name, m->width);
+    if (m->type != SAME_LDA_MICRO && m->rows > 1 && m->stride > ((int64_t)1 << 62) / 8 / m->rows)
+        return fail_without_handle(SAME_LDA_EINVAL, "%s: the stride %lld of %s is too large", call, (long long)m->stride, name);
+    if (m->rows == 0) return SAME_LDA_OK;
+    if (!m->data || (m->type == SAME_LDA_MICRO && !m->scales)) return fail_without_handle(SAME_LDA_EINVAL, "%s: %s has no data", call, name);
+    const uintptr_t align = m->type == SAME_LDA_MICRO ? 16 : (uintptr_t)element_bytes(m->type);
+    if ((uintptr_t)m->data % align || (m->type == SAME_LDA_MICRO && (uintptr_t)m->scales % 4))
+        return fail_without_handle(SAME_LDA_EINVAL, "%s: %s is not aligned (elements to their size, codes to 16 bytes, scales to 4)", call, name);
+    return SAME_LDA_OK;
+}
+
+int check_tokens(const char* call, const void* tokens, int32_t token_bytes, int64_t n)
+{
+    if (token_bytes != 4 && token_bytes != 8) return fail_without_handle(SAME_LDA_EINVAL, "%s: tokens have %d bytes, not 4 or 8", call, token_bytes);
+    if ((uintptr_t)tokens % token_bytes) return fail_without_handle(SAME_LDA_EINVAL, "%s: tokens are not aligned to their size", call);
+    if (n < 0 || n >= (int64_t)1 << 31) return fail_without_handle(SAME_LDA_EINVAL, "%s: %lld tokens, not in [0, 2^31)", call, (long long)n);
+    return SAME_LDA_OK;
+}
+
+int launched(const char* call)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SAME_LDA_OK : fail_without_handle(SAME_LDA_EHIP, "%s: %s", call, hipGetErrorString(e));
+}
+
+// Whether chunks of v elements of every row are aligned to their size (16 bytes at most).
+bool chunks_fit(const same_lda_rows* m, int v)
+{
+    if (m->type == SAME_LDA_MICRO) return true;
+    const int64_t bytes = (int64_t)v * element_bytes(m->type);
+    const int64_t align = bytes < 16 ? bytes : 16;
+    return m->width % v == 0 && (uintptr_t)m->data % align == 0 && (m->rows < 2 || m->stride * element_bytes(m->type) % align == 0);
+}
+
+// Lanes that share a row of so many chunks: the power of two from 1 to 64 that leaves the fewest idle.
+int lanes_log2_for(int64_t chunks)
+{
+    int l = 0;
+    while (l < 6 && ((int64_t)1 << l) < chunks) ++l;
+    return l;
+}
+
+int64_t at_most(int64_t n, int64_t most) { return n < most ? n : most; }
+
+constexpr int64_t kMaxGroups = (int64_t)1 << 22;     // workgroups of a launch (256 threads each: below 2^32 threads)
+
+template <class TI, class TO, int V>
+int embed_launch(same::EmbedArgs& a, int32_t width, hipStream_t st)
+{
+    a.chunks = width / V;
+    a.lanes_log2 = lanes_log2_for(a.chunks);
+    const int64_t per = (int64_t)256 >> a.lanes_log2;
+    const int64_t groups = at_most((a.n + per - 1) / per, kMaxGroups);
+    hipLaunchKernelGGL((same::embed_kernel<TI, TO, V>), dim3((unsigned)groups), dim3(256), 0, st, a);
+    return launched("embed");
+}
+
+// The widest chunks that both sides are aligned for: 16 bytes of the narrower type, two elements, or one.
+template <class TI, class TO>
+int embed_by_width(same::EmbedArgs& a, const same_lda_rows* table, const same_lda_rows* out, hipStream_t st)
+{
+    constexpr int kWide = sizeof(TI) == 4 && sizeof(TO) == 4 ? 4 : 8;
+    if (out->width % kWide == 0 && chunks_fit(table, kWide) && chunks_fit(out, kWide)) return embed_launch<TI, TO, kWide>(a, out->width, st);
+    if (out->width % 2 == 0 && chunks_fit(table, 2) && chunks_fit(out, 2)) return embed_launch<TI, TO, 2>(a, out->width, st);
+    return embed_launch<TI, TO, 1>(a, out->width, st);
+}
+
+template <class TI>
+int embed_to(same::EmbedArgs& a, const same_lda_rows* table, const same_lda_rows* out, hipStream_t st)
+{
+    switch (out->type) {
+        case SAME_LDA_FLOAT:  return embed_by_width<TI, float>(a, table, out, st);
+        case SAME_LDA_BFLOAT: return embed_by_width<TI, __bf16>(a, table, out, st);
+        default:              return embed_by_width<TI, _Float16>(a, table, out, st);
+    }
+}
+
+// Workspace of the gradient, in this order; every part starts at a multiple of 256 bytes.
+struct GradSpace {
+    size_t keys[2], pos[2], hist, start, partial, bytes;
+    uint32_t tiles;
+    int64_t ranges;
+    int passes, bits;
+};
+
+GradSpace grad_space(int64_t n, int64_t rows, int32_t width)
+{
+    GradSpace s;
+    size_t at = 0;
+    const auto part = [&at](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
+    int bits = 1;
+    while (((int64_t)1 << bits) <= rows) ++bits;                     // words 0 .. rows - 1, and rows for padding
+    s.passes = (bits + same::kDigitBits - 1) / same::kDigitBits;
+    s.bits = (bits + s.passes - 1) / s.passes;
+    s.tiles = (uint32_t)((n + same::kTileTokens - 1) / same::kTileTokens);
+    s.ranges = (n + same::kLongRun - 1) / same::kLongRun;
+    if (n <= same::kLongRun) s.ranges = 0;                           // no run can be long
+    for (int i = 0; i < 2; ++i) { s.keys[i] = part((size_t)n * 4); s.pos[i] = part((size_t)n * 4); }
+    s.hist = part(((size_t)s.tiles << s.bits) * 4);
+    s.start = part(((size_t)rows + 1) * 4);
+    s.partial = part((size_t)s.ranges * 2 * (size_t)width * 4);
+    s.bytes = at;
+    return s;
+}
+
+template <class TI, class TO, int V>
+int grad_launch(same::GradArgs& a, hipStream_t st)
+{
+    a.chunks = a.width / V;
+    a.lanes_log2 = lanes_log2_for(a.chunks);
+    const int64_t per = (int64_t)256 >> a.lanes_log2;
+    const unsigned across = (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2);
+    const int64_t most = kMaxGroups / across;                        // across <= SAME_LDA_WIDTH_MAX / 64
+    hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V>), dim3((unsigned)at_most((a.ranges + a.rows + per - 1) / per, most), across), dim3(256), 0, st, a);
+    if (a.ranges > 0)
+        hipLaunchKernelGGL((same::embed_grad_join_kernel<TO, V>), dim3((unsigned)at_most((a.ranges + per - 1) / per, most), across), dim3(256), 0, st, a);
+    return launched("embed_grad");
+}
+
+template <class TI, class TO>
+int grad_by_width(same::GradArgs& a, const same_lda_rows* grad, const same_lda_rows* out, hipStream_t st)
+{
+    constexpr int kWide = sizeof(TI) == 4 && sizeof(TO) == 4 ? 4 : 8;
+    if (chunks_fit(grad, kWide) && chunks_fit(out, kWide)) return grad_launch<TI, TO, kWide>(a, st);
+    if (chunks_fit(grad, 2) && chunks_fit(out, 2)) return grad_launch<TI, TO, 2>(a, st);
+    return grad_launch<TI, TO, 1>(a, st);
+}
+
+template <class TI>
+int grad_to(same::GradArgs& a, const same_lda_rows* grad, const same_lda_rows* out, hipStream_t st)
+{
+    switch (out->type) {
+        case SAME_LDA_FLOAT:  return grad_by_width<TI, float>(a, grad, out, st);
+        case SAME_LDA_BFLOAT: return grad_by_width<TI, __bf16>(a, grad, out, st);
+        default:              return grad_by_width<TI, _Float16>(a, grad, out, st);
+    }
+}
+
+int check_grad(const same_lda_rows* grad, const same_lda_rows* table_grad)
+{
+    int rc = check_rows("embed_grad", "grad", grad, 0);
+    if (!rc) rc = check_rows("embed_grad", "table_grad", table_grad, 0);
+    if (!rc && grad->width != table_grad->width)
+        rc = fail_without_handle(SAME_LDA_EINVAL, "embed_grad: rows of %d and of %d elements", grad->width, table_grad->width);
+    return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int same_lda_embed(const same_lda_rows* table, const void* tokens, int32_t token_bytes, float scale, const same_lda_rows* out, void* hip_stream)
+{
+    int rc = check_rows("embed", "table", table, -1);
+    if (!rc) rc = check_rows("embed", "out", out, 0);
+    if (!rc) rc = check_tokens("embed", tokens, token_bytes, out->rows);
+    if (rc) return rc;
+    if (table->width != out->width) return fail_without_handle(SAME_LDA_EINVAL, "embed: rows of %d and of %d elements", table->width, out->width);
+    if (!tokens && out->rows != table->rows)
+        return fail_without_handle(SAME_LDA_EINVAL, "embed: without tokens all %lld rows are written, not %lld", (long long)table->rows, (long long)out->rows);
+    if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "embed: the scale must be finite");
+    if (out->rows == 0) return SAME_LDA_OK;
+    const bool micro = table->type == SAME_LDA_MICRO;
+    same::EmbedArgs a = {table->data, table->scales, table->rows, micro ? same::micro_code_pitch(table->width) : table->stride, {tokens, token_bytes == 8},
+                         out->rows, scale, out->data, out->stride, 0, 0};
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    switch (table->type) {
+        case SAME_LDA_FLOAT:  return embed_to<float>(a, table, out, st);
+        case SAME_LDA_BFLOAT: return embed_to<__bf16>(a, table, out, st);
+        case SAME_LDA_HALF:   return embed_to<_Float16>(a, table, out, st);
+        default:              return embed_to<uint8_t>(a, table, out, st);
+    }
+}
+
+int same_lda_embed_grad_workspace(const same_lda_rows* grad, const same_lda_rows* table_grad, size_t* bytes)
+{
+    if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: bytes is null");
+    const int rc = check_grad(grad, table_grad);
+    if (rc) return rc;
+    *bytes = grad_space(grad->rows, table_grad->rows, grad->width).bytes;
+    return SAME_LDA_OK;
+}
+
+int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale, int32_t accumulate,
+                        const same_lda_rows* table_grad, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    int rc = check_grad(grad, table_grad);
+    if (!rc) rc = check_tokens("embed_grad", tokens, token_bytes, grad->rows);
+    if (rc) return rc;
+    if (!tokens && grad->rows > 0) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: tokens is null");
+    if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: the scale must be finite");
+    const int64_t n = grad->rows, rows = table_grad->rows;
+    const GradSpace s = grad_space(n, rows, grad->width);
+    if (rows == 0 || (n == 0 && accumulate)) return SAME_LDA_OK;
+    if (!workspace || workspace_bytes < s.bytes || (uintptr_t)workspace % 16)
+        return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: needs %zu bytes of workspace aligned to 16 (got %zu)", s.bytes, workspace ? workspace_bytes : (size_t)0);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    char* const w = static_cast<char*>(workspace);
+    const same::Tokens t = {tokens, token_bytes == 8};
+    const int32_t *keys = nullptr, *pos = nullptr;
+    uint32_t* const hist = reinterpret_cast<uint32_t*>(w + s.hist);
+    int32_t* const start = reinterpret_cast<int32_t*>(w + s.start);
+    for (int i = 0; n > 0 && i < s.passes; ++i) {
+        int32_t* const keys_to = reinterpret_cast<int32_t*>(w + s.keys[i & 1]);
+        int32_t* const pos_to = reinterpret_cast<int32_t*>(w + s.pos[i & 1]);
+        hipLaunchKernelGGL(same::token_histogram, dim3(s.tiles), dim3(256), 0, st, t, rows, keys, n, i * s.bits, s.bits, s.tiles, hist);
+        hipLaunchKernelGGL(same::token_offsets, dim3(1), dim3(1024), 0, st, hist, (int64_t)s.tiles << s.bits);
+        hipLaunchKernelGGL(same::token_place, dim3(s.tiles), dim3(256), 0, st, t, rows, keys, pos, n, i * s.bits, s.bits, s.tiles, hist, keys_to, pos_to);
+        keys = keys_to; pos = pos_to;
+    }
+    hipLaunchKernelGGL(same::word_runs, dim3((unsigned)((rows + 256) / 256)), dim3(256), 0, st, keys, n, rows, start);
+    if ((rc = launched("embed_grad"))) return rc;
+    same::GradArgs a = {grad->data, grad->stride, pos, keys, start, rows, scale, accumulate, table_grad->data, table_grad->stride,
+                        reinterpret_cast<float*>(w + s.partial), s.ranges, grad->width, 0, 0};
+    switch (grad->type) {
+        case SAME_LDA_FLOAT:  return grad_to<float>(a, grad, table_grad, st);
+        case SAME_LDA_BFLOAT: return grad_to<__bf16>(a, grad, table_grad, st);
+        default:              return grad_to<_Float16>(a, grad, table_grad, st);
+    }
+}
+
+int same_lda_micro_size(int64_t rows, int32_t width, size_t* code_bytes, size_t* scale_bytes)
+{
+    if (!code_bytes || !scale_bytes) return fail_without_handle(SAME_LDA_EINVAL, "micro_size: code_bytes or scale_bytes is null");
+    if (rows < 0 || rows >= (int64_t)1 << 31 || width < 1 || width > SAME_LDA_WIDTH_MAX)
+        return fail_without_handle(SAME_LDA_EINVAL, "micro_size: bad shape %lld x %d", (long long)rows, width);
+    *code_bytes = (size_t)rows * (size_t)same::micro_code_pitch(width);
+    *scale_bytes = (size_t)rows * (size_t)same::micro_scale_pitch(width);
+    return SAME_LDA_OK;
+}
+
+int same_lda_micro_quantize(const same_lda_rows* x, const same_lda_rows* micro_out, void* hip_stream)
+{
+    int rc = check_rows("micro_quantize", "x", x, 0);
+    if (!rc) rc = check_rows("micro_quantize", "micro_out", micro_out, 1);
+    if (rc) return rc;
+    if (x->rows != micro_out->rows || x->width != micro_out->width)
+        return fail_without_handle(SAME_LDA_EINVAL, "micro_quantize: %lld x %d into %lld x %d", (long long)x->rows, x->width, (long long)micro_out->rows, micro_out->width);
+    if (x->rows == 0) return SAME_LDA_OK;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const same_lda_rows whole = {x->data, nullptr, x->rows, x->stride, 8, x->type};       // alignment of rows, whatever their width
+    const same::QuantizeArgs a = {x->data, x->rows, x->stride, x->width, chunks_fit(&whole, 8), static_cast<uint8_t*>(micro_out->data), micro_out->scales};
+    const int64_t pieces = x->rows * same::micro_groups(x->width) * 16;
+    const dim3 grid((unsigned)at_most((pieces + 255) / 256, kMaxGroups));
+    switch (x->type) {
+        case SAME_LDA_FLOAT:  hipLaunchKernelGGL(same::micro_quantize_kernel<float>, grid, dim3(256), 0, st, a); break;
+        case SAME_LDA_BFLOAT: hipLaunchKernelGGL(same::micro_quantize_kernel<__bf16>, grid, dim3(256), 0, st, a); break;
+        default:              hipLaunchKernelGGL(same::micro_quantize_kernel<_Float16>, grid, dim3(256), 0, st, a); break;
+    }
+    return launched("micro_quantize");
+}
+
+int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* hip_stream)
+{
+    int rc = check_rows("micro_product", "a", a, 1);
+    if (!rc) rc = check_rows("micro_product", "b", b, 1);
+    if (rc) return rc;
+    if (a->width != b->width) return fail_without_handle(SAME_LDA_EINVAL, "micro_product: rows of %d and of %d elements", a->width, b->width);
+    if (b->rows == 0) return SAME_LDA_OK;                                                  // no columns: out is not looked at
+    if ((rc = check_rows("micro_product", "out", out, 0, INT32_MAX))) return rc;
+    if (out->rows != a->rows || out->width != b->rows)
+        return fail_without_handle(SAME_LDA_EINVAL, "micro_product: %lld rows by %lld rows do not give %lld x %d", (long long)a->rows, (long long)b->rows,
+                                   (long long)out->rows, out->width);
+    if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "micro_product: the scale must be finite");
+    if (a->rows == 0) return SAME_LDA_OK;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const int64_t ta = (a->rows + 63) / 64, tb = (b->rows + 63) / 64;
+    const same::ProductArgs p = {static_cast<const uint8_t*>(a->data), a->scales, static_cast<const uint8_t*>(b->data), b->scales, a->rows, b->rows,
+                                 (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, tb, ta * tb};
+    const dim3 grid((unsigned)at_most(p.tiles, kMaxGroups));
+    switch (out->type) {
+        case SAME_LDA_FLOAT:  hipLaunchKernelGGL(same::micro_product_kernel<float>, grid, dim3(256), 0, st, p); break;
+        case SAME_LDA_BFLOAT: hipLaunchKernelGGL(same::micro_product_kernel<__bf16>, grid, dim3(256), 0, st, p); break;
+        default:              hipLaunchKernelGGL(same::micro_product_kernel<_Float16>, grid, dim3(256), 0, st, p); break;
+    }
+    return launched("micro_product");
+}
+
+}  // extern "C"
