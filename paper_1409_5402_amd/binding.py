@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 
 import numpy as np
@@ -40,10 +41,6 @@ class SameLdaError(RuntimeError):
 class _Csc(Structure):
     _fields_ = [("D", c_int32), ("V", c_int32), ("nnz", c_int64), ("colptr", c_void_p),
                 ("rowidx", c_void_p), ("val", c_void_p), ("on_device", c_int32)]
-
-
-class _Rows(Structure):
-    _fields_ = [("data", c_void_p), ("scales", c_void_p), ("rows", c_int64), ("stride", c_int64), ("width", c_int32), ("type", c_int32)]
 
 
 _lib = None
@@ -86,12 +83,12 @@ def load(path: str | None = None) -> ctypes.CDLL:
         L.same_lda_sddmm.argtypes = [c_void_p, c_void_p, c_int32]
         L.same_lda_vb_exp_elog_beta.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
         L.same_lda_vb_estep.argtypes = [c_void_p, c_void_p, c_void_p, c_float, c_int32, c_void_p, c_void_p]
-        L.same_lda_embed.argtypes = [POINTER(_Rows), c_void_p, c_int32, c_float, POINTER(_Rows), c_void_p]
-        L.same_lda_embed_grad_workspace.argtypes = [POINTER(_Rows), POINTER(_Rows), POINTER(c_size_t)]
-        L.same_lda_embed_grad.argtypes = [POINTER(_Rows), c_void_p, c_int32, c_float, c_int32, POINTER(_Rows), c_void_p, c_size_t, c_void_p]
+        L.same_lda_embed.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_void_p, c_void_p]
+        L.same_lda_embed_grad_workspace.argtypes = [c_void_p, c_void_p, POINTER(c_size_t)]
+        L.same_lda_embed_grad.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
         L.same_lda_micro_size.argtypes = [c_int64, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
-        L.same_lda_micro_quantize.argtypes = [POINTER(_Rows), POINTER(_Rows), c_void_p]
-        L.same_lda_micro_product.argtypes = [POINTER(_Rows), POINTER(_Rows), c_float, POINTER(_Rows), c_void_p]
+        L.same_lda_micro_quantize.argtypes = [c_void_p, c_void_p, c_void_p]
+        L.same_lda_micro_product.argtypes = [c_void_p, c_void_p, c_float, c_void_p, c_void_p]
         L.same_lda_set_timing.argtypes = [c_void_p, c_int32]
         L.same_lda_get_timing.argtypes = [c_void_p, POINTER(c_double), POINTER(c_int64)]
         L.same_lda_selftest.argtypes = [POINTER(c_int64)]
@@ -330,23 +327,23 @@ class SameLDA:
 
 
 # ---- Word tables as an embedding.  These functions take torch tensors on one GPU, run on torch's current stream of that
-# GPU and return at once; what a call allocates (outputs, scratch) comes from torch's allocator.
-
-_types = None
-
-
-def _type_of(dtype) -> int:
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    t = _types.get(dtype)
-    if t is None:
-        raise TypeError(f"{dtype} is not one of float32, bfloat16 and float16")
-    return t
-
+# GPU and return at once; what a call allocates (outputs, scratch) comes from torch's allocator.  A call's own time on the host
+# counts where tokens come one by one, so operands are checked and passed on in few steps.
 
 MICRO = 3
+_pack_rows = struct.Struct("PPqqii").pack          # same_lda_rows, passed by the address of its bytes
+_torch = None
+_types = {}                                        # element types by torch's
+_library = None
+
+
+def _setup():
+    """torch and the library, at the first call of an operator."""
+    global _torch, _types, _library
+    import torch
+    _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    _library = load()
+    _torch = torch
 
 
 class MicroMatrix:
@@ -356,12 +353,13 @@ class MicroMatrix:
     __slots__ = ("codes", "scales", "width", "rows")
 
     def __init__(self, codes, scales, width):
-        import torch
+        if _torch is None:
+            _setup()
         width = int(width)
         groups = -(-width // 128)
         rows = codes.shape[0]
-        if (width < 1 or codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(codes.shape) != (rows, 64 * groups)
-                or tuple(scales.shape) != (rows, 4 * groups) or not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device):
+        if (width < 1 or codes.dtype != _torch.uint8 or scales.dtype != _torch.uint8 or codes.shape != (rows, 64 * groups)
+                or scales.shape != (rows, 4 * groups) or not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device):
             raise ValueError(f"rows of {width} elements need contiguous uint8 codes [rows, {64 * groups}] and scales [rows, {4 * groups}] on one device")
         self.codes, self.scales, self.width, self.rows = codes, scales, width, rows
 
@@ -373,6 +371,9 @@ class MicroMatrix:
     def device(self):
         return self.codes.device
 
+    def get_device(self):
+        return self.codes.get_device()
+
     def __getitem__(self, rows):
         """A range of rows (a slice without a step), not copied."""
         if not isinstance(rows, slice) or rows.step not in (None, 1):
@@ -380,60 +381,55 @@ class MicroMatrix:
         return MicroMatrix(self.codes[rows], self.scales[rows], self.width)
 
 
-def _rows(x) -> _Rows:
-    if isinstance(x, MicroMatrix):
-        return _Rows(x.codes.data_ptr() or None, x.scales.data_ptr() or None, x.rows, x.width, x.width, MICRO)
+def _rows(x) -> bytes:
+    """A matrix as a same_lda_rows."""
+    if type(x) is MicroMatrix:
+        return _pack_rows(x.codes.data_ptr(), x.scales.data_ptr(), x.rows, x.width, x.width, MICRO)
+    kind = _types.get(x.dtype)
+    if kind is None:
+        raise TypeError(f"{x.dtype} is not one of float32, bfloat16 and float16")
     if x.dim() != 2:
         raise ValueError(f"a matrix has two dimensions, not {x.dim()}")
     rows, width = x.shape
     stride, inner = x.stride()
     if inner != 1 and width > 1 or stride < width and rows > 1:
         raise ValueError("the elements of a row must be contiguous and rows must not overlap")
-    return _Rows(x.data_ptr() or None, None, rows, stride if rows > 1 else width, width, _type_of(x.dtype))
+    return _pack_rows(x.data_ptr(), 0, rows, stride if rows > 1 else width, width, kind)
 
 
-class _On:
-    """The GPU that the operands live on as the current one, and torch's stream there."""
-
-    __slots__ = ("device", "before", "stream")
-
-    def __init__(self, *operands):
-        self.device = operands[0].device
-        for x in operands:
-            if x.device != self.device or x.device.type != "cuda":
-                raise ValueError(f"all operands must be on one GPU (got {[str(y.device) for y in operands]})")
-
-    def __enter__(self):
-        import torch
-        self.before = torch.cuda.current_device()
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.device)
-        return torch.cuda.current_stream(self.device).cuda_stream or None
-
-    def __exit__(self, *_):
-        if self.before != self.device.index:
-            import torch
-            torch.cuda.set_device(self.before)
+def _gpu(*operands) -> int:
+    """The number of the GPU that all operands are on."""
+    index = operands[0].get_device()
+    for x in operands:
+        if x is not None and (x.get_device() != index or index < 0):
+            raise ValueError(f"all operands must be on one GPU (got {[str(y.device) for y in operands if y is not None]})")
+    return index
 
 
-def _done(rc):
+def _run(index, call, *arguments):
+    """One call of the library on torch's stream of GPU `index`, which is the current one meanwhile."""
+    if _torch._C._cuda_getDevice() == index:
+        rc = call(*arguments, _torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with _torch.cuda.device(index):
+            rc = call(*arguments, _torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
-        raise SameLdaError(rc, load().same_lda_last_error(None).decode())
+        raise SameLdaError(rc, _library.same_lda_last_error(None).decode())
 
 
 def _token_ids(tokens):
-    import torch
-    if tokens.dtype not in (torch.int32, torch.int64):
+    if _torch is None:
+        _setup()
+    if tokens.dtype is not _torch.int64 and tokens.dtype is not _torch.int32:
         raise TypeError(f"tokens are int32 or int64, not {tokens.dtype}")
-    return tokens.contiguous()
+    return tokens if tokens.is_contiguous() else tokens.contiguous()
 
 
-def _output(out, shape, dtype, device):
-    import torch
+def _output(out, shape, dtype, default, device):
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape) or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype}")
+        return _torch.empty(shape, dtype=dtype or default, device=device)
+    if out.shape != shape or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype or out.dtype}")
     return out
 
 
@@ -442,72 +438,66 @@ def embed(table, tokens, scale=1.0, dtype=None, out=None):
     `dtype` (default: the table's, float32 for a MicroMatrix).  An id outside the table (padding) gives zeros.  `out`: a tensor of
     shape tokens.shape + (width,) whose leading dimensions can be viewed as one."""
     ids = _token_ids(tokens)
-    with _On(table, ids, *(() if out is None else (out,))) as stream:
-        if dtype is None and out is None:
-            import torch
-            dtype = torch.float32 if isinstance(table, MicroMatrix) else table.dtype
-        out = _output(out, (*tokens.shape, table.shape[1]), dtype, ids.device)
-        flat = out if out.dim() == 2 else out.view(-1, out.shape[-1])
-        if ids.numel():
-            _done(load().same_lda_embed(byref(_rows(table)), ids.data_ptr(), ids.element_size(), scale, byref(_rows(flat)), stream))
+    index = _gpu(ids, table, out)
+    out = _output(out, (*tokens.shape, table.shape[1]), dtype, _torch.float32 if type(table) is MicroMatrix else table.dtype, ids.device)
+    flat = out if out.dim() == 2 else out.view(-1, out.shape[-1])
+    _run(index, _library.same_lda_embed, _rows(table), ids.data_ptr() if ids.numel() else _EMPTY, ids.element_size(), scale, _rows(flat))
     return out
+
+
+_EMPTY = 16        # stands for the address of a list of no tokens: not null, never read
 
 
 def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumulate=False):
     """The gradient of ``embed(table, tokens, scale)`` with respect to a table of `rows` rows, from that of its result: `grad`
     of shape tokens.shape + (width,).  `dtype` (default: grad's) is the result's type.  `out`: where it is written, or added to with
     ``accumulate=True``; `rows` is then out's.  Equal calls give equal bits."""
-    import torch
     ids = _token_ids(tokens)
-    if tuple(grad.shape[:-1]) != tuple(tokens.shape):
+    if grad.shape[:-1] != tokens.shape:
         raise ValueError(f"grad has shape {tuple(grad.shape)}, tokens {tuple(tokens.shape)}")
-    if accumulate and out is None:
-        raise ValueError("accumulate needs out")
-    if rows is None:
-        if out is None:
-            raise ValueError("rows or out must say how many rows the table has")
-        rows = out.shape[0]
-    with _On(grad, ids, *(() if out is None else (out,))) as stream:
-        out = _output(out, (int(rows), grad.shape[-1]), grad.dtype if dtype is None and out is None else dtype, ids.device)
-        flat = grad if grad.dim() == 2 else grad.reshape(-1, grad.shape[-1])
-        g, o = _rows(flat), _rows(out)
-        n = c_size_t()
-        L = load()
-        _done(L.same_lda_embed_grad_workspace(byref(g), byref(o), byref(n)))
-        space = torch.empty(n.value, dtype=torch.uint8, device=ids.device)
-        _done(L.same_lda_embed_grad(byref(g), ids.data_ptr() or None, ids.element_size(), scale, 1 if accumulate else 0, byref(o), space.data_ptr() or None, n.value, stream))
+    if out is None and (accumulate or rows is None):
+        raise ValueError("accumulate needs out" if accumulate else "rows or out must say how many rows the table has")
+    index = _gpu(ids, grad, out)
+    out = _output(out, (out.shape[0] if rows is None else int(rows), grad.shape[-1]), dtype, grad.dtype, ids.device)
+    g, o = _rows(grad if grad.dim() == 2 else grad.reshape(-1, grad.shape[-1])), _rows(out)
+    n = c_size_t()
+    if _library.same_lda_embed_grad_workspace(g, o, byref(n)):
+        raise SameLdaError(-1, _library.same_lda_last_error(None).decode())
+    space = _torch.empty(n.value, dtype=_torch.uint8, device=ids.device)
+    _run(index, _library.same_lda_embed_grad, g, ids.data_ptr() if ids.numel() else _EMPTY, ids.element_size(), scale, 1 if accumulate else 0, o,
+         space.data_ptr(), n.value)
     return out
 
 
 def micro_quantize(x, out=None) -> MicroMatrix:
     """A matrix in microscaled four-bit floating point."""
-    import torch
-    with _On(x, *(() if out is None else (out,))) as stream:
-        r = _rows(x)
-        if out is None:
-            groups = -(-r.width // 128)
-            out = MicroMatrix(torch.empty(r.rows, 64 * groups, dtype=torch.uint8, device=x.device),
-                              torch.empty(r.rows, 4 * groups, dtype=torch.uint8, device=x.device), r.width)
-        _done(load().same_lda_micro_quantize(byref(r), byref(_rows(out)), stream))
+    if _torch is None:
+        _setup()
+    index = _gpu(x, out)
+    r = _rows(x)
+    if out is None:
+        rows, width = x.shape
+        groups = -(-width // 128)
+        device = x.device
+        out = MicroMatrix(_torch.empty((rows, 64 * groups), dtype=_torch.uint8, device=device), _torch.empty((rows, 4 * groups), dtype=_torch.uint8, device=device), width)
+    _run(index, _library.same_lda_micro_quantize, r, _rows(out))
     return out
 
 
 def micro_dequantize(q, dtype=None, out=None):
     """The numbers that a MicroMatrix stands for, in `dtype` (default: float32)."""
-    import torch
-    with _On(q, *(() if out is None else (out,))) as stream:
-        out = _output(out, q.shape, torch.float32 if dtype is None and out is None else dtype, q.device)
-        _done(load().same_lda_embed(byref(_rows(q)), None, 8, 1.0, byref(_rows(out)), stream))
+    index = _gpu(q, out)
+    out = _output(out, q.shape, dtype, _torch.float32, q.device)
+    _run(index, _library.same_lda_embed, _rows(q), None, 8, 1.0, _rows(out))
     return out
 
 
 def micro_product(a, b, scale=1.0, dtype=None, out=None):
     """scale * a @ b.T in `dtype` (default: float32) for a MicroMatrix `b`; `a` is a MicroMatrix, or a matrix that is rounded to
     one first."""
-    import torch
-    if not isinstance(a, MicroMatrix):
+    if type(a) is not MicroMatrix:
         a = micro_quantize(a)
-    with _On(a, b, *(() if out is None else (out,))) as stream:
-        out = _output(out, (a.rows, b.rows), torch.float32 if dtype is None and out is None else dtype, a.device)
-        _done(load().same_lda_micro_product(byref(_rows(a)), byref(_rows(b)), scale, byref(_rows(out)), stream))
+    index = _gpu(a, b, out)
+    out = _output(out, (a.rows, b.rows), dtype, _torch.float32, a.codes.device)
+    _run(index, _library.same_lda_micro_product, _rows(a), _rows(b), scale, _rows(out))
     return out

@@ -175,6 +175,27 @@ int check_grad(const same_lda_rows* grad, const same_lda_rows* table_grad)
     return rc;
 }
 
+template <class TO, int F>
+void product_tiles(same::ProductArgs& p, hipStream_t st)
+{
+    p.tiles_a = (p.rows_a + 64 * F - 1) / (64 * F);
+    p.tiles_b = (p.rows_b + 64 * F - 1) / (64 * F);
+    hipLaunchKernelGGL((same::micro_product_kernel<TO, F>), dim3((unsigned)(p.tiles_a * p.tiles_b)), dim3(256), 0, st, p);
+}
+
+template <class TO>
+void product_to(same::ProductArgs& p, hipStream_t st)
+{
+    if (p.rows_a <= 16) {
+        p.tiles_b = (p.rows_b + 15) / 16;
+        hipLaunchKernelGGL(same::micro_product_few_kernel<TO>, dim3((unsigned)at_most((p.tiles_b + 3) / 4, kMaxGroups)), dim3(256), 0, st, p);
+        return;
+    }
+    const int64_t large = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
+    if (large >= 256 && p.groups >= 8) product_tiles<TO, 4>(p, st);
+    else                               product_tiles<TO, 2>(p, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -294,14 +315,12 @@ int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float
     if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "micro_product: the scale must be finite");
     if (a->rows == 0) return SAME_LDA_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const int64_t ta = (a->rows + 63) / 64, tb = (b->rows + 63) / 64;
-    const same::ProductArgs p = {static_cast<const uint8_t*>(a->data), a->scales, static_cast<const uint8_t*>(b->data), b->scales, a->rows, b->rows,
-                                 (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, tb, ta * tb};
-    const dim3 grid((unsigned)at_most(p.tiles, kMaxGroups));
+    same::ProductArgs p = {static_cast<const uint8_t*>(a->data), a->scales, static_cast<const uint8_t*>(b->data), b->scales, a->rows, b->rows,
+                           (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, 0, 0};
     switch (out->type) {
-        case SAME_LDA_FLOAT:  hipLaunchKernelGGL(same::micro_product_kernel<float>, grid, dim3(256), 0, st, p); break;
-        case SAME_LDA_BFLOAT: hipLaunchKernelGGL(same::micro_product_kernel<__bf16>, grid, dim3(256), 0, st, p); break;
-        default:              hipLaunchKernelGGL(same::micro_product_kernel<_Float16>, grid, dim3(256), 0, st, p); break;
+        case SAME_LDA_FLOAT:  product_to<float>(p, st); break;
+        case SAME_LDA_BFLOAT: product_to<__bf16>(p, st); break;
+        default:              product_to<_Float16>(p, st); break;
     }
     return launched("micro_product");
 }

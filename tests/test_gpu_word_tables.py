@@ -309,7 +309,7 @@ def test_product_matches_the_oracle(M, N, K, out):
     check()
 
 
-@pytest.mark.parametrize("M, N, K", PRODUCTS + [(3, 2000, 8192), (700, 900, 1100), (2048, 64, 320)])
+@pytest.mark.parametrize("M, N, K", PRODUCTS + [(3, 2000, 8192), (700, 900, 1100), (2048, 64, 320), (4100, 4150, 1100), (3900, 4300, 1200)])
 def test_product_of_small_numbers_is_exact(M, N, K):
     """Scales of one: every sum is a multiple of 1/4 below 2^22, exact in binary32 in any order; a wrong pairing of elements or
     blocks shows."""

@@ -1,7 +1,6 @@
 """Refusals of the word-table operators: everything here is found on the host, before any device call."""
 import ctypes
 
-import numpy as np
 import pytest
 import torch
 
@@ -12,8 +11,13 @@ F, B, H, M = 0, 1, 2, 3
 P = 1 << 20        # an address that is only looked at
 
 
+class Rows(ctypes.Structure):
+    """same_lda_rows, field by field."""
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("stride", ctypes.c_int64), ("width", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
 def rows(rows=4, width=8, type=F, stride=None, data=P, scales=None):
-    return binding._Rows(data, scales if scales is not None else (P if type == M else None), rows, width if stride is None else stride, width, type)
+    return Rows(data, scales if scales is not None else (P if type == M else None), rows, width if stride is None else stride, width, type)
 
 
 def refused(rc, *words):
@@ -147,4 +151,8 @@ def test_binding_refuses_what_it_cannot_pass_on():
         binding._rows(x.t())
     with pytest.raises(ValueError):
         binding._rows(x[0])
-    assert np.all([binding._rows(x[:, 2:7]).stride == 8, binding._rows(x[1:2, 2:7]).stride == 5])
+    for view, stride in ((x[:, 2:7], 8), (x[1:2, 2:7], 5)):
+        r = Rows.from_buffer_copy(binding._rows(view))
+        assert (r.data, r.scales, r.rows, r.stride, r.width, r.type) == (view.data_ptr(), None, view.shape[0], stride, 5, F)
+    r = Rows.from_buffer_copy(binding._rows(q))
+    assert (r.data, r.scales, r.rows, r.width, r.type) == (codes.data_ptr(), scales.data_ptr(), 4, 8, M)
