@@ -463,9 +463,9 @@ def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumul
     n = c_size_t()
     if _library.same_lda_embed_grad_workspace(g, o, byref(n)):
         raise SameLdaError(-1, _library.same_lda_last_error(None).decode())
-    space = _torch.empty(n.value, dtype=_torch.uint8, device=ids.device)
+    space = _torch.empty(n.value, dtype=_torch.uint8, device=ids.device) if n.value else None
     _run(index, _library.same_lda_embed_grad, g, ids.data_ptr() if ids.numel() else _EMPTY, ids.element_size(), scale, 1 if accumulate else 0, o,
-         space.data_ptr(), n.value)
+         space.data_ptr() if n.value else None, n.value)
     return out
 
 

@@ -63,9 +63,8 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a)
 // on the tokens alone (no atomics: two calls give the same bits).
 
 // Stable radix sort of the words by digits of `bits` bits (at most kDigitBits), least significant first.  A workgroup owns a
-// tile of consecutive tokens.  Per pass: counts per (digit, tile); their exclusive sum in that order; placement.
-constexpr int kTileTokens = 4096;
-constexpr int kTileRows = kTileTokens / 256;
+// tile of 256 * R consecutive tokens.  Per pass: counts per (digit, tile); for every digit their exclusive sum over the tiles;
+// placement, which adds up the digits before its own.
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 
@@ -75,19 +74,27 @@ __device__ __forceinline__ int32_t word_of(const Tokens& tokens, int64_t i, int6
     return t >= 0 && t < rows ? (int32_t)t : (int32_t)rows;
 }
 
-// keys null: the first pass takes the words from the tokens
-__global__ __launch_bounds__(256) void token_histogram(Tokens tokens, int64_t rows, const int32_t* __restrict__ keys, int64_t n, int shift, int bits,
+// A token on its way through the sort: its word and its place in the list, moved together (the scattered stores of a pass are what
+// it waits for, and one of 8 bytes costs what one of 4 does).
+struct alignas(8) Placed {
+    int32_t word, pos;
+};
+
+// from null: the first pass takes the words from the tokens
+template <int R>
+__global__ __launch_bounds__(256) void token_histogram(Tokens tokens, int64_t rows, const Placed* __restrict__ from, int64_t n, int shift, int bits,
                                                        uint32_t tiles, uint32_t* __restrict__ hist)
 {
     __shared__ uint32_t h[kDigits];
     const uint32_t digits = 1u << bits;
     for (uint32_t d = threadIdx.x; d < digits; d += 256) h[d] = 0u;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kTileTokens;
-    for (int j = 0; j < kTileRows; ++j) {
+    const int64_t first = (int64_t)blockIdx.x * (256 * R);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
         const int64_t i = first + (int64_t)j * 256 + threadIdx.x;
         if (i < n) {
-            const int32_t key = keys ? keys[i] : word_of(tokens, i, rows);
+            const int32_t key = from ? from[i].word : word_of(tokens, i, rows);
             atomicAdd(&h[((uint32_t)key >> shift) & (digits - 1u)], 1u);
         }
     }
@@ -95,69 +102,75 @@ __global__ __launch_bounds__(256) void token_histogram(Tokens tokens, int64_t ro
     for (uint32_t d = threadIdx.x; d < digits; d += 256) hist[(size_t)d * tiles + blockIdx.x] = h[d];
 }
 
-// exclusive sum in place, by one workgroup
-__global__ __launch_bounds__(1024) void token_offsets(uint32_t* __restrict__ hist, int64_t cells)
+// Workgroup d: the counts of digit d in every tile become the number of its tokens in the tiles before, total[d] their number.
+__global__ __launch_bounds__(256) void token_offsets(uint32_t* __restrict__ hist, uint32_t tiles, uint32_t* __restrict__ total)
 {
-    __shared__ uint32_t wave_total[16];
+    __shared__ uint32_t wave_total[4];
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    uint32_t* const mine = hist + (size_t)blockIdx.x * tiles;
     uint32_t base = 0;
-    for (int64_t first = 0; first < cells; first += 4096) {
-        const int64_t at = first + threadIdx.x * 4;
-        uint32_t x[4], mine = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { x[j] = at + j < cells ? hist[at + j] : 0u; mine += x[j]; }
-        uint32_t incl = mine;
+    for (uint32_t first = 0; first < tiles; first += 256) {
+        const uint32_t at = first + threadIdx.x, x = at < tiles ? mine[at] : 0u;
+        uint32_t incl = x;
         for (int o = 1; o < 64; o <<= 1) {
             const uint32_t up = __shfl_up(incl, o);
             if (lane >= o) incl += up;
         }
         if (lane == 63) wave_total[wv] = incl;
         __syncthreads();
-        uint32_t before = base, all = base;
-        for (int i = 0; i < 16; ++i) { if (i < wv) before += wave_total[i]; all += wave_total[i]; }
-        uint32_t run = before + incl - mine;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (at + j < cells) hist[at + j] = run;
-            run += x[j];
-        }
-        base = all;
+        uint32_t before = base;
+        for (int i = 0; i < 4; ++i) { if (i < wv) before += wave_total[i]; base += wave_total[i]; }
+        if (at < tiles) mine[at] = before + incl - x;
         __syncthreads();
     }
+    if (threadIdx.x == 0) total[blockIdx.x] = base;
 }
 
-// A token's place: the start of its (digit, tile) run, plus the tokens of the same digit in the waves before its own, in the
+// A token's place: the tokens of lower digits, those of its digit in the tiles before, in the waves before its own, in the
 // earlier rows of its wave and in the lower lanes of its row.
-__global__ __launch_bounds__(256) void token_place(Tokens tokens, int64_t rows, const int32_t* __restrict__ keys_in, const int32_t* __restrict__ pos_in,
-                                                   int64_t n, int shift, int bits, uint32_t tiles, const uint32_t* __restrict__ start,
-                                                   int32_t* __restrict__ keys_out, int32_t* __restrict__ pos_out)
+template <int R>
+__global__ __launch_bounds__(256) void token_place(Tokens tokens, int64_t rows, const Placed* __restrict__ from, int64_t n, int shift, int bits, uint32_t tiles, const uint32_t* __restrict__ start,
+                                                   const uint32_t* __restrict__ total, Placed* __restrict__ to)
 {
     __shared__ uint32_t cnt[4][kDigits];
+    __shared__ uint32_t wave_total[4];
     const uint32_t digits = 1u << bits;
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     for (uint32_t d = lane; d < digits; d += 64) cnt[wv][d] = 0u;
+    const uint32_t d0 = 2u * threadIdx.x;                          // a thread's two digits
+    const uint32_t t0 = d0 < digits ? total[d0] : 0u, t1 = d0 + 1u < digits ? total[d0 + 1u] : 0u;
+    uint32_t p0 = d0 < digits ? start[(size_t)d0 * tiles + blockIdx.x] : 0u, p1 = d0 + 1u < digits ? start[(size_t)(d0 + 1u) * tiles + blockIdx.x] : 0u;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kTileTokens + (int64_t)wv * (kTileRows * 64) + lane;
-    int32_t key[kTileRows], pos[kTileRows];
+    const int64_t first = (int64_t)blockIdx.x * (256 * R) + (int64_t)wv * (R * 64) + lane;
+    Placed x[R];
 #pragma unroll
-    for (int j = 0; j < kTileRows; ++j) {
+    for (int j = 0; j < R; ++j) {
         const int64_t i = first + (int64_t)j * 64;
         const bool in = i < n;
-        key[j] = in ? (keys_in ? keys_in[i] : word_of(tokens, i, rows)) : 0;
-        pos[j] = in ? (pos_in ? pos_in[i] : (int32_t)i) : 0;
-        if (in) atomicAdd(&cnt[wv][((uint32_t)key[j] >> shift) & (digits - 1u)], 1u);
+        x[j] = !in ? Placed{0, 0} : from ? from[i] : Placed{word_of(tokens, i, rows), (int32_t)i};
+        if (in) atomicAdd(&cnt[wv][((uint32_t)x[j].word >> shift) & (digits - 1u)], 1u);
     }
+    uint32_t incl = t0 + t1;
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t up = __shfl_up(incl, o);
+        if (lane >= o) incl += up;
+    }
+    if (lane == 63) wave_total[wv] = incl;
     __syncthreads();
-    for (uint32_t d = threadIdx.x; d < digits; d += 256) {
-        uint32_t p = start[(size_t)d * tiles + blockIdx.x];
-        for (int v = 0; v < 4; ++v) { const uint32_t c = cnt[v][d]; cnt[v][d] = p; p += c; }
-    }
+    uint32_t below_digit = incl - t0 - t1;
+    for (int i = 0; i < wv; ++i) below_digit += wave_total[i];
+    p0 += below_digit;
+    p1 += below_digit + t0;
+    if (d0 < digits)
+        for (int v = 0; v < 4; ++v) { const uint32_t c = cnt[v][d0]; cnt[v][d0] = p0; p0 += c; }
+    if (d0 + 1u < digits)
+        for (int v = 0; v < 4; ++v) { const uint32_t c = cnt[v][d0 + 1u]; cnt[v][d0 + 1u] = p1; p1 += c; }
     __syncthreads();
     const uint64_t below = (1ull << lane) - 1ull;
 #pragma unroll
-    for (int j = 0; j < kTileRows; ++j) {
+    for (int j = 0; j < R; ++j) {
         const bool in = first + (int64_t)j * 64 < n;
-        const uint32_t dgt = ((uint32_t)key[j] >> shift) & (digits - 1u);
+        const uint32_t dgt = ((uint32_t)x[j].word >> shift) & (digits - 1u);
         uint64_t peers = __ballot(in);                             // the lanes of this row that hold the same digit
         for (int bit = 0; bit < bits; ++bit) {
             const bool one = (dgt >> bit) & 1u;
@@ -168,35 +181,45 @@ __global__ __launch_bounds__(256) void token_place(Tokens tokens, int64_t rows, 
             const uint32_t rank = (uint32_t)__popcll((unsigned long long)(peers & below));
             const uint32_t p = cnt[wv][dgt] + rank;                // every peer reads the place before the first one moves it on
             if (rank == 0u) cnt[wv][dgt] = p + (uint32_t)__popcll((unsigned long long)peers);
-            if ((int64_t)p < n) {                                  // always true; keeps a wrong count from becoming a wild store
-                keys_out[p] = key[j];
-                pos_out[p] = pos[j];
-            }
+            if ((int64_t)p < n) to[p] = x[j];                      // always true; keeps a wrong count from becoming a wild store
         }
     }
 }
 
-// start[w] = first place of word w among the sorted tokens, rows + 1 entries (the last: the number of tokens of any word)
-__global__ __launch_bounds__(256) void word_runs(const int32_t* __restrict__ keys, int64_t n, int64_t rows, int32_t* __restrict__ start)
+// start[w] = first place of word w among the sorted tokens, rows + 1 entries (the last: the number of tokens of any word).  The
+// token at place p writes the entries of the words after its predecessor's up to its own, the end those after the last: a few each
+// where tokens are many, else the lanes of a wave share the long gaps.
+__global__ __launch_bounds__(256) void word_runs(const Placed* __restrict__ sorted, int64_t n, int64_t rows, int32_t* __restrict__ start)
 {
-    const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (w > rows) return;
-    int64_t lo = 0, hi = n;
-    while (lo < hi) { const int64_t mid = (lo + hi) >> 1; if (keys[mid] < (int32_t)w) lo = mid + 1; else hi = mid; }
-    start[w] = (int32_t)lo;
+    constexpr int64_t kOwn = 8;
+    const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    int64_t lo = 0, hi = -1;                                       // first and last word to write
+    if (p <= n) {
+        lo = p > 0 ? (int64_t)sorted[p - 1].word + 1 : 0;
+        hi = p < n ? sorted[p].word : rows;
+    }
+    for (int64_t w = lo; w <= hi && w < lo + kOwn; ++w) start[w] = (int32_t)p;
+    uint64_t wide = __ballot(hi - lo >= kOwn);
+    const int lane = threadIdx.x & 63;
+    while (wide) {
+        const int from = __builtin_ctzll(wide);
+        wide &= wide - 1ull;
+        const int64_t first = __shfl((long long)lo, from) + kOwn, last = __shfl((long long)hi, from), q = __shfl((long long)p, from);
+        for (int64_t w = first + lane; w <= last; w += 64) start[w] = (int32_t)q;
+    }
 }
 
 // A run of more than kLongRun tokens is cut at the multiples of kLongRun: group j sums the places [j, j + 1) * kLongRun of long
 // runs into two rows of partial sums (2j: the run that the range begins in, 2j + 1: a long run that starts behind the
 // range's first place; such a run goes on behind the range's end, so there is one at most).  Short runs are summed by
-// the group of their word.
-constexpr int kLongRun = 256;
+// the group of their word.  A sum takes its rows eight at a time, a trip to memory each: with 64 tokens the longest
+// chain is eight trips, with 256 the hottest words' chains were what a batch of 65,537 tokens waited for.
+constexpr int kLongRun = 64;
 
 struct GradArgs {
     const void* grad;
     int64_t stride;
-    const int32_t* pos;      // [n] sorted tokens: their places in the list
-    const int32_t* keys;     // [n] and their words
+    const Placed* sorted;    // [n]
     const int32_t* start;    // [rows + 1]
     int64_t rows;
     float scale;
@@ -206,34 +229,49 @@ struct GradArgs {
     float* partial;          // [2 * ranges][width]
     int64_t ranges;
     int32_t width, chunks, lanes_log2;
+    Tokens tokens;           // few tokens only: the list itself,
+    int32_t n;               // its length
+    int32_t words;           // and the words of a workgroup
 };
 
+// acc += the rows at places at(0) .. at(count - 1) of the list, count in [1, N]: all loads before the first addition (at(q) is a
+// place to read from for q >= count too)
+template <class TI, int V, int N, class At>
+__device__ __forceinline__ void add_rows(float (&acc)[V], const TI* __restrict__ from, int64_t stride, int count, At at)
+{
+    float x[N][V];
+#pragma unroll
+    for (int q = 0; q < N; ++q) load_chunk<TI, V>(x[q], from + (int64_t)at(q) * stride);
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = q < count ? acc[j] + x[q][j] : acc[j];
+}
+
+// By the 2^lanes_log2 lanes of a group, all of them active: a lane fetches one place of the run for all.
 template <class TI, int V>
 __device__ __forceinline__ void sum_run(float (&acc)[V], const GradArgs& a, int64_t lo, int64_t hi, int c)
 {
-    const TI* const from = static_cast<const TI*>(a.grad) + c * V;
-    int64_t p = lo;
-    for (; p + 4 <= hi; p += 4) {
-        float x[4][V];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) load_chunk<TI, V>(x[q], from + (int64_t)a.pos[p + q] * a.stride);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += x[q][j];
-    }
-    for (; p < hi; ++p) {
-        float x[V];
-        load_chunk<TI, V>(x, from + (int64_t)a.pos[p] * a.stride);
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += x[j];
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+    const TI* const from = static_cast<const TI*>(a.grad) + (int64_t)c * V;
+    for (int64_t base = lo; base < hi; base += lanes) {
+        const int here = hi - base < lanes ? (int)(hi - base) : lanes;
+        const int32_t mine = a.sorted[base + (lane < here ? lane : here - 1)].pos;
+        for (int q = 0; q < here; q += 8) {
+            const auto at = [&](int i) { return __shfl(mine, q + i < here ? q + i : here - 1, lanes); };
+            const int left = here - q;
+            if (left > 4)       add_rows<TI, V, 8>(acc, from, a.stride, left < 8 ? left : 8, at);
+            else if (left > 2)  add_rows<TI, V, 4>(acc, from, a.stride, left, at);
+            else if (left == 2) add_rows<TI, V, 2>(acc, from, a.stride, 2, at);
+            else                add_rows<TI, V, 1>(acc, from, a.stride, 1, at);
+        }
     }
 }
 
 template <class TO, int V>
 __device__ __forceinline__ void write_row(const GradArgs& a, int64_t w, int c, float (&acc)[V], bool any)
 {
-    TO* const to = static_cast<TO*>(a.out) + w * a.out_stride + c * V;
+    TO* const to = static_cast<TO*>(a.out) + w * a.out_stride + (int64_t)c * V;
     if (a.accumulate) {
         if (!any) return;
         float old[V];
@@ -251,60 +289,171 @@ template <class TI, class TO, int V>
 __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
 {
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int c = blockIdx.y * lanes + lane;
+    const int column = blockIdx.y * lanes + lane;
+    const bool mine = column < a.chunks;
+    const int c = mine ? column : a.chunks - 1;                     // lanes behind the row's end follow its last chunk and write nothing
     const int64_t item0 = ((int64_t)blockIdx.x << (8 - a.lanes_log2)) + (threadIdx.x >> a.lanes_log2);
-    if (c >= a.chunks) return;
     for (int64_t item = item0; item < a.ranges + a.rows; item += (int64_t)gridDim.x << (8 - a.lanes_log2)) {
         if (item < a.ranges) {
             const int64_t n = a.start[a.rows], lo = item * kLongRun;
             if (lo >= n) continue;
             const int64_t hi = lo + kLongRun < n ? lo + kLongRun : n;
-            const int32_t w0 = a.keys[lo], w1 = a.keys[hi - 1];
+            const int32_t w0 = a.sorted[lo].word, w1 = a.sorted[hi - 1].word;
             const int64_t s0 = a.start[w0], e0 = a.start[w0 + 1];
             if (e0 - s0 > kLongRun) {
                 float acc[V] = {};
                 sum_run<TI, V>(acc, a, lo, e0 < hi ? e0 : hi, c);
-                store_chunk<float, V>(a.partial + (size_t)(2 * item) * a.width + c * V, acc);
+                if (mine) store_chunk<float, V>(a.partial + (size_t)(2 * item) * a.width + (int64_t)c * V, acc);
             }
             const int64_t s1 = a.start[w1], e1 = a.start[w1 + 1];
             if (w1 != w0 && e1 - s1 > kLongRun) {
                 float acc[V] = {};
                 sum_run<TI, V>(acc, a, s1, hi, c);
-                store_chunk<float, V>(a.partial + (size_t)(2 * item + 1) * a.width + c * V, acc);
+                if (mine) store_chunk<float, V>(a.partial + (size_t)(2 * item + 1) * a.width + (int64_t)c * V, acc);
             }
         } else {
             const int64_t w = item - a.ranges, lo = a.start[w], hi = a.start[w + 1];
             if (hi - lo > kLongRun) continue;
             float acc[V] = {};
             sum_run<TI, V>(acc, a, lo, hi, c);
-            write_row<TO, V>(a, w, c, acc, hi > lo);
+            if (mine) write_row<TO, V>(a, w, c, acc, hi > lo);
         }
     }
 }
 
-// The row of the long run that starts in range blockIdx.x, if there is one: its partial sums in order.
-template <class TO, int V>
-__global__ __launch_bounds__(256) void embed_grad_join_kernel(GradArgs a)
+// The rows of the long runs that start in the ranges of a workgroup, one range per group of lanes: the partial sums of a run in
+// order.  A run of more than kLongJoin of them is left to the whole workgroup: its groups sum consecutive parts, then the
+// parts' sums are added in pairs, pairs of pairs and so on.  Groups are of few lanes (kJoinLanesLog2): the hottest word's partial sums (2 MB of a million
+// tokens of natural text at 256 elements) are then read by as many compute units as there are groups to a row.
+constexpr int kLongJoin = 32;
+constexpr int kJoinLanesLog2 = 3;
+
+// acc += rows first .. behind - 1 of the partial sums of a run: row 0 is `head`, row k is 2 (item + k)
+template <int V>
+__device__ __forceinline__ void add_partials(float (&acc)[V], const GradArgs& a, int64_t item, int64_t head, int64_t first, int64_t behind, int c)
 {
-    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int c = blockIdx.y * lanes + lane;
-    const int64_t item0 = ((int64_t)blockIdx.x << (8 - a.lanes_log2)) + (threadIdx.x >> a.lanes_log2);
-    if (c >= a.chunks) return;
+    for (int64_t r = first; r < behind; r += 8) {
+        const auto at = [&](int i) {
+            const int64_t k = r + i < behind ? r + i : behind - 1;
+            return (int32_t)(k == 0 ? head : 2 * (item + k));
+        };
+        add_rows<float, V, 8>(acc, a.partial + (int64_t)c * V, a.width, behind - r < 8 ? (int)(behind - r) : 8, at);
+    }
+}
+
+template <class TO, int V>
+__global__ __launch_bounds__(1024) void embed_grad_join_kernel(GradArgs a)
+{
+    __shared__ float part[512 * V];
+    __shared__ int32_t later[1024 / kLongJoin + 2];                 // ranges that a long join starts in: at least kLongJoin apart
+    __shared__ int32_t n_later;
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = 1024 >> a.lanes_log2;
+    const int column = blockIdx.y * lanes + lane;
+    const int c = column < a.chunks ? column : a.chunks - 1;
     const int64_t n = a.start[a.rows];
-    for (int64_t item = item0; item * kLongRun < n; item += (int64_t)gridDim.x << (8 - a.lanes_log2)) {
-        const int64_t first = item * kLongRun, behind = first + kLongRun < n ? first + kLongRun : n;
-        int32_t w = a.keys[behind - 1];
+    if (threadIdx.x == 0) n_later = 0;
+    __syncthreads();
+    const int64_t item = (int64_t)blockIdx.x * groups + group, first = item * kLongRun;
+    if (first < n) {
+        const int64_t behind = first + kLongRun < n ? first + kLongRun : n;
+        const int32_t w = a.sorted[behind - 1].word;
         const int64_t s = a.start[w], e = a.start[w + 1];
-        if (s < first || e - s <= kLongRun) continue;
-        float acc[V];
-        load_chunk<float, V>(acc, a.partial + (size_t)(s == first ? 2 * item : 2 * item + 1) * a.width + c * V);
-        for (int64_t r = item + 1; r * kLongRun < e; ++r) {
-            float x[V];
-            load_chunk<float, V>(x, a.partial + (size_t)(2 * r) * a.width + c * V);
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += x[j];
+        if (s >= first && e - s > kLongRun) {
+            const int64_t rows = (e - 1) / kLongRun - item + 1;
+            if (rows <= kLongJoin) {
+                float acc[V] = {};
+                add_partials<V>(acc, a, item, s == first ? 2 * item : 2 * item + 1, 0, rows, c);
+                if (column < a.chunks) write_row<TO, V>(a, w, c, acc, true);
+            } else if (lane == 0) {
+                later[atomicAdd(&n_later, 1)] = (int32_t)item;
+            }
         }
-        write_row<TO, V>(a, w, c, acc, true);
+    }
+    __syncthreads();
+    for (int q = 0; q < n_later; ++q) {
+        const int64_t it = later[q], from = it * kLongRun;
+        const int32_t w = a.sorted[from + kLongRun - 1].word;              // the run goes on behind its first range
+        const int64_t s = a.start[w], e = a.start[w + 1];
+        const int64_t rows = (e - 1) / kLongRun - it + 1, each = (rows + groups - 1) / groups;
+        const int64_t lo = group * each, hi = lo + each < rows ? lo + each : rows;
+        float acc[V] = {};
+        add_partials<V>(acc, a, it, s == from ? 2 * it : 2 * it + 1, lo, hi, c);
+for (int o = groups >> 1; o > 0; o >>= 1) {
+            if (group >= o && group < 2 * o)
+#pragma unroll
+                for (int j = 0; j < V; ++j) part[j * 512 + threadIdx.x - (o << a.lanes_log2)] = acc[j];
+            __syncthreads();
+            if (group < o)
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += part[j * 512 + threadIdx.x];
+            __syncthreads();
+        }
+        if (group == 0 && column < a.chunks) write_row<TO, V>(a, w, c, acc, true);
+    }
+}
+
+// Few tokens: one launch, no sort.  A workgroup owns `words` consecutive words, reads the whole list and keeps the places of
+// its words' tokens in order; a group of lanes then finds a word's places among them 2^lanes_log2 at a time.
+constexpr int kFewTokens = 2048;
+
+template <class TI, class TO, int V>
+__global__ __launch_bounds__(256) void embed_grad_few_kernel(GradArgs a)
+{
+    constexpr int kRows = kFewTokens / 256;
+    __shared__ uint32_t list[kFewTokens];                           // word - first word of the workgroup in the upper half, place in the lower
+    __shared__ uint32_t found[kRows][4];
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = 256 >> a.lanes_log2;
+    const int wv = threadIdx.x >> 6, wlane = threadIdx.x & 63;
+    const int64_t w0 = (int64_t)blockIdx.x * a.words;
+    const int64_t behind = w0 + a.words < a.rows ? w0 + a.words : a.rows;
+    int64_t t[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) t[j] = j * 256 + (int)threadIdx.x < a.n ? a.tokens.at(j * 256 + threadIdx.x) : -1;
+    uint64_t in[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        in[j] = __ballot(t[j] >= w0 && t[j] < behind);
+        if (wlane == 0) found[j][wv] = (uint32_t)__popcll((unsigned long long)in[j]);
+    }
+    __syncthreads();
+    uint32_t count = 0;
+#pragma unroll
+    for (int j = 0; j < kRows; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (v == wv && ((in[j] >> wlane) & 1ull))
+                list[count + (uint32_t)__popcll((unsigned long long)(in[j] & ((1ull << wlane) - 1ull)))] = (uint32_t)(t[j] - w0) << 16 | (uint32_t)(j * 256 + threadIdx.x);
+            count += found[j][v];
+        }
+    __syncthreads();
+
+    const int column = blockIdx.y * lanes + lane;
+    const bool mine = column < a.chunks;
+    const int c = mine ? column : a.chunks - 1;
+    const TI* const from = static_cast<const TI*>(a.grad) + (int64_t)c * V;
+    const uint64_t group_lanes = lanes == 64 ? ~0ull : ((1ull << lanes) - 1ull);
+    for (int word = group; word < a.words; word += groups) {        // words is a multiple of groups: all lanes stay
+        float acc[V] = {};
+        bool any = false;
+        for (uint32_t b = 0; b < count; b += lanes) {
+            const uint32_t entry = b + lane < count ? list[b + lane] : ~0u;
+            uint64_t hit = (__ballot(entry >> 16 == (uint32_t)word) >> (wlane - lane)) & group_lanes;
+            any |= hit != 0ull;
+            while (hit) {                                           // the group's own lanes agree on it
+                int32_t place[8];
+                int left = 0;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    place[q] = hit ? (int32_t)(list[b + (uint32_t)__builtin_ctzll(hit)] & 0xFFFFu) : place[q ? q - 1 : 0];
+                    left += hit != 0ull;
+                    hit &= hit - 1ull;
+                }
+                const auto at = [&](int i) { return place[i]; };
+                if (left > 2) add_rows<TI, V, 8>(acc, from, a.stride, left, at);
+                else          add_rows<TI, V, 2>(acc, from, a.stride, left, at);
+            }
+        }
+        if (mine && w0 + word < a.rows) write_row<TO, V>(a, w0 + word, c, acc, any);
     }
 }
 

@@ -107,30 +107,46 @@ int embed_to(same::EmbedArgs& a, const same_lda_rows* table, const same_lda_rows
 
 // Workspace of the gradient, in this order; every part starts at a multiple of 256 bytes.
 struct GradSpace {
-    size_t keys[2], pos[2], hist, start, partial, bytes;
+    size_t sorted[2], hist, total, start, partial, bytes;
     uint32_t tiles;
     int64_t ranges;
     int passes, bits;
+    bool small_tiles;
 };
+
+constexpr int kTileRows = 16, kSmallTileRows = 4;                    // rows of 256 tokens in a tile of the sort
+constexpr int64_t kSmallTiles = 1 << 22;                             // up to this many tokens the tiles are small
 
 GradSpace grad_space(int64_t n, int64_t rows, int32_t width)
 {
-    GradSpace s;
+    GradSpace s = {};
+    if (n <= same::kFewTokens) return s;
     size_t at = 0;
     const auto part = [&at](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     int bits = 1;
     while (((int64_t)1 << bits) <= rows) ++bits;                     // words 0 .. rows - 1, and rows for padding
     s.passes = (bits + same::kDigitBits - 1) / same::kDigitBits;
     s.bits = (bits + s.passes - 1) / s.passes;
-    s.tiles = (uint32_t)((n + same::kTileTokens - 1) / same::kTileTokens);
+    s.small_tiles = n <= kSmallTiles;
+    const int64_t tile = 256 * (s.small_tiles ? kSmallTileRows : kTileRows);
+    s.tiles = (uint32_t)((n + tile - 1) / tile);
     s.ranges = (n + same::kLongRun - 1) / same::kLongRun;
-    if (n <= same::kLongRun) s.ranges = 0;                           // no run can be long
-    for (int i = 0; i < 2; ++i) { s.keys[i] = part((size_t)n * 4); s.pos[i] = part((size_t)n * 4); }
+    for (int i = 0; i < 2; ++i) s.sorted[i] = part((size_t)n * sizeof(same::Placed));
     s.hist = part(((size_t)s.tiles << s.bits) * 4);
+    s.total = part(sizeof(uint32_t) << s.bits);
     s.start = part(((size_t)rows + 1) * 4);
     s.partial = part((size_t)s.ranges * 2 * (size_t)width * 4);
     s.bytes = at;
     return s;
+}
+
+template <int R>
+void sort_pass(const same::GradArgs& a, const GradSpace& s, int64_t n, int pass, uint32_t* hist, uint32_t* total, same::Placed* to, hipStream_t st)
+{
+    const int shift = pass * s.bits;
+    hipLaunchKernelGGL(same::token_histogram<R>, dim3(s.tiles), dim3(256), 0, st, a.tokens, a.rows, a.sorted, n, shift, s.bits, s.tiles, hist);
+    hipLaunchKernelGGL(same::token_offsets, dim3(1u << s.bits), dim3(256), 0, st, hist, s.tiles, total);
+    hipLaunchKernelGGL(same::token_place<R>, dim3(s.tiles), dim3(256), 0, st, a.tokens, a.rows, a.sorted, n, shift, s.bits, s.tiles, hist, total, to);
 }
 
 template <class TI, class TO, int V>
@@ -141,9 +157,21 @@ int grad_launch(same::GradArgs& a, hipStream_t st)
     const int64_t per = (int64_t)256 >> a.lanes_log2;
     const unsigned across = (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2);
     const int64_t most = kMaxGroups / across;                        // across <= SAME_LDA_WIDTH_MAX / 64
+    if (!a.start) {                                                  // few tokens
+        // as many words per workgroup as leave 2048 workgroups, 64 at most: a workgroup reads the whole list
+        int64_t words = a.rows * across / 2048 / per * per;
+        words = words < per ? per : at_most(words, per > 64 ? per : 64);
+        const int64_t least = ((a.rows + most - 1) / most + per - 1) / per * per;
+        words = words > least ? words : least;
+        a.words = (int32_t)words;
+        hipLaunchKernelGGL((same::embed_grad_few_kernel<TI, TO, V>), dim3((unsigned)((a.rows + words - 1) / words), across), dim3(256), 0, st, a);
+        return launched("embed_grad");
+    }
     hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V>), dim3((unsigned)at_most((a.ranges + a.rows + per - 1) / per, most), across), dim3(256), 0, st, a);
-    if (a.ranges > 0)
-        hipLaunchKernelGGL((same::embed_grad_join_kernel<TO, V>), dim3((unsigned)at_most((a.ranges + per - 1) / per, most), across), dim3(256), 0, st, a);
+    if (a.lanes_log2 > same::kJoinLanesLog2 && a.chunks <= 65535 << same::kJoinLanesLog2) a.lanes_log2 = same::kJoinLanesLog2;
+    const int64_t items = (int64_t)1024 >> a.lanes_log2;             // ranges of a workgroup
+    hipLaunchKernelGGL((same::embed_grad_join_kernel<TO, V>), dim3((unsigned)((a.ranges + items - 1) / items), (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2)),
+                       dim3(1024), 0, st, a);
     return launched("embed_grad");
 }
 
@@ -243,26 +271,27 @@ int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t t
     const int64_t n = grad->rows, rows = table_grad->rows;
     const GradSpace s = grad_space(n, rows, grad->width);
     if (rows == 0 || (n == 0 && accumulate)) return SAME_LDA_OK;
-    if (!workspace || workspace_bytes < s.bytes || (uintptr_t)workspace % 16)
+    if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes || (uintptr_t)workspace % 16))
         return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: needs %zu bytes of workspace aligned to 16 (got %zu)", s.bytes, workspace ? workspace_bytes : (size_t)0);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     char* const w = static_cast<char*>(workspace);
-    const same::Tokens t = {tokens, token_bytes == 8};
-    const int32_t *keys = nullptr, *pos = nullptr;
-    uint32_t* const hist = reinterpret_cast<uint32_t*>(w + s.hist);
-    int32_t* const start = reinterpret_cast<int32_t*>(w + s.start);
-    for (int i = 0; n > 0 && i < s.passes; ++i) {
-        int32_t* const keys_to = reinterpret_cast<int32_t*>(w + s.keys[i & 1]);
-        int32_t* const pos_to = reinterpret_cast<int32_t*>(w + s.pos[i & 1]);
-        hipLaunchKernelGGL(same::token_histogram, dim3(s.tiles), dim3(256), 0, st, t, rows, keys, n, i * s.bits, s.bits, s.tiles, hist);
-        hipLaunchKernelGGL(same::token_offsets, dim3(1), dim3(1024), 0, st, hist, (int64_t)s.tiles << s.bits);
-        hipLaunchKernelGGL(same::token_place, dim3(s.tiles), dim3(256), 0, st, t, rows, keys, pos, n, i * s.bits, s.bits, s.tiles, hist, keys_to, pos_to);
-        keys = keys_to; pos = pos_to;
+    same::GradArgs a = {grad->data, grad->stride, nullptr, nullptr, rows, scale, accumulate, table_grad->data, table_grad->stride,
+                        nullptr, s.ranges, grad->width, 0, 0, {tokens, token_bytes == 8}, (int32_t)n, 0};
+    if (n > same::kFewTokens) {
+        uint32_t* const hist = reinterpret_cast<uint32_t*>(w + s.hist);
+        uint32_t* const total = reinterpret_cast<uint32_t*>(w + s.total);
+        int32_t* const start = reinterpret_cast<int32_t*>(w + s.start);
+        for (int i = 0; i < s.passes; ++i) {
+            same::Placed* const to = reinterpret_cast<same::Placed*>(w + s.sorted[i & 1]);
+            if (s.small_tiles) sort_pass<kSmallTileRows>(a, s, n, i, hist, total, to, st);
+            else               sort_pass<kTileRows>(a, s, n, i, hist, total, to, st);
+            a.sorted = to;
+        }
+        hipLaunchKernelGGL(same::word_runs, dim3((unsigned)((n + 256) / 256)), dim3(256), 0, st, a.sorted, n, rows, start);
+        if ((rc = launched("embed_grad"))) return rc;
+        a.start = start;
+        a.partial = reinterpret_cast<float*>(w + s.partial);
     }
-    hipLaunchKernelGGL(same::word_runs, dim3((unsigned)((rows + 256) / 256)), dim3(256), 0, st, keys, n, rows, start);
-    if ((rc = launched("embed_grad"))) return rc;
-    same::GradArgs a = {grad->data, grad->stride, pos, keys, start, rows, scale, accumulate, table_grad->data, table_grad->stride,
-                        reinterpret_cast<float*>(w + s.partial), s.ranges, grad->width, 0, 0};
     switch (grad->type) {
         case SAME_LDA_FLOAT:  return grad_to<float>(a, grad, table_grad, st);
         case SAME_LDA_BFLOAT: return grad_to<__bf16>(a, grad, table_grad, st);

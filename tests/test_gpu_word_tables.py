@@ -2,8 +2,8 @@
 
 Tolerances.  u = 2^-24 is half a step of binary32, eps/2 half a step of the output's type (with its smallest subnormal over 2
 as the absolute floor).  A lookup is one product in binary32 and one rounding: u + eps/2.  A sum of m terms in binary32 in any order is
-off by at most m u times the sum of their magnitudes (to first order; 1.01 covers the rest); a run of more than 256 tokens is summed
-in pieces of 256, so m counts the terms of a piece and the pieces.  Then one product and one rounding: u + eps/2.
+off by at most m u times the sum of their magnitudes (to first order; 1.01 covers the rest); a run of more than 256 tokens may be
+summed in pieces, so m counts the terms of a piece and the pieces.  Then one product and one rounding: u + eps/2.
 Products of four-bit numbers are exact in binary32, and every addition of the matrix instruction is taken to be off by a whole
 step: 2 u per term.  Rounding to four bits and reading back are exact."""
 import numpy as np
@@ -137,7 +137,8 @@ def check_grad(G, t, V, scale, got, out, before=None):
 
 # one token, tiles of the sort and their borders, runs of every length up to several pieces, words in one, two and three digits
 @pytest.mark.parametrize("n, V, width", [(1, 1, 1), (1, 5000, 64), (2, 3, 65), (77, 2000, 50), (255, 1, 16), (256, 1, 16), (257, 1, 16), (513, 2, 24), (4095, 10, 3),
-                                         (4096, 300, 8), (4097, 511, 8), (4100, 512, 12), (9001, 70_000, 33), (20_000, 3, 130), (12_345, 300_000, 4), (30_000, 40, 257)])
+                                         (4096, 300, 8), (4097, 511, 8), (4100, 512, 12), (2048, 5000, 20), (2049, 700, 7), (63, 1, 8), (64, 2, 8),
+                                         (65, 1, 8), (9001, 70_000, 33), (20_000, 3, 130), (12_345, 300_000, 4), (30_000, 40, 257)])
 @pytest.mark.parametrize("kind", ["even", "skewed"])
 def test_embed_grad_matches_the_oracle(n, V, width, kind):
     rng = np.random.default_rng(n + V)

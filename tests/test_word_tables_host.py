@@ -72,10 +72,11 @@ def test_shapes_types_tokens_and_scales_are_refused():
     refused(L.same_lda_embed_grad(ref(a), P, 4, 1.0, 0, ref(rows(width=7)), P, 1 << 30, None), "elements")
     refused(L.same_lda_embed_grad(ref(m), P, 4, 1.0, 0, ref(a), P, 1 << 30, None), "must not be microscaled")
     refused(L.same_lda_embed_grad_workspace(ref(a), ref(a), None), "null")
-    assert L.same_lda_embed_grad_workspace(ref(a), ref(a), ref(n)) == 0 and n.value > 0
-    refused(L.same_lda_embed_grad(ref(a), P, 4, 1.0, 0, ref(a), P, n.value - 1, None), "workspace")
-    refused(L.same_lda_embed_grad(ref(a), P, 4, 1.0, 0, ref(a), None, n.value, None), "workspace")
-    refused(L.same_lda_embed_grad(ref(a), P, 4, 1.0, 0, ref(a), P + 8, n.value, None), "workspace")
+    many = rows(rows=50_000)
+    assert L.same_lda_embed_grad_workspace(ref(many), ref(a), ref(n)) == 0 and n.value > 0
+    refused(L.same_lda_embed_grad(ref(many), P, 4, 1.0, 0, ref(a), P, n.value - 1, None), "workspace")
+    refused(L.same_lda_embed_grad(ref(many), P, 4, 1.0, 0, ref(a), None, n.value, None), "workspace")
+    refused(L.same_lda_embed_grad(ref(many), P, 4, 1.0, 0, ref(a), P + 8, n.value, None), "workspace")
     refused(L.same_lda_micro_quantize(ref(m), ref(m), None), "must not be microscaled")
     refused(L.same_lda_micro_quantize(ref(a), ref(a), None), "must be microscaled")
     refused(L.same_lda_micro_quantize(ref(a), ref(rows(type=M, rows=5)), None), "into")
