@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "element.h"
 #include "micro_format.h"
@@ -78,177 +79,356 @@ struct ProductArgs {
     void* out;
     int64_t out_stride;
     int64_t tiles_a, tiles_b;
+    int32_t wide;            // 16 bytes of a row of out are aligned
 };
 
 __device__ __forceinline__ v8i fragment(v4i x) { return __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1); }
 
-// Few rows of a (at most 16): the table is read once, straight from memory into the operands of 16x16x128 instructions: lane l
-// gives block l / 16 of row l % 16 of a group of 128, so four lanes read the 64 bytes of a row's group.
-template <class TO>
+// Few rows of a (at most 16 * MF): the table is read once, straight from memory into the operands of 16x16x128 instructions: lane l
+// gives block l / 16 of row l % 16 of a group of 128, so four lanes read the 64 bytes of a row's group.  A wave takes 16 * RF
+// rows of the table; with KW = 4 the four waves of a workgroup take a quarter of the groups each and their sums are added in
+// order, so that long rows are in flight from more waves.
+template <int N>
+struct alignas(4) ScaleWords {
+    uint32_t v[N];
+};
+
+template <class TO, int MF, int RF, int KW>
 __global__ __launch_bounds__(256) void micro_product_few_kernel(ProductArgs p)
 {
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    constexpr int kUnroll = MF * RF >= 8 ? 2 : 4;                              // groups in flight
+    __shared__ v4f others[KW > 1 ? KW - 1 : 1][MF][RF][64];
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int64_t pitch = (int64_t)p.groups * 64, spitch = (int64_t)p.groups * 4;
-    const int64_t ra = r < p.rows_a ? r : p.rows_a - 1;                        // rows behind the last are computed from it and not written
-    const uint8_t* const fa = p.a + ra * pitch + g * 16;
-    const uint8_t* const sa = p.a_scales + ra * spitch + g;
-    for (int64_t tile = (int64_t)blockIdx.x * 4 + wv; tile < p.tiles_b; tile += (int64_t)gridDim.x * 4) {
-        const int64_t j = tile * 16 + r, rb = j < p.rows_b ? j : p.rows_b - 1;
-        const uint8_t* const fb = p.b + rb * pitch + g * 16;
-        const uint8_t* const sb = p.b_scales + rb * spitch + g;
-        v4f acc = {};
-        int k = 0;
-        for (; k + 4 <= p.groups; k += 4) {
-            v4i xa[4], xb[4];
-            int ea[4], eb[4];
+    const uint8_t* fa[MF];
+    const uint8_t* sa[MF];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                xb[q] = *reinterpret_cast<const v4i*>(fb + (int64_t)(k + q) * 64);
-                eb[q] = sb[(k + q) * 4];
-                xa[q] = *reinterpret_cast<const v4i*>(fa + (int64_t)(k + q) * 64);
-                ea[q] = sa[(k + q) * 4];
+    for (int f = 0; f < MF; ++f) {
+        const int64_t i = 16 * f + r < p.rows_a ? 16 * f + r : p.rows_a - 1;   // rows behind the last are computed from it and not written
+        fa[f] = p.a + i * pitch + g * 16;
+        sa[f] = p.a_scales + i * spitch;
+    }
+    const int each = (p.groups + KW - 1) / KW, part = KW > 1 ? wv : 0;
+    const int k0 = part * each, k1 = k0 + each < p.groups ? k0 + each : p.groups;
+    for (int64_t tile = (int64_t)blockIdx.x * (4 / KW) + (KW > 1 ? 0 : wv); tile < p.tiles_b; tile += (int64_t)gridDim.x * (4 / KW)) {
+        const uint8_t* fb[RF];
+        const uint8_t* sb[RF];
+#pragma unroll
+        for (int f = 0; f < RF; ++f) {
+            const int64_t j = (tile * RF + f) * 16 + r, row = j < p.rows_b ? j : p.rows_b - 1;
+            fb[f] = p.b + row * pitch + g * 16;
+            sb[f] = p.b_scales + row * spitch;
+        }
+        v4f acc[MF][RF] = {};
+        const auto groups = [&](int k, auto many) {
+            constexpr int N = decltype(many)::value;
+            v4i xa[N][MF], xb[N][RF];
+            ScaleWords<N> ea[MF], eb[RF];
+#pragma unroll
+            for (int f = 0; f < RF; ++f) {
+                eb[f] = *reinterpret_cast<const ScaleWords<N>*>(sb[f] + (int64_t)k * 4);
+#pragma unroll
+                for (int q = 0; q < N; ++q) xb[q][f] = *reinterpret_cast<const v4i*>(fb[f] + (int64_t)(k + q) * 64);
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(xa[q]), fragment(xb[q]), acc, kFormatE2M1, kFormatE2M1, 0, ea[q], 0, eb[q]);
-        }
-        for (; k < p.groups; ++k)
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(*reinterpret_cast<const v4i*>(fa + (int64_t)k * 64)),
-                                                                   fragment(*reinterpret_cast<const v4i*>(fb + (int64_t)k * 64)), acc, kFormatE2M1, kFormatE2M1, 0,
-                                                                   sa[k * 4], 0, sb[k * 4]);
+            for (int f = 0; f < MF; ++f) {
+                ea[f] = *reinterpret_cast<const ScaleWords<N>*>(sa[f] + (int64_t)k * 4);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int64_t i = 4 * g + v;
-            if (i < p.rows_a && j < p.rows_b) static_cast<TO*>(p.out)[i * p.out_stride + j] = (TO)(p.scale * acc[v]);
+                for (int q = 0; q < N; ++q) xa[q][f] = *reinterpret_cast<const v4i*>(fa[f] + (int64_t)(k + q) * 64);
+            }
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+#pragma unroll
+                for (int f = 0; f < MF; ++f)
+#pragma unroll
+                    for (int h = 0; h < RF; ++h)
+                        acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(xa[q][f]), fragment(xb[q][h]), acc[f][h], kFormatE2M1, kFormatE2M1,
+                                                                                     0, (int)(ea[f].v[q] >> (8 * g)), 0, (int)(eb[h].v[q] >> (8 * g)));
+        };
+        int k = k0;
+        for (; k + kUnroll <= k1; k += kUnroll) groups(k, std::integral_constant<int, kUnroll>());
+        for (; k < k1; ++k) groups(k, std::integral_constant<int, 1>());
+        if constexpr (KW > 1) {
+            __syncthreads();                                                   // the sums of the tile before have been read
+            if (wv > 0)
+#pragma unroll
+                for (int f = 0; f < MF; ++f)
+#pragma unroll
+                    for (int h = 0; h < RF; ++h) others[wv - 1][f][h][lane] = acc[f][h];
+            __syncthreads();
+            if (wv > 0) continue;
+#pragma unroll
+            for (int q = 0; q < KW - 1; ++q)
+#pragma unroll
+                for (int f = 0; f < MF; ++f)
+#pragma unroll
+                    for (int h = 0; h < RF; ++h) acc[f][h] += others[q][f][h][lane];
         }
+#pragma unroll
+        for (int f = 0; f < MF; ++f)
+#pragma unroll
+            for (int h = 0; h < RF; ++h)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int64_t i = 16 * f + 4 * g + v, j = (tile * RF + h) * 16 + r;
+                    if (i < p.rows_a && j < p.rows_b) static_cast<TO*>(p.out)[i * p.out_stride + j] = (TO)(p.scale * acc[f][h][v]);
+                }
     }
 }
 
-// Many rows: a workgroup of four waves (2 x 2) computes a tile of 64 F x 64 F sums, a wave a quarter of it as F x F sums of
-// 32 x 32 (32x32x64 instructions: lane l gives block l / 32 of row l % 32).  The rows' bytes come through LDS in stages of 256
-// elements, 128 bytes of codes and 8 of scales per row, straight from memory, one stage ahead of the one that is multiplied.
-// A row's eight blocks of 16 bytes are stored in the order block ^ ((row / 2) % 8): eight lanes write a row, and any eight
-// consecutive rows that are read at one block then lie in different banks.
+// Many rows: a workgroup of WM x WN waves computes a tile of (32 FM WM) x (32 FN WN) sums, a wave FM x FN sums of 32 x 32 of it
+// (32x32x64 instructions: lane l gives block l / 32 of row l % 32).  The rows' bytes come through LDS straight from memory.
+// Codes come in stages of two groups of 128 elements, 128 bytes of a row, one stage ahead of the one that is multiplied.  A row's
+// eight blocks of 16 bytes are stored in the order block ^ ((row / 2) % 8): eight lanes write a row, and any eight
+// consecutive rows that are read at one block then lie in different banks.  A row's scales are fetched for kScaleGroups
+// groups at once: what a compute unit's loads cost is the lines that they touch, and with 8 bytes per row and stage the
+// scales touched as many as the codes (8192 x 8192 x 8192: 303 us, then SCALES_US).
 constexpr int kStageGroups = 2;
 
-template <int F>
-struct ProductStage {
-    v4i codes[2 * 64 * F][8];
-    uint32_t scales[2 * 64 * F][2];
+template <int R, int kStages, int kScaleGroups>
+struct ProductSpace {
+    v4i codes[kStages][R][8];
+    uint32_t scales[kScaleGroups > kStageGroups ? 2 : kStages][R][kScaleGroups];
+    uint32_t ahead[kStages > 1 ? 512 : 1];                                     // what is fetched for the cache alone
 };
 
 // The tile of workgroup b: workgroups go to the eight dies in turn, and a die takes a run of consecutive tiles, eight tile rows
 // at a time and column by column, so that what runs on a die at once shares rows of both operands in its cache.
-__device__ __forceinline__ void tile_of(int64_t b, const ProductArgs& p, int64_t& ta, int64_t& tb)
+__device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_a, uint32_t tiles_b, uint32_t& ta, uint32_t& tb)
 {
-    const int64_t all = p.tiles_a * p.tiles_b, die = b & 7, each = all >> 3, more = all & 7;
-    const int64_t t = die * each + (die < more ? die : more) + (b >> 3);
-    const int64_t band = t / (8 * p.tiles_b), first = band * 8, in = p.tiles_a - first < 8 ? p.tiles_a - first : 8, at = t - first * p.tiles_b;
-    ta = first + at % in;
+    const uint32_t all = tiles_a * tiles_b, die = b & 7u, each = all >> 3, more = all & 7u;
+    const uint32_t t = die * each + (die < more ? die : more) + (b >> 3);
+    const uint32_t first = t / (8u * tiles_b) * 8u, in = tiles_a - first < 8u ? tiles_a - first : 8u, at = t - first * tiles_b;
     tb = at / in;
+    ta = first + at - tb * in;
 }
 
-template <class TO, int F>
-__global__ __launch_bounds__(256, F == 4 ? 1 : 2) void micro_product_kernel(ProductArgs p)
+// 16 or 4 bytes per lane from base + offset straight to consecutive places of LDS from `to` on.  Written as assembly because the
+// compiler takes the builtin for a store that any later read from LDS may depend on, and waits for it there: here the only
+// readers are behind arrived().  No register is written.
+__device__ __forceinline__ void to_lds_16(const uint8_t* base, uint32_t offset, const void* to)
 {
-    constexpr int kRows = 64 * F;                                              // of either operand in a tile
-    __shared__ ProductStage<F> stage0, stage1;
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "m0");
+}
+__device__ __forceinline__ void to_lds_4(const uint8_t* base, uint32_t offset, const void* to)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(at), "v"(offset), "s"(base) : "m0");
+}
+// f(0), f(1), ... f(N - 1), the argument a constant
+template <class F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
+
+// All of this wave's loads but the last N have come, then all waves'.
+template <int N>
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    __syncthreads();
+}
+
+// A wave's sums go out by way of LDS, 32 rows of its part of the tile at a time, so that a lane stores 16 bytes of one row.
+template <int FM, int FN, int WM, int WN>
+constexpr int kStripPitch = 32 * FN + 8;                                       // floats: the two halves of a wave write to different banks
+
+template <class TO, int FM, int FN, int WM, int WN, int kStages, int kScaleGroups>
+__global__ __launch_bounds__(64 * WM * WN, FM * FN * WM * WN > 16 ? WM * WN / 4 : kStages == 1 ? 4 : 2) void micro_product_kernel(ProductArgs p)
+{
+    constexpr int kW = WM * WN, kA = 32 * FM * WM, kB = 32 * FN * WN;          // waves, rows of a and of b
+    constexpr int kPitch = kStripPitch<FM, FN, WM, WN>;
+    union Space {
+        ProductSpace<kA + kB, kStages, kScaleGroups> in;
+        float strip[kW][32 * kPitch];
+    };
+    __shared__ Space space;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t pitch = (int64_t)p.groups * 64, spitch = (int64_t)p.groups * 4;
+    uint32_t ta, tb;
+    tile_of(blockIdx.x, (uint32_t)p.tiles_a, (uint32_t)p.tiles_b, ta, tb);
+    const int64_t i0 = (int64_t)ta * kA, j0 = (int64_t)tb * kB;
+    const int last_a = (int)(p.rows_a - i0 < kA ? p.rows_a - i0 : kA) - 1, last_b = (int)(p.rows_b - j0 < kB ? p.rows_b - j0 : kB) - 1;
     const int stages = (p.groups + kStageGroups - 1) / kStageGroups;
-    int64_t ta, tb;
-    tile_of(blockIdx.x, p, ta, tb);
-    const int64_t i0 = ta * kRows, j0 = tb * kRows;
-    const int last_a = (int)(p.rows_a - i0 < kRows ? p.rows_a - i0 : kRows) - 1, last_b = (int)(p.rows_b - j0 < kRows ? p.rows_b - j0 : kRows) - 1;
-    const uint8_t* const base_a = p.a + i0 * pitch;
-    const uint8_t* const base_b = p.b + j0 * pitch;
-    const uint8_t* const sbase_a = p.a_scales + i0 * spitch;
-    const uint8_t* const sbase_b = p.b_scales + j0 * spitch;
+    const bool odd = p.groups % kStageGroups;
 
-    // a wave's instruction fills 8 rows of codes or 32 rows of scales; rows behind the last are filled from it
+    // Codes: an instruction of a wave fills 8 rows.  Rows behind the last are filled from it.
+    constexpr int kCodeA = kA / (8 * kW), kCodes = (kA + kB) / (8 * kW);
+    static_assert(kA % (8 * kW) == 0 && kB % (8 * kW) == 0, "every wave fetches the same number of pieces of either operand");
     const int crow = wv * 8 + (lane >> 3), cblock = (lane & 7) ^ ((crow >> 1) & 7);
-    const int srow = wv * 32 + (lane >> 1);
-    const auto load = [&](ProductStage<F>& to, int st) {
-        const int group = st * kStageGroups;
-        const int c = group + (cblock >> 2) < p.groups ? cblock : cblock & 3;   // the last stage may hold one group: any bytes for the other
-        const int s = group + (lane & 1) < p.groups ? lane & 1 : 0;
+    uint32_t from[kCodes];
 #pragma unroll
-        for (int i = 0; i < 2 * F; ++i) {
-            const int row = i * 32 + crow;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base_a + (row < last_a ? row : last_a) * pitch + group * 64 + c * 16),
-                                             (__attribute__((address_space(3))) void*)&to.codes[i * 32 + wv * 8][0], 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base_b + (row < last_b ? row : last_b) * pitch + group * 64 + c * 16),
-                                             (__attribute__((address_space(3))) void*)&to.codes[kRows + i * 32 + wv * 8][0], 16, 0, 0);
-        }
+    for (int i = 0; i < kCodeA; ++i) from[i] = (uint32_t)min(i * 8 * kW + crow, last_a) * (uint32_t)pitch + cblock * 16;
 #pragma unroll
-        for (int i = 0; i < (F + 1) / 2; ++i) {
-            if (F % 2 && wv * 32 + i * 128 >= kRows) break;
-            const int row = i * 128 + srow;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(sbase_a + (row < last_a ? row : last_a) * spitch + group * 4 + s * 4),
-                                             (__attribute__((address_space(3))) void*)&to.scales[i * 128 + wv * 32][0], 4, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(sbase_b + (row < last_b ? row : last_b) * spitch + group * 4 + s * 4),
-                                             (__attribute__((address_space(3))) void*)&to.scales[kRows + i * 128 + wv * 32][0], 4, 0, 0);
+    for (int i = kCodeA; i < kCodes; ++i) from[i] = (uint32_t)min((i - kCodeA) * 8 * kW + crow, last_b) * (uint32_t)pitch + cblock * 16;
+    const uint8_t* const codes_a = p.a + i0 * pitch;
+    const uint8_t* const codes_b = p.b + j0 * pitch;
+    const auto load = [&](int st, auto which) {                                // instruction `which` of stage st
+        constexpr int i = decltype(which)::value;
+        auto& to = space.in.codes[st & (kStages - 1)];
+        if constexpr (i < kCodeA) to_lds_16(codes_a + (int64_t)st * 128, from[i], &to[i * 8 * kW + wv * 8][0]);
+        else                      to_lds_16(codes_b + (int64_t)st * 128, from[i], &to[kA + (i - kCodeA) * 8 * kW + wv * 8][0]);
+    };
+    // Before the last stage is loaded: where it holds one group, the lanes of the other fetch the first one's bytes again.
+    const auto last_stage_next = [&] {
+        if (!odd) return;
+#pragma unroll
+        for (int i = 0; i < kCodes; ++i) from[i] -= cblock >= 4 ? 64 : 0;
+    };
+
+    // Scales: pieces of kPiece groups of a row, a lane each; where the row ends inside a piece it is the row's last kPiece groups.
+    constexpr int kPiece = kScaleGroups > kStageGroups ? 4 : 1, kPieces = kScaleGroups / kPiece, kRowsAtOnce = 64 / kPieces;
+    static_assert((kA + kB) % (kRowsAtOnce * kW) == 0 && kA % kRowsAtOnce == 0, "");
+    const uint8_t* const scales_a = p.a_scales + i0 * spitch;
+    const uint8_t* const scales_b = p.b_scales + j0 * spitch;
+    const auto first_of_piece = [&](int g) { return min(g / kPiece * kPiece, p.groups - kPiece); };   // of the piece that holds group g
+    const auto load_scales = [&](int c) {                                      // groups c * kScaleGroups and on
+        auto& to = space.in.scales[c & (sizeof(space.in.scales) / sizeof(space.in.scales[0]) - 1)];
+        const int first = first_of_piece(c * kScaleGroups + (lane % kPieces) * kPiece);
+#pragma unroll
+        for (int i = 0; i < (kA + kB) / (kRowsAtOnce * kW); ++i) {
+            const int row0 = (i * kW + wv) * kRowsAtOnce, row = row0 + lane / kPieces;   // of a, then of b: the same for a whole wave
+            const uint32_t at = (uint32_t)(row0 < kA ? min(row, last_a) : min(row - kA, last_b)) * (uint32_t)spitch + (uint32_t)first * 4;
+            if constexpr (kPiece == 4) to_lds_16(row0 < kA ? scales_a : scales_b, at, &to[row0][0]);
+            else                       to_lds_4(row0 < kA ? scales_a : scales_b, at, &to[row0][0]);
         }
+    };
+
+    // A line of memory that no workgroup of the die has read yet takes as long as a stage's products, and all that share it wait.
+    // Every workgroup therefore touches some lines of a stage kAhead stages before it loads it: of a's rows the part that is its own
+    // among the kShareA tiles of a tile row that run on a die at once, of b's likewise.
+    constexpr int kAhead = 2, kShareA = 4, kShareB = 8, kTouchA = kA / (kShareA * kW), kTouchB = kB / (kShareB * kW);
+    static_assert(kTouchA + kTouchB <= 64, "");
+    const bool touch_a = lane < kTouchA;
+    const int touch_row = touch_a ? (int)(tb % kShareA) * (kTouchA * kW) + wv * kTouchA + lane : (int)(ta % kShareB) * (kTouchB * kW) + wv * kTouchB + (lane - kTouchA) % kTouchB;
+    const uint8_t* const touch_from = touch_a ? codes_a + min(touch_row, last_a) * pitch : codes_b + min(touch_row, last_b) * pitch;
+    const auto touch = [&](int st) {
+        const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)&space.in.ahead[wv * 64];
+        if (lane < kTouchA + kTouchB)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(touch_from + (int64_t)min(st, stages - 1) * 128) : "m0");
     };
 
     const int r = lane & 31, half = lane >> 5;
-    const int ra = (wv >> 1) * 32 * F + r, rb = kRows + (wv & 1) * 32 * F + r;   // rows of the stage that this lane multiplies (and every 32nd on)
+    const int wi = wv / WN * 32 * FM, wj = wv % WN * 32 * FN;                  // the wave's part of the tile
     const int turn = (r >> 1) & 7;
-    v16f acc[F][F] = {};
-    const auto multiply = [&](const ProductStage<F>& from, int steps) {
-        uint32_t ea[F][2], eb[F][2];                                           // bytes 0 and 2: this lane's blocks of two steps
+    v16f acc[FM][FN] = {};
+    constexpr int kSteps = 4, kReads = FM + FN, kRow = FM * FN;
+    uint32_t ea[FM][2], eb[FN][2];                                             // bytes 0 and 2: this lane's blocks of two steps
+    uint32_t words[kReads][2];                                                 // the next stage's as they are read
+    v4i xa[2][FM], xb[2][FN];                                                  // blocks of this step and the next
+    const auto fetch = [&](int st, int s, int q) {                             // read q of step s of a stage: first all that its first row of products needs
+        const auto& at = space.in.codes[st & (kStages - 1)];
+        if (q < FN) xb[s & 1][q] = at[kA + wj + 32 * q + r][(2 * s + half) ^ turn];
+        else        xa[s & 1][q - FN] = at[wi + 32 * (q - FN) + r][(2 * s + half) ^ turn];
+    };
+    const auto fetch_scales = [&](int st, int q) {
+        const int g = st * kStageGroups, h = min(g + 1, p.groups - 1), c = g / kScaleGroups;
+        const auto& at = space.in.scales[c & (sizeof(space.in.scales) / sizeof(space.in.scales[0]) - 1)];
+        const int row = q < FN ? kA + wj + 32 * q + r : wi + 32 * (q - FN) + r;
+        words[q][0] = at[row][g / kPiece * kPiece - c * kScaleGroups + g - first_of_piece(g)];
+        words[q][1] = at[row][h / kPiece * kPiece - c * kScaleGroups + h - first_of_piece(h)];
+    };
+    const auto exponents = [&](uint32_t keep) {                                // a second group that is not there counts 2^-254 times: nothing
 #pragma unroll
-        for (int f = 0; f < F; ++f)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                ea[f][w] = from.scales[ra + 32 * f][w] >> (8 * half);
-                eb[f][w] = from.scales[rb + 32 * f][w] >> (8 * half);
-            }
-        const auto step = [&](auto which) {
-            constexpr int s = decltype(which)::value;
-            v4i xa[F], xb[F];
-#pragma unroll
-            for (int f = 0; f < F; ++f) {
-                xa[f] = from.codes[ra + 32 * f][(2 * s + half) ^ turn];
-                xb[f] = from.codes[rb + 32 * f][(2 * s + half) ^ turn];
-            }
-#pragma unroll
-            for (int f = 0; f < F; ++f)
-#pragma unroll
-                for (int h = 0; h < F; ++h)
-                    acc[f][h] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fragment(xa[f]), fragment(xb[h]), acc[f][h], kFormatE2M1, kFormatE2M1,
-                                                                                (s & 1) * 2, (int)ea[f][s >> 1], (s & 1) * 2, (int)eb[h][s >> 1]);
-        };
-        step(std::integral_constant<int, 0>());
-        step(std::integral_constant<int, 1>());
-        if (steps > 2) {
-            step(std::integral_constant<int, 2>());
-            step(std::integral_constant<int, 3>());
+        for (int q = 0; q < kReads; ++q) {
+            uint32_t(&e)[2] = q < FN ? eb[q] : ea[q - FN];
+            e[0] = words[q][0] >> (8 * half);
+            e[1] = words[q][1] >> (8 * half) & keep;
         }
     };
-
-    load(stage0, 0);
-    for (int st = 0; st < stages; st += 2) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);                                    // vmcnt(0): this wave's part of the stage has come
-        __syncthreads();
-        if (st + 1 < stages) load(stage1, st + 1);
-        multiply(stage0, p.groups - st * kStageGroups > 1 ? 4 : 2);
-        if (st + 1 >= stages) break;
-        __builtin_amdgcn_s_waitcnt(0x0f70);
-        __syncthreads();
-        if (st + 2 < stages) load(stage0, st + 2);
-        multiply(stage1, p.groups - (st + 1) * kStageGroups > 1 ? 4 : 2);
-    }
-
-#pragma unroll
-    for (int f = 0; f < F; ++f)
-#pragma unroll
-        for (int h = 0; h < F; ++h)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int64_t i = i0 + (wv >> 1) * 32 * F + 32 * f + 8 * (v >> 2) + 4 * half + (v & 3), j = j0 + (wv & 1) * 32 * F + 32 * h + r;
-                if (i < p.rows_a && j < p.rows_b) static_cast<TO*>(p.out)[i * p.out_stride + j] = (TO)(p.scale * acc[f][h][v]);
+    const uint32_t keep_last = odd ? 0u : ~0u;
+    // Multiplies a stage in four steps of 64 elements, a product of 32 x 32 x 64 per slot; in the slots' shadows the blocks of the
+    // next step are read from LDS and with kMore the next stage is loaded.  In the middle of the last step the next stage has to have
+    // arrived: its first blocks are read before the last products are done, and every wave has read what the stage after it
+    // will overwrite.  A slot's product lasts 32 cycles, what stands beside it should not last longer.
+    const auto multiply = [&](int st, auto more) {
+        constexpr bool kMore = decltype(more)::value;
+        if constexpr (kMore) {
+            if (st + 2 == stages) last_stage_next();
+            const int g = (st + 1) * kStageGroups;                             // scales that no stage before the next needs
+            if constexpr (kScaleGroups > kStageGroups) {
+                if (st * kStageGroups % kScaleGroups == 0 && st * kStageGroups + kScaleGroups < p.groups) load_scales(st * kStageGroups / kScaleGroups + 1);
+            } else {
+                load_scales(g / kScaleGroups);
             }
+        }
+        each_of(std::make_integer_sequence<int, kSteps * kRow>(), [&](auto slot) {
+            constexpr int m = decltype(slot)::value, s = m / kRow, at = m % kRow, f = at / FN, h = at % FN;
+            if constexpr (s + 1 < kSteps) {
+                constexpr int q0 = at * kReads / kRow, q1 = (at + 1) * kReads / kRow;
+                each_of(std::make_integer_sequence<int, q1 - q0>(), [&](auto q) { fetch(st, s + 1, q0 + decltype(q)::value); });
+            }
+            if constexpr (kMore && m < 2 * kRow) {
+                constexpr int l0 = m * kCodes / (2 * kRow), l1 = (m + 1) * kCodes / (2 * kRow);
+                each_of(std::make_integer_sequence<int, l1 - l0>(), [&](auto q) { load(st + 1, std::integral_constant<int, l0 + decltype(q)::value>()); });
+            }
+            if constexpr (kMore && m == 2 * kRow) touch(st + 1 + kAhead);
+            if constexpr (kMore && s + 1 == kSteps) {
+                constexpr int kFrom = kRow / 2;
+                if constexpr (at == kFrom) arrived<1>();
+                if constexpr (at >= kFrom) {
+                    constexpr int q0 = (at - kFrom) * kReads / (kRow - kFrom), q1 = (at + 1 - kFrom) * kReads / (kRow - kFrom);
+                    each_of(std::make_integer_sequence<int, q1 - q0>(), [&](auto q) {
+                        fetch(st + 1, 0, q0 + decltype(q)::value);
+                        fetch_scales(st + 1, q0 + decltype(q)::value);
+                    });
+                }
+            }
+            acc[f][h] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fragment(xa[s & 1][f]), fragment(xb[s & 1][h]), acc[f][h], kFormatE2M1, kFormatE2M1,
+                                                                        (s & 1) * 2, (int)ea[f][s >> 1], (s & 1) * 2, (int)eb[h][s >> 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (kMore) exponents(st + 2 < stages ? ~0u : keep_last);
+    };
+    if (stages == 1) last_stage_next();
+    each_of(std::make_integer_sequence<int, kCodes>(), [&](auto i) { load(0, i); });
+    load_scales(0);
+    if constexpr (kStages > 1) {
+#pragma unroll
+        for (int st = 1; st <= kAhead; ++st) touch(st);
+        arrived<kAhead>();
+    } else {
+        arrived<0>();
+    }
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) fetch(0, 0, q);
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) fetch_scales(0, q);
+    exponents(stages > 1 ? ~0u : keep_last);
+    if constexpr (kStages > 1)
+        for (int st = 0; st + 1 < stages; ++st) multiply(st, std::true_type());
+    multiply(stages - 1, std::false_type());
+
+    __syncthreads();
+    float* const strip = space.strip[wv];
+    constexpr int V = 16 / sizeof(TO), kAcross = 32 * FN / V;                  // elements of a store, stores of a row
+    TO* const out = static_cast<TO*>(p.out) + (i0 + wi) * p.out_stride + j0 + wj;
+    const int64_t behind_i = p.rows_a - i0 - wi, behind_j = p.rows_b - j0 - wj;
+#pragma unroll
+    for (int f = 0; f < FM; ++f) {
+#pragma unroll
+        for (int h = 0; h < FN; ++h)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) strip[(8 * (v >> 2) + 4 * half + (v & 3)) * kPitch + 32 * h + r] = p.scale * acc[f][h][v];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (p.wide && behind_i >= 32 * FM && behind_j >= 32 * FN) {
+#pragma unroll
+            for (int q = 0; q < 32 * kAcross / 64; ++q) {
+                const int at = q * 64 + lane, row = at / kAcross, column = at % kAcross * V;
+                float x[V];
+                load_chunk<float, V>(x, strip + row * kPitch + column);
+                store_chunk<TO, V>(out + (32 * f + row) * p.out_stride + column, x);
+            }
+        } else {
+            for (int at = lane; at < 32 * 32 * FN; at += 64) {
+                const int row = at / (32 * FN), column = at % (32 * FN);
+                if (32 * f + row < behind_i && column < behind_j) out[(32 * f + row) * p.out_stride + column] = (TO)strip[row * kPitch + column];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
 }
 
 }  // namespace same

@@ -203,25 +203,43 @@ int check_grad(const same_lda_rows* grad, const same_lda_rows* table_grad)
     return rc;
 }
 
-template <class TO, int F>
+template <class TO, int FM, int FN, int WM, int WN, int kStages, int kScaleGroups>
 void product_tiles(same::ProductArgs& p, hipStream_t st)
 {
-    p.tiles_a = (p.rows_a + 64 * F - 1) / (64 * F);
-    p.tiles_b = (p.rows_b + 64 * F - 1) / (64 * F);
-    hipLaunchKernelGGL((same::micro_product_kernel<TO, F>), dim3((unsigned)(p.tiles_a * p.tiles_b)), dim3(256), 0, st, p);
+    p.tiles_a = (p.rows_a + 32 * FM * WM - 1) / (32 * FM * WM);
+    p.tiles_b = (p.rows_b + 32 * FN * WN - 1) / (32 * FN * WN);
+    hipLaunchKernelGGL((same::micro_product_kernel<TO, FM, FN, WM, WN, kStages, kScaleGroups>), dim3((unsigned)(p.tiles_a * p.tiles_b)), dim3(64 * WM * WN), 0, st, p);
 }
 
+template <class TO, int MF, int RF, int KW>
+void product_few(same::ProductArgs& p, hipStream_t st)
+{
+    p.tiles_b = (p.rows_b + 16 * RF - 1) / (16 * RF);
+    hipLaunchKernelGGL((same::micro_product_few_kernel<TO, MF, RF, KW>), dim3((unsigned)at_most((p.tiles_b + 4 / KW - 1) / (4 / KW), kMaxGroups)), dim3(256), 0, st, p);
+}
+
+template <class TO, int MF>
+void product_few_by_shape(same::ProductArgs& p, hipStream_t st)
+{
+    if (p.groups < 8)                product_few<TO, MF, 1, 1>(p, st);
+    else if (p.rows_b < 64 * 512)    product_few<TO, MF, 1, 4>(p, st);
+    else                             product_few<TO, MF, 4, 4>(p, st);
+}
+
+#ifndef PRODUCT_BIG
+#define PRODUCT_BIG product_tiles<TO, 4, 2, 2, 4, 2, 4>(p, st)
+#endif
 template <class TO>
 void product_to(same::ProductArgs& p, hipStream_t st)
 {
-    if (p.rows_a <= 16) {
-        p.tiles_b = (p.rows_b + 15) / 16;
-        hipLaunchKernelGGL(same::micro_product_few_kernel<TO>, dim3((unsigned)at_most((p.tiles_b + 3) / 4, kMaxGroups)), dim3(256), 0, st, p);
-        return;
-    }
+    if (p.rows_a <= 16) return product_few_by_shape<TO, 1>(p, st);
+    if (p.rows_a <= 32) return product_few_by_shape<TO, 2>(p, st);
+    if (p.rows_a <= 64) return product_few_by_shape<TO, 4>(p, st);
     const int64_t large = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
-    if (large >= 256 && p.groups >= 8) product_tiles<TO, 4>(p, st);
-    else                               product_tiles<TO, 2>(p, st);
+    if (large >= 256 && p.groups >= 8) PRODUCT_BIG;
+    else if (p.groups >= 4) product_tiles<TO, 2, 2, 2, 2, 2, 4>(p, st);
+    else if (p.groups > 2) product_tiles<TO, 2, 2, 2, 2, 2, 2>(p, st);
+    else                   product_tiles<TO, 2, 2, 2, 2, 1, 2>(p, st);
 }
 
 }  // namespace
@@ -345,7 +363,9 @@ int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float
     if (a->rows == 0) return SAME_LDA_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     same::ProductArgs p = {static_cast<const uint8_t*>(a->data), a->scales, static_cast<const uint8_t*>(b->data), b->scales, a->rows, b->rows,
-                           (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, 0, 0};
+                           (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, 0, 0, 0};
+    const same_lda_rows strip = {out->data, nullptr, out->rows, out->stride, 16 / element_bytes(out->type), out->type};   // alignment of rows, whatever their width
+    p.wide = chunks_fit(&strip, strip.width);
     switch (out->type) {
         case SAME_LDA_FLOAT:  product_to<float>(p, st); break;
         case SAME_LDA_BFLOAT: product_to<__bf16>(p, st); break;
