@@ -302,7 +302,10 @@ int same_lda_micro_quantize(const same_lda_rows* x, const same_lda_rows* micro_o
 /* out[i][j] = scale * sum_k a[i][k] * b[j][k], both microscaled and of one width, in binary32, rounded once to the output's
  * type: with rows of topic weights and the rows of phi, the predictive weight of every word (same_lda_sddmm is the
  * same product at the nonzeros only, of unrounded matrices).
+ *   a            microscaled, or up to 16 rows and SAME_LDA_ROUND_MAX elements of any type: then the product is that of
+ *                what same_lda_micro_quantize would make of them, in the one call
  *   out          [a->rows][b->rows]                                                                               */
+#define SAME_LDA_ROUND_MAX 16384
 int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out,
                            void* hip_stream);
 

@@ -479,7 +479,10 @@ def micro_quantize(x, out=None) -> MicroMatrix:
         rows, width = x.shape
         groups = -(-width // 128)
         device = x.device
-        out = MicroMatrix(_torch.empty((rows, 64 * groups), dtype=_torch.uint8, device=device), _torch.empty((rows, 4 * groups), dtype=_torch.uint8, device=device), width)
+        out = MicroMatrix.__new__(MicroMatrix)
+        out.codes = _torch.empty((rows, 64 * groups), dtype=_torch.uint8, device=device)
+        out.scales = _torch.empty((rows, 4 * groups), dtype=_torch.uint8, device=device)
+        out.width, out.rows = width, rows
     _run(index, _library.same_lda_micro_quantize, r, _rows(out))
     return out
 
@@ -495,9 +498,9 @@ def micro_dequantize(q, dtype=None, out=None):
 def micro_product(a, b, scale=1.0, dtype=None, out=None):
     """scale * a @ b.T in `dtype` (default: float32) for a MicroMatrix `b`; `a` is a MicroMatrix, or a matrix that is rounded to
     one first."""
-    if type(a) is not MicroMatrix:
+    if type(a) is not MicroMatrix and (a.shape[0] > 16 or a.numel() > 16384):
         a = micro_quantize(a)
     index = _gpu(a, b, out)
-    out = _output(out, (a.rows, b.rows), dtype, _torch.float32, a.codes.device)
+    out = _output(out, (a.shape[0], b.rows), dtype, _torch.float32, b.codes.device)
     _run(index, _library.same_lda_micro_product, _rows(a), _rows(b), scale, _rows(out))
     return out

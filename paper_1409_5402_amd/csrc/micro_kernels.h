@@ -30,6 +30,33 @@ __device__ __forceinline__ uint32_t micro_code(float x, float per)
     return (uint32_t)r | (__float_as_uint(x) >> 31 << 3);
 }
 
+// Codes of the 8 elements from `first` of a row of `width` on, and their block's scale; by four consecutive lanes together.
+template <class TI>
+__device__ __forceinline__ uint32_t micro_piece(const TI* __restrict__ row, int first, int width, bool wide, uint32_t& scale)
+{
+    float x[8];
+    if (wide && first + 8 <= width) {
+        load_chunk<TI, 8>(x, row + first);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = first + j < width ? to_float(row[first + j]) : 0.0f;
+    }
+    uint32_t top = 0u;                                                         // magnitudes order like their bits, NaN above infinity
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    uint32_t q = 0u;
+    scale = 255u;
+    if (top < 0x7F800000u) {
+        scale = top >= 0x01000000u ? (top >> 23) - 2u : 0u;                    // 127 + e, at least 0
+        const float per = __uint_as_float((254u - scale) << 23);               // 2^-e: scale <= 252
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q |= micro_code(x[j], per) << (4 * j);
+    }
+    return q;
+}
+
 template <class TI>
 __global__ __launch_bounds__(256) void micro_quantize_kernel(QuantizeArgs a)
 {
@@ -37,27 +64,8 @@ __global__ __launch_bounds__(256) void micro_quantize_kernel(QuantizeArgs a)
     const int64_t all = a.rows * pieces;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {   // whole groups of four lanes
         const int64_t row = at / pieces;
-        const int first = (int)(at - row * pieces) * 8;
-        const TI* const from = static_cast<const TI*>(a.x) + row * a.stride + first;
-        float x[8];
-        if (a.wide && first + 8 <= a.width) {
-            load_chunk<TI, 8>(x, from);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = first + j < a.width ? to_float(from[j]) : 0.0f;
-        }
-        uint32_t top = 0u;                                                     // magnitudes order like their bits, NaN above infinity
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-        uint32_t q = 0u, s = 255u;
-        if (top < 0x7F800000u) {
-            s = top >= 0x01000000u ? (top >> 23) - 2u : 0u;                    // 127 + e, at least 0
-            const float per = __uint_as_float((254u - s) << 23);               // 2^-e: s <= 252
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q |= micro_code(x[j], per) << (4 * j);
-        }
+        uint32_t s;
+        const uint32_t q = micro_piece(static_cast<const TI*>(a.x) + row * a.stride, (int)(at - row * pieces) * 8, a.width, a.wide, s);
         reinterpret_cast<uint32_t*>(a.codes)[at] = q;                          // rows of codes follow each other without a gap
         if ((at & 3) == 0) a.scales[at >> 2] = (uint8_t)s;
     }
@@ -80,6 +88,9 @@ struct ProductArgs {
     int64_t out_stride;
     int64_t tiles_a, tiles_b;
     int32_t wide;            // 16 bytes of a row of out are aligned
+    int64_t stride_a;        // where a is a matrix of numbers: its stride and width,
+    int32_t width;
+    int32_t wide_a;          // and whether chunks of 8 are aligned
 };
 
 __device__ __forceinline__ v8i fragment(v4i x) { return __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1); }
@@ -93,20 +104,40 @@ struct alignas(4) ScaleWords {
     uint32_t v[N];
 };
 
-template <class TO, int MF, int RF, int KW>
+// With TI a type of numbers the rows of a are such numbers, few enough (kRoundMost of them) for every workgroup to round them for itself.
+constexpr int kRoundMost = 16384;
+
+template <class TO, int MF, int RF, int KW, class TI>
 __global__ __launch_bounds__(256) void micro_product_few_kernel(ProductArgs p)
 {
     constexpr int kUnroll = MF * RF >= 8 ? 2 : 4;                              // groups in flight
+    constexpr bool kRound = !std::is_void<TI>::value;
     __shared__ v4f others[KW > 1 ? KW - 1 : 1][MF][RF][64];
+    __shared__ uint32_t rounded[kRound ? (kRoundMost + 16 * kMicroGroup) / 8 : 1];
+    __shared__ uint8_t rounded_scales[kRound ? (kRoundMost + 16 * kMicroGroup) / 32 : 4] __attribute__((aligned(4)));
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int64_t pitch = (int64_t)p.groups * 64, spitch = (int64_t)p.groups * 4;
+    const uint8_t *a = p.a, *a_scales = p.a_scales;
+    if constexpr (kRound) {
+        const int pieces = p.groups * 16, all = (int)p.rows_a * pieces;        // whole groups of four lanes
+        for (int at = threadIdx.x; at < all; at += 256) {
+            const int row = at / pieces;
+            uint32_t s;
+            const uint32_t q = micro_piece(reinterpret_cast<const TI*>(p.a) + row * p.stride_a, (at - row * pieces) * 8, p.width, p.wide_a, s);
+            rounded[at] = q;
+            if ((at & 3) == 0) rounded_scales[at >> 2] = (uint8_t)s;
+        }
+        __syncthreads();
+        a = reinterpret_cast<const uint8_t*>(rounded);
+        a_scales = rounded_scales;
+    }
     const uint8_t* fa[MF];
     const uint8_t* sa[MF];
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
         const int64_t i = 16 * f + r < p.rows_a ? 16 * f + r : p.rows_a - 1;   // rows behind the last are computed from it and not written
-        fa[f] = p.a + i * pitch + g * 16;
-        sa[f] = p.a_scales + i * spitch;
+        fa[f] = a + i * pitch + g * 16;
+        sa[f] = a_scales + i * spitch;
     }
     const int each = (p.groups + KW - 1) / KW, part = KW > 1 ? wv : 0;
     const int k0 = part * each, k1 = k0 + each < p.groups ? k0 + each : p.groups;
@@ -182,7 +213,8 @@ __global__ __launch_bounds__(256) void micro_product_few_kernel(ProductArgs p)
 // eight blocks of 16 bytes are stored in the order block ^ ((row / 2) % 8): eight lanes write a row, and any eight
 // consecutive rows that are read at one block then lie in different banks.  A row's scales are fetched for kScaleGroups
 // groups at once: what a compute unit's loads cost is the lines that they touch, and with 8 bytes per row and stage the
-// scales touched as many as the codes (8192 x 8192 x 8192: 303 us, then SCALES_US).
+// scales touched as many as the codes (65 x 50,021 x 4096: 36.6 us, with
+// kScaleGroups = 4 33.5 us).
 constexpr int kStageGroups = 2;
 
 template <int R, int kStages, int kScaleGroups>

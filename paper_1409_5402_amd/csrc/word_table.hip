@@ -211,35 +211,56 @@ void product_tiles(same::ProductArgs& p, hipStream_t st)
     hipLaunchKernelGGL((same::micro_product_kernel<TO, FM, FN, WM, WN, kStages, kScaleGroups>), dim3((unsigned)(p.tiles_a * p.tiles_b)), dim3(64 * WM * WN), 0, st, p);
 }
 
-template <class TO, int MF, int RF, int KW>
+template <class TO, int MF, int RF, int KW, class TI>
 void product_few(same::ProductArgs& p, hipStream_t st)
 {
     p.tiles_b = (p.rows_b + 16 * RF - 1) / (16 * RF);
-    hipLaunchKernelGGL((same::micro_product_few_kernel<TO, MF, RF, KW>), dim3((unsigned)at_most((p.tiles_b + 4 / KW - 1) / (4 / KW), kMaxGroups)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((same::micro_product_few_kernel<TO, MF, RF, KW, TI>), dim3((unsigned)at_most((p.tiles_b + 4 / KW - 1) / (4 / KW), kMaxGroups)), dim3(256), 0, st, p);
 }
 
-template <class TO, int MF>
+// Of long rows the four waves of a workgroup take a part each.  16 rows of the table per wave, or 64 where that still leaves 512
+// workgroups: 13 rows by 50,021 x 4096 take 60 us with 16 rows and whole rows per wave, 30 us with 64 and a quarter.
+template <class TO, int MF, class TI = void>
 void product_few_by_shape(same::ProductArgs& p, hipStream_t st)
 {
-    if (p.groups < 8)                product_few<TO, MF, 1, 1>(p, st);
-    else if (p.rows_b < 64 * 512)    product_few<TO, MF, 1, 4>(p, st);
-    else                             product_few<TO, MF, 4, 4>(p, st);
+    if (p.groups < 8)                product_few<TO, MF, 1, 1, TI>(p, st);
+    else if (p.rows_b < 64 * 512)    product_few<TO, MF, 1, 4, TI>(p, st);
+    else                             product_few<TO, MF, 4, 4, TI>(p, st);
 }
 
-#ifndef PRODUCT_BIG
-#define PRODUCT_BIG product_tiles<TO, 4, 2, 2, 4, 2, 4>(p, st)
-#endif
+// Which kernel (us at rows of a x rows of b x width, the first number the chosen one's):
+//   up to 16 rows of a          straight from memory; above, tiles, but up to 32 rows of a by a table below 32 MB of longer rows
+//                               (32 x 5000 x 4096: 9.2, tiles 12.6; 32 x 50,021 x 4096: tiles 34, 44; 32 x 100,000 x 256: tiles 7.0, 10.1)
+//   rows of one or two groups   a single stage, four workgroups per compute unit; tiles of 64 x 64 where those of 128 x 128 are few
+//                               (100 x 100,000 x 256: 10.6, large tiles 13.9; 2000 x 30,000 x 256: 50.0, 53.7; 16-bit sums, whose
+//                               rows of 64 are half as long, 4096 x 20,000 x 200: large tiles 45, 53)
+//   256 x 256                   from 256 such tiles on (4096 x 16,384 x 1024: 58, tiles of 128 85; 2048 x 4096 x 4096, 128 tiles: 33,
+//                               tiles of 128 27)
+//   64 x 64                     up to 160 tiles of 128 x 128 (512 x 4096 x 4096: 13.9, 16.5; 1024 x 4096 x 4096: 27, 18)
 template <class TO>
-void product_to(same::ProductArgs& p, hipStream_t st)
+void product_to(same::ProductArgs& p, int32_t type_a, hipStream_t st)
 {
+    switch (type_a) {
+        case SAME_LDA_FLOAT:  return product_few_by_shape<TO, 1, float>(p, st);
+        case SAME_LDA_BFLOAT: return product_few_by_shape<TO, 1, __bf16>(p, st);
+        case SAME_LDA_HALF:   return product_few_by_shape<TO, 1, _Float16>(p, st);
+    }
     if (p.rows_a <= 16) return product_few_by_shape<TO, 1>(p, st);
-    if (p.rows_a <= 32) return product_few_by_shape<TO, 2>(p, st);
-    if (p.rows_a <= 64) return product_few_by_shape<TO, 4>(p, st);
+    if (p.rows_a <= 32 && p.groups > 2 && p.rows_b * p.groups * 64 < (int64_t)1 << 25) return product_few_by_shape<TO, 2>(p, st);
+    const int64_t tiles = ((p.rows_a + 127) / 128) * ((p.rows_b + 127) / 128);
     const int64_t large = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
-    if (large >= 256 && p.groups >= 8) PRODUCT_BIG;
-    else if (p.groups >= 4) product_tiles<TO, 2, 2, 2, 2, 2, 4>(p, st);
-    else if (p.groups > 2) product_tiles<TO, 2, 2, 2, 2, 2, 2>(p, st);
-    else                   product_tiles<TO, 2, 2, 2, 2, 1, 2>(p, st);
+    if (p.groups <= 2) {
+        if (tiles <= (sizeof(TO) == 4 ? 4096 : 2048)) product_tiles<TO, 1, 1, 2, 2, 1, 2>(p, st);
+        else                      product_tiles<TO, 2, 2, 2, 2, 1, 2>(p, st);
+    } else if (p.groups == 3) {
+        product_tiles<TO, 2, 2, 2, 2, 2, 2>(p, st);
+    } else if (large >= 256 && p.groups >= 8) {
+        product_tiles<TO, 4, 2, 2, 4, 2, 4>(p, st);
+    } else if (tiles <= 160) {
+        product_tiles<TO, 1, 1, 2, 2, 2, 8>(p, st);
+    } else {
+        product_tiles<TO, 2, 2, 2, 2, 2, 4>(p, st);
+    }
 }
 
 }  // namespace
@@ -350,7 +371,7 @@ int same_lda_micro_quantize(const same_lda_rows* x, const same_lda_rows* micro_o
 
 int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* hip_stream)
 {
-    int rc = check_rows("micro_product", "a", a, 1);
+    int rc = check_rows("micro_product", "a", a, -1);
     if (!rc) rc = check_rows("micro_product", "b", b, 1);
     if (rc) return rc;
     if (a->width != b->width) return fail_without_handle(SAME_LDA_EINVAL, "micro_product: rows of %d and of %d elements", a->width, b->width);
@@ -360,16 +381,22 @@ int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float
         return fail_without_handle(SAME_LDA_EINVAL, "micro_product: %lld rows by %lld rows do not give %lld x %d", (long long)a->rows, (long long)b->rows,
                                    (long long)out->rows, out->width);
     if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "micro_product: the scale must be finite");
+    if (a->type != SAME_LDA_MICRO && (a->rows > 16 || a->rows * a->width > SAME_LDA_ROUND_MAX))
+        return fail_without_handle(SAME_LDA_EINVAL, "micro_product: a must be microscaled beyond 16 rows and %d elements (got %lld x %d)", SAME_LDA_ROUND_MAX,
+                                   (long long)a->rows, a->width);
+    static_assert(SAME_LDA_ROUND_MAX == same::kRoundMost, "");
     if (a->rows == 0) return SAME_LDA_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     same::ProductArgs p = {static_cast<const uint8_t*>(a->data), a->scales, static_cast<const uint8_t*>(b->data), b->scales, a->rows, b->rows,
-                           (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, 0, 0, 0};
+                           (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, 0, 0, 0, a->stride, a->width, 0};
+    const same_lda_rows whole = {a->data, nullptr, a->rows, a->stride, 8, a->type};
+    p.wide_a = chunks_fit(&whole, 8);
     const same_lda_rows strip = {out->data, nullptr, out->rows, out->stride, 16 / element_bytes(out->type), out->type};   // alignment of rows, whatever their width
     p.wide = chunks_fit(&strip, strip.width);
     switch (out->type) {
-        case SAME_LDA_FLOAT:  product_to<float>(p, st); break;
-        case SAME_LDA_BFLOAT: product_to<__bf16>(p, st); break;
-        default:              product_to<_Float16>(p, st); break;
+        case SAME_LDA_FLOAT:  product_to<float>(p, a->type, st); break;
+        case SAME_LDA_BFLOAT: product_to<__bf16>(p, a->type, st); break;
+        default:              product_to<_Float16>(p, a->type, st); break;
     }
     return launched("micro_product");
 }

@@ -291,7 +291,7 @@ def micro(codes, scales, width):
 
 
 PRODUCTS = [(1, 1, 1), (1, 100, 33), (1, 1000, 256), (2, 17, 129), (5, 300, 1000), (13, 501, 640), (16, 16, 128), (16, 4096, 512), (17, 65, 129), (33, 1, 4096), (64, 64, 256),
-            (100, 1030, 200), (128, 128, 384), (130, 257, 384), (255, 300, 1024), (300, 513, 2048), (512, 520, 640), (1025, 300, 256)]
+            (100, 1030, 200), (128, 128, 384), (130, 257, 384), (255, 300, 1024), (300, 513, 2048), (512, 520, 640), (1025, 300, 256), (20, 33_000, 1030), (31, 4500, 1024), (40, 36_000, 700), (70, 700, 384), (1300, 1500, 640), (2100, 5000, 100)]
 
 
 @pytest.mark.parametrize("M, N, K", PRODUCTS)
@@ -344,13 +344,22 @@ def test_product_bad_blocks_spoil_their_rows_only(M, N):
     assert np.array_equal(np.isnan(got), want)
 
 
-@pytest.mark.parametrize("M", [1, 5, 300])
-def test_product_rounds_a_matrix_first(M):
-    rng = np.random.default_rng(M)
+@pytest.mark.parametrize("M, N, K", [(1, 130, 1), (1, 130, 300), (5, 33, 300), (16, 1000, 1024), (3, 70, 1025), (1, 500, 16384), (1, 40_000, 1500), (2, 300, 8192), (2, 300, 8193), (17, 64, 8),
+                                     (300, 130, 300)])
+def test_product_rounds_a_matrix_first(M, N, K):
+    """In the same call where it is small (16 rows, 16384 elements), in a call before otherwise: the same bits."""
+    rng = np.random.default_rng(M + K)
+    b = micro(*random_micro(rng, N, K), K)
     for dtype in TYPES.values():
-        x = numbers_of(rng, M, 300, dtype).to(DEV)
-        b = micro(*random_micro(rng, 130, 300), 300)
-        assert torch.equal(binding.micro_product(x, b, 0.5, dtype=dtype), binding.micro_product(binding.micro_quantize(x), b, 0.5, dtype=dtype))
+        x = numbers_of(rng, M, K, dtype).to(DEV)
+        x.view(-1)[::5] = 0.0
+        want = binding.micro_product(binding.micro_quantize(x), b, 0.5, dtype=dtype)
+        assert torch.equal(binding.micro_product(x, b, 0.5, dtype=dtype), want)
+        view, _ = guarded(M, K, dtype, K + 3, 1)
+        view.copy_(x)
+        assert torch.equal(binding.micro_product(view, b, 0.5, dtype=dtype), want)
+        x[M - 1, K // 2] = float("nan")
+        assert torch.isnan(binding.micro_product(x, b)[M - 1]).all()
 
 
 def test_product_without_rows():
