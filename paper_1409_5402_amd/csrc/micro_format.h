@@ -21,24 +21,25 @@ __device__ __forceinline__ float micro_power(uint32_t s)
     return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
 }
 
-// The three bits of a size are the low exponent bits and the top fraction bit of the binary32 number size * 2^-126, the
-// subnormal .5 among them: two exact products give the element.
-__device__ __forceinline__ float micro_element(uint32_t code, float power)
-{
-    return __uint_as_float((code & 7u) << 22 | (code & 8u) << 28) * 0x1p126f * power;
-}
-
 // elements [first, first + V) of a row; V = 8 and 2 start at multiples of V
 template <int V>
 __device__ __forceinline__ void load_micro(float (&x)[V], const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int first)
 {
     static_assert(V == 8 || V == 2 || V == 1, "");
+    typedef float v2f __attribute__((ext_vector_type(2)));
     const float power = micro_power(scales[first / kMicroBlock]);
     uint32_t q;
     if constexpr (V == 8) q = *reinterpret_cast<const uint32_t*>(codes + first / 2);
     else                  q = (uint32_t)codes[first / 2] >> (V == 1 ? 4 * (first & 1) : 0);
+    v2f p[4];
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, power, 0);              // two elements of a byte, times the scale: exact
+    if constexpr (V == 8) {
+        p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, power, 1);
+        p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, power, 2);
+        p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, power, 3);
+    }
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = micro_element(q >> (4 * j), power);
+    for (int j = 0; j < V; ++j) x[j] = p[j / 2][j % 2];
 }
 
 }  // namespace same

@@ -23,13 +23,6 @@ struct QuantizeArgs {
     uint8_t* scales;
 };
 
-__device__ __forceinline__ uint32_t micro_code(float x, float per)
-{
-    const float t = fabsf(x) * per;
-    const float r = t < 2.0f ? rintf(2.0f * t) : t < 4.0f ? rintf(t) + 2.0f : fminf(rintf(0.5f * t) + 4.0f, 7.0f);
-    return (uint32_t)r | (__float_as_uint(x) >> 31 << 3);
-}
-
 // Codes of the 8 elements from `first` of a row of `width` on, and their block's scale; by four consecutive lanes together.
 template <class TI>
 __device__ __forceinline__ uint32_t micro_piece(const TI* __restrict__ row, int first, int width, bool wide, uint32_t& scale)
@@ -50,9 +43,11 @@ __device__ __forceinline__ uint32_t micro_piece(const TI* __restrict__ row, int 
     scale = 255u;
     if (top < 0x7F800000u) {
         scale = top >= 0x01000000u ? (top >> 23) - 2u : 0u;                    // 127 + e, at least 0
-        const float per = __uint_as_float((254u - scale) << 23);               // 2^-e: scale <= 252
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q |= micro_code(x[j], per) << (4 * j);
+        const float power = micro_power(scale);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[0], x[1], power, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[2], x[3], power, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[4], x[5], power, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[6], x[7], power, 3);
     }
     return q;
 }
@@ -63,7 +58,7 @@ __global__ __launch_bounds__(256) void micro_quantize_kernel(QuantizeArgs a)
     const int64_t pieces = micro_groups(a.width) * (kMicroGroup / 8);          // of 8 elements, per row
     const int64_t all = a.rows * pieces;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {   // whole groups of four lanes
-        const int64_t row = at / pieces;
+        const int64_t row = all >> 32 ? at / pieces : (int64_t)((uint32_t)at / (uint32_t)pieces);             // a division of 64 bits takes as long as the rest
         uint32_t s;
         const uint32_t q = micro_piece(static_cast<const TI*>(a.x) + row * a.stride, (int)(at - row * pieces) * 8, a.width, a.wide, s);
         reinterpret_cast<uint32_t*>(a.codes)[at] = q;                          // rows of codes follow each other without a gap

@@ -72,6 +72,7 @@ int lanes_log2_for(int64_t chunks)
 
 int64_t at_most(int64_t n, int64_t most) { return n < most ? n : most; }
 
+constexpr int64_t kComputeUnits = 256;
 constexpr int64_t kMaxGroups = (int64_t)1 << 22;     // workgroups of a launch (256 threads each: below 2^32 threads)
 
 template <class TI, class TO, int V>
@@ -80,7 +81,7 @@ int embed_launch(same::EmbedArgs& a, int32_t width, hipStream_t st)
     a.chunks = width / V;
     a.lanes_log2 = lanes_log2_for(a.chunks);
     const int64_t per = (int64_t)256 >> a.lanes_log2;
-    const int64_t groups = at_most((a.n + per - 1) / per, kMaxGroups);
+    const int64_t groups = at_most(a.n > 2 * per * kComputeUnits ? (a.n + 2 * per - 1) / (2 * per) : (a.n + per - 1) / per, kMaxGroups);   // two tokens in turn where they are many
     hipLaunchKernelGGL((same::embed_kernel<TI, TO, V>), dim3((unsigned)groups), dim3(256), 0, st, a);
     return launched("embed");
 }
