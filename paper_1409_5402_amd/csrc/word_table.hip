@@ -118,10 +118,20 @@ struct GradSpace {
 constexpr int kTileRows = 16, kSmallTileRows = 4;                    // rows of 256 tokens in a tile of the sort
 constexpr int64_t kSmallTiles = 1 << 22;                             // up to this many tokens the tiles are small
 
-GradSpace grad_space(int64_t n, int64_t rows, int32_t width)
+// One launch without a sort: up to 8192 tokens with two workgroups per compute unit, or 16,384 with one where rows of the gradient
+// are short (16,384 tokens into 2000 x 64 f32: 27 us, sorted 42; into 30,000 x 1024 bf16: 59, 60; into 2000 x 1024 f32, where the
+// most frequent word keeps one compute unit busy: 56, 44); and a grid below 2^32 threads.
+constexpr int kFewerTokens = 8192;
+bool few_tokens(int64_t n, int64_t rows, const same_lda_rows* grad)
 {
+    return n <= ((int64_t)grad->width * element_bytes(grad->type) <= 2048 ? same::kFewTokens : kFewerTokens) && rows * ((grad->width + 63) / 64) < (int64_t)1 << 30;
+}
+
+GradSpace grad_space(const same_lda_rows* grad, int64_t rows)
+{
+    const int64_t n = grad->rows, width = grad->width;
     GradSpace s = {};
-    if (n <= same::kFewTokens) return s;
+    if (few_tokens(n, rows, grad)) return s;
     size_t at = 0;
     const auto part = [&at](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     int bits = 1;
@@ -159,13 +169,17 @@ int grad_launch(same::GradArgs& a, hipStream_t st)
     const unsigned across = (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2);
     const int64_t most = kMaxGroups / across;                        // across <= SAME_LDA_WIDTH_MAX / 64
     if (!a.start) {                                                  // few tokens
-        // as many words per workgroup as leave 2048 workgroups, 64 at most: a workgroup reads the whole list
-        int64_t words = a.rows * across / 2048 / per * per;
-        words = words < per ? per : at_most(words, per > 64 ? per : 64);
-        const int64_t least = ((a.rows + most - 1) / most + per - 1) / per * per;
-        words = words > least ? words : least;
-        a.words = (int32_t)words;
-        hipLaunchKernelGGL((same::embed_grad_few_kernel<TI, TO, V>), dim3((unsigned)((a.rows + words - 1) / words), across), dim3(256), 0, st, a);
+        // two workgroups per compute unit, for each reads the whole list; more where a workgroup's words would be more than fit
+        if (a.lanes_log2 < 2) a.lanes_log2 = 2;                      // 256 groups at most, and words
+        const int64_t groups = (int64_t)1024 >> a.lanes_log2;
+        a.unit_log2 = 0;
+        while (a.unit_log2 < 5 && ((int64_t)a.width * (int64_t)sizeof(TO) << a.unit_log2) < 128) ++a.unit_log2;
+        const int64_t units = ((a.rows - 1) >> a.unit_log2) + 1, most_units = same::kFewWords >> a.unit_log2;
+        int64_t workgroups = at_most((a.rows + groups - 1) / groups, 2 * kComputeUnits / across > 1 ? 2 * kComputeUnits / across : 1);
+        workgroups = workgroups < (units + most_units - 1) / most_units ? (units + most_units - 1) / most_units : workgroups;
+        a.words = (int32_t)((units + workgroups - 1) / workgroups << a.unit_log2);
+        if (a.n <= kFewerTokens) hipLaunchKernelGGL((same::embed_grad_few_kernel<TI, TO, V, kFewerTokens / 1024>), dim3((unsigned)workgroups, across), dim3(1024), 0, st, a);
+        else                     hipLaunchKernelGGL((same::embed_grad_few_kernel<TI, TO, V, same::kFewTokens / 1024>), dim3((unsigned)workgroups, across), dim3(1024), 0, st, a);
         return launched("embed_grad");
     }
     hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V>), dim3((unsigned)at_most((a.ranges + a.rows + per - 1) / per, most), across), dim3(256), 0, st, a);
@@ -296,7 +310,7 @@ int same_lda_embed_grad_workspace(const same_lda_rows* grad, const same_lda_rows
     if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: bytes is null");
     const int rc = check_grad(grad, table_grad);
     if (rc) return rc;
-    *bytes = grad_space(grad->rows, table_grad->rows, grad->width).bytes;
+    *bytes = grad_space(grad, table_grad->rows).bytes;
     return SAME_LDA_OK;
 }
 
@@ -309,15 +323,15 @@ int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t t
     if (!tokens && grad->rows > 0) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: tokens is null");
     if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: the scale must be finite");
     const int64_t n = grad->rows, rows = table_grad->rows;
-    const GradSpace s = grad_space(n, rows, grad->width);
+    const GradSpace s = grad_space(grad, rows);
     if (rows == 0 || (n == 0 && accumulate)) return SAME_LDA_OK;
     if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes || (uintptr_t)workspace % 16))
         return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: needs %zu bytes of workspace aligned to 16 (got %zu)", s.bytes, workspace ? workspace_bytes : (size_t)0);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     char* const w = static_cast<char*>(workspace);
     same::GradArgs a = {grad->data, grad->stride, nullptr, nullptr, rows, scale, accumulate, table_grad->data, table_grad->stride,
-                        nullptr, s.ranges, grad->width, 0, 0, {tokens, token_bytes == 8}, (int32_t)n, 0};
-    if (n > same::kFewTokens) {
+                        nullptr, s.ranges, grad->width, 0, 0, {tokens, token_bytes == 8}, (int32_t)n, 0, 0};
+    if (!few_tokens(n, rows, grad)) {
         uint32_t* const hist = reinterpret_cast<uint32_t*>(w + s.hist);
         uint32_t* const total = reinterpret_cast<uint32_t*>(w + s.total);
         int32_t* const start = reinterpret_cast<int32_t*>(w + s.start);

@@ -137,8 +137,8 @@ def check_grad(G, t, V, scale, got, out, before=None):
 
 # one token, tiles of the sort and their borders, runs of every length up to several pieces, words in one, two and three digits
 @pytest.mark.parametrize("n, V, width", [(1, 1, 1), (1, 5000, 64), (2, 3, 65), (77, 2000, 50), (255, 1, 16), (256, 1, 16), (257, 1, 16), (513, 2, 24), (4095, 10, 3),
-                                         (4096, 300, 8), (4097, 511, 8), (4100, 512, 12), (2048, 5000, 20), (2049, 700, 7), (63, 1, 8), (64, 2, 8),
-                                         (65, 1, 8), (9001, 70_000, 33), (20_000, 3, 130), (12_345, 300_000, 4), (30_000, 40, 257)])
+                                         (4096, 300, 8), (4097, 511, 8), (4100, 512, 12), (2048, 5000, 20), (2049, 700, 7), (8192, 900, 12), (8193, 900, 12), (16_384, 700, 6), (16_385, 700, 6), (16_000, 5, 66), (12_000, 40_000, 2), (8000, 3, 300), (7001, 20_000, 1), (6000, 1300, 2), (5000, 40, 1000), (63, 1, 8), (64, 2, 8),
+                                         (65, 1, 8), (9001, 70_000, 33), (20_000, 3, 130), (22_345, 300_000, 4), (30_000, 40, 257), (19_001, 70_000, 33), (20_480, 511, 8), (20_481, 512, 12)])
 @pytest.mark.parametrize("kind", ["even", "skewed"])
 def test_embed_grad_matches_the_oracle(n, V, width, kind):
     rng = np.random.default_rng(n + V)
