@@ -84,10 +84,11 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a)
 // on the tokens alone (no atomics: two calls give the same bits).
 
 // Stable radix sort of the words by digits of `bits` bits (at most kDigitBits), least significant first.  A workgroup owns a
-// tile of 256 * R consecutive tokens.  Per pass: counts per (digit, tile); for every digit their exclusive sum over the tiles;
-// placement, which adds up the digits before its own.
+// tile of 256 * R consecutive tokens.  Per pass: counts per (digit, tile); for every digit their exclusive sum over the tiles (up to
+// kFewTiles tiles the placement adds them up for itself); placement, which adds up the digits before its own.
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
+constexpr uint32_t kFewTiles = 64;
 
 __device__ __forceinline__ int32_t word_of(const Tokens& tokens, int64_t i, int64_t rows)
 {
@@ -104,7 +105,7 @@ struct alignas(8) Placed {
 // from null: the first pass takes the words from the tokens
 template <int R>
 __global__ __launch_bounds__(256) void token_histogram(Tokens tokens, int64_t rows, const Placed* __restrict__ from, int64_t n, int shift, int bits,
-                                                       uint32_t tiles, uint32_t* __restrict__ hist)
+                                                       uint32_t tiles, uint32_t* __restrict__ hist)   // tiles: a multiple of 4, the last ones may be empty
 {
     __shared__ uint32_t h[kDigits];
     const uint32_t digits = 1u << bits;
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(256) void token_offsets(uint32_t* __restrict__ hist
 
 // A token's place: the tokens of lower digits, those of its digit in the tiles before, in the waves before its own, in the
 // earlier rows of its wave and in the lower lanes of its row.
-template <int R>
+template <int R, bool kFew>
 __global__ __launch_bounds__(256) void token_place(Tokens tokens, int64_t rows, const Placed* __restrict__ from, int64_t n, int shift, int bits, uint32_t tiles, const uint32_t* __restrict__ start,
                                                    const uint32_t* __restrict__ total, Placed* __restrict__ to)
 {
@@ -159,8 +160,24 @@ __global__ __launch_bounds__(256) void token_place(Tokens tokens, int64_t rows, 
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     for (uint32_t d = lane; d < digits; d += 64) cnt[wv][d] = 0u;
     const uint32_t d0 = 2u * threadIdx.x;                          // a thread's two digits
-    const uint32_t t0 = d0 < digits ? total[d0] : 0u, t1 = d0 + 1u < digits ? total[d0 + 1u] : 0u;
-    uint32_t p0 = d0 < digits ? start[(size_t)d0 * tiles + blockIdx.x] : 0u, p1 = d0 + 1u < digits ? start[(size_t)(d0 + 1u) * tiles + blockIdx.x] : 0u;
+    uint32_t t0 = 0u, t1 = 0u, p0 = 0u, p1 = 0u;                   // their tokens, and those of them in the tiles before
+    if constexpr (kFew) {
+        const auto sums = [&](uint32_t d, uint32_t& all, uint32_t& before) {
+            const uint4* const row = reinterpret_cast<const uint4*>(start + (size_t)d * tiles);
+#pragma unroll 4
+            for (uint32_t q = 0; q < tiles / 4u; ++q) {
+                const uint4 c = row[q];
+                const uint32_t x[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                for (uint32_t j = 0; j < 4u; ++j) { all += x[j]; before += 4u * q + j < blockIdx.x ? x[j] : 0u; }
+            }
+        };
+        if (d0 < digits) sums(d0, t0, p0);
+        if (d0 + 1u < digits) sums(d0 + 1u, t1, p1);
+    } else {
+        if (d0 < digits) { t0 = total[d0]; p0 = start[(size_t)d0 * tiles + blockIdx.x]; }
+        if (d0 + 1u < digits) { t1 = total[d0 + 1u]; p1 = start[(size_t)(d0 + 1u) * tiles + blockIdx.x]; }
+    }
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * (256 * R) + (int64_t)wv * (R * 64) + lane;
     Placed x[R];
@@ -209,7 +226,7 @@ __global__ __launch_bounds__(256) void token_place(Tokens tokens, int64_t rows, 
 
 // start[w] = first place of word w among the sorted tokens, rows + 1 entries (the last: the number of tokens of any word).  The
 // token at place p writes the entries of the words after its predecessor's up to its own, the end those after the last: a few each
-// where tokens are many, else the lanes of a wave share the long gaps.
+// where tokens are many, and the lanes of a wave share a long gap.
 __global__ __launch_bounds__(256) void word_runs(const Placed* __restrict__ sorted, int64_t n, int64_t rows, int32_t* __restrict__ start)
 {
     constexpr int64_t kOwn = 8;
@@ -228,6 +245,16 @@ __global__ __launch_bounds__(256) void word_runs(const Placed* __restrict__ sort
         const int64_t first = __shfl((long long)lo, from) + kOwn, last = __shfl((long long)hi, from), q = __shfl((long long)p, from);
         for (int64_t w = first + lane; w <= last; w += 64) start[w] = (int32_t)q;
     }
+}
+
+// The same where words are many for the tokens (16,385 in 140,000: 16 us by gaps): every word looks for its place.
+__global__ __launch_bounds__(256) void word_runs_sparse(const Placed* __restrict__ sorted, int64_t n, int64_t rows, int32_t* __restrict__ start)
+{
+    const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (w > rows) return;
+    int64_t lo = 0, hi = n;
+    while (lo < hi) { const int64_t mid = (lo + hi) >> 1; if (sorted[mid].word < (int32_t)w) lo = mid + 1; else hi = mid; }
+    start[w] = (int32_t)lo;
 }
 
 // A run of more than kLongRun tokens is cut at the multiples of kLongRun: group j sums the places [j, j + 1) * kLongRun of long
@@ -270,12 +297,33 @@ __device__ __forceinline__ void add_rows(float (&acc)[V], const TI* __restrict__
         for (int j = 0; j < V; ++j) acc[j] = q < count ? acc[j] + x[q][j] : acc[j];
 }
 
-// By the 2^lanes_log2 lanes of a group, all of them active: a lane fetches one place of the run for all.
-template <class TI, int V>
+// By the 2^lanes_log2 lanes of a group, all of them active: a lane fetches one place of the run for all, or, where lanes are few,
+// each fetches eight, those of the next rows while these are on their way (16,385 tokens into 140,000 x 16: 24 us with one place
+// per lane and four lanes, now 15).
+template <class TI, int V, bool kNarrow>
 __device__ __forceinline__ void sum_run(float (&acc)[V], const GradArgs& a, int64_t lo, int64_t hi, int c)
 {
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
     const TI* const from = static_cast<const TI*>(a.grad) + (int64_t)c * V;
+    if constexpr (kNarrow) {
+        if (lo >= hi) return;
+        int32_t place[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) place[q] = a.sorted[lo + q < hi ? lo + q : hi - 1].pos;
+        for (int64_t p = lo; p < hi; p += 8) {
+            int32_t here[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) here[q] = place[q];
+            if (p + 8 < hi)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) place[q] = a.sorted[p + 8 + q < hi ? p + 8 + q : hi - 1].pos;
+            const auto at = [&](int i) { return here[i]; };
+            const int left = hi - p < 8 ? (int)(hi - p) : 8;
+            if (left > 2) add_rows<TI, V, 8>(acc, from, a.stride, left, at);
+            else          add_rows<TI, V, 2>(acc, from, a.stride, left, at);
+        }
+        return;
+    }
     for (int64_t base = lo; base < hi; base += lanes) {
         const int here = hi - base < lanes ? (int)(hi - base) : lanes;
         const int32_t mine = a.sorted[base + (lane < here ? lane : here - 1)].pos;
@@ -307,7 +355,7 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int64_t w, int c, f
     store_chunk<TO, V>(to, acc);
 }
 
-template <class TI, class TO, int V>
+template <class TI, class TO, int V, bool kNarrow>
 __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
 {
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
@@ -324,20 +372,20 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
             const int64_t s0 = a.start[w0], e0 = a.start[w0 + 1];
             if (e0 - s0 > kLongRun) {
                 float acc[V] = {};
-                sum_run<TI, V>(acc, a, lo, e0 < hi ? e0 : hi, c);
+                sum_run<TI, V, kNarrow>(acc, a, lo, e0 < hi ? e0 : hi, c);
                 if (mine) store_chunk<float, V>(a.partial + (size_t)(2 * item) * a.width + (int64_t)c * V, acc);
             }
             const int64_t s1 = a.start[w1], e1 = a.start[w1 + 1];
             if (w1 != w0 && e1 - s1 > kLongRun) {
                 float acc[V] = {};
-                sum_run<TI, V>(acc, a, s1, hi, c);
+                sum_run<TI, V, kNarrow>(acc, a, s1, hi, c);
                 if (mine) store_chunk<float, V>(a.partial + (size_t)(2 * item + 1) * a.width + (int64_t)c * V, acc);
             }
         } else {
             const int64_t w = item - a.ranges, lo = a.start[w], hi = a.start[w + 1];
             if (hi - lo > kLongRun) continue;
             float acc[V] = {};
-            sum_run<TI, V>(acc, a, lo, hi, c);
+            sum_run<TI, V, kNarrow>(acc, a, lo, hi, c);
             if (mine) write_row<TO, V>(a, w, c, acc, hi > lo);
         }
     }

@@ -140,7 +140,7 @@ GradSpace grad_space(const same_lda_rows* grad, int64_t rows)
     s.bits = (bits + s.passes - 1) / s.passes;
     s.small_tiles = n <= kSmallTiles;
     const int64_t tile = 256 * (s.small_tiles ? kSmallTileRows : kTileRows);
-    s.tiles = (uint32_t)((n + tile - 1) / tile);
+    s.tiles = (uint32_t)(((n + tile - 1) / tile + 3) & ~(int64_t)3);        // four counts in one load
     s.ranges = (n + same::kLongRun - 1) / same::kLongRun;
     for (int i = 0; i < 2; ++i) s.sorted[i] = part((size_t)n * sizeof(same::Placed));
     s.hist = part(((size_t)s.tiles << s.bits) * 4);
@@ -156,8 +156,12 @@ void sort_pass(const same::GradArgs& a, const GradSpace& s, int64_t n, int pass,
 {
     const int shift = pass * s.bits;
     hipLaunchKernelGGL(same::token_histogram<R>, dim3(s.tiles), dim3(256), 0, st, a.tokens, a.rows, a.sorted, n, shift, s.bits, s.tiles, hist);
+    if (s.tiles <= same::kFewTiles) {
+        hipLaunchKernelGGL((same::token_place<R, true>), dim3(s.tiles), dim3(256), 0, st, a.tokens, a.rows, a.sorted, n, shift, s.bits, s.tiles, hist, total, to);
+        return;
+    }
     hipLaunchKernelGGL(same::token_offsets, dim3(1u << s.bits), dim3(256), 0, st, hist, s.tiles, total);
-    hipLaunchKernelGGL(same::token_place<R>, dim3(s.tiles), dim3(256), 0, st, a.tokens, a.rows, a.sorted, n, shift, s.bits, s.tiles, hist, total, to);
+    hipLaunchKernelGGL((same::token_place<R, false>), dim3(s.tiles), dim3(256), 0, st, a.tokens, a.rows, a.sorted, n, shift, s.bits, s.tiles, hist, total, to);
 }
 
 template <class TI, class TO, int V>
@@ -182,7 +186,9 @@ int grad_launch(same::GradArgs& a, hipStream_t st)
         else                     hipLaunchKernelGGL((same::embed_grad_few_kernel<TI, TO, V, same::kFewTokens / 1024>), dim3((unsigned)workgroups, across), dim3(1024), 0, st, a);
         return launched("embed_grad");
     }
-    hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V>), dim3((unsigned)at_most((a.ranges + a.rows + per - 1) / per, most), across), dim3(256), 0, st, a);
+    const dim3 grid((unsigned)at_most((a.ranges + a.rows + per - 1) / per, most), across);
+    if (a.lanes_log2 < 4) hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V, true>), grid, dim3(256), 0, st, a);
+    else                  hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V, false>), grid, dim3(256), 0, st, a);
     if (a.lanes_log2 > same::kJoinLanesLog2 && a.chunks <= 65535 << same::kJoinLanesLog2) a.lanes_log2 = same::kJoinLanesLog2;
     const int64_t items = (int64_t)1024 >> a.lanes_log2;             // ranges of a workgroup
     hipLaunchKernelGGL((same::embed_grad_join_kernel<TO, V>), dim3((unsigned)((a.ranges + items - 1) / items), (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2)),
@@ -341,7 +347,8 @@ int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t t
             else               sort_pass<kTileRows>(a, s, n, i, hist, total, to, st);
             a.sorted = to;
         }
-        hipLaunchKernelGGL(same::word_runs, dim3((unsigned)((n + 256) / 256)), dim3(256), 0, st, a.sorted, n, rows, start);
+        if (rows > 4 * n) hipLaunchKernelGGL(same::word_runs_sparse, dim3((unsigned)((rows + 256) / 256)), dim3(256), 0, st, a.sorted, n, rows, start);
+        else              hipLaunchKernelGGL(same::word_runs, dim3((unsigned)((n + 256) / 256)), dim3(256), 0, st, a.sorted, n, rows, start);
         if ((rc = launched("embed_grad"))) return rc;
         a.start = start;
         a.partial = reinterpret_cast<float*>(w + s.partial);

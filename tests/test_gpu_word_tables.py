@@ -184,10 +184,12 @@ def test_embed_grad_is_exact_on_integers_and_on_one_word():
         t = torch.full((n,), 2, device=DEV, dtype=torch.int32)
         got = binding.embed_grad(g, t, 4)                            # sums below 2^24: every order gives the integer
         assert torch.equal(got[2].double(), g.double().sum(0)) and torch.all(got[[0, 1, 3]] == 0)
-    g = torch.randint(-8, 9, (200_003, 20), device=DEV, dtype=torch.float32)
-    t = (torch.rand(200_003, device=DEV) ** 6 * 5000).long()
-    want = torch.zeros(5000, 20, dtype=torch.float64, device=DEV).index_add_(0, t, g.double())
-    assert torch.equal(binding.embed_grad(g, t, 5000).double(), want)
+    # many tokens: words of two digits and of three, tiles of either size, words that are few and many for the tokens
+    for n, V, width in [(200_003, 5000, 20), (70_001, 300_000, 3), (70_001, 270_000, 2), (4_300_001, 600, 2)]:
+        g = torch.randint(-8, 9, (n, width), device=DEV, dtype=torch.float32)
+        t = (torch.rand(n, device=DEV, dtype=torch.float64) ** 6 * V).long()
+        want = torch.zeros(V, width, dtype=torch.float64, device=DEV).index_add_(0, t, g.double())
+        assert torch.equal(binding.embed_grad(g, t, V).double(), want)
 
 
 def test_embed_grad_without_tokens_or_words():
