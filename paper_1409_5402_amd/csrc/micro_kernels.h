@@ -108,8 +108,8 @@ __global__ __launch_bounds__(256) void micro_product_few_kernel(ProductArgs p)
     constexpr int kUnroll = MF * RF >= 8 ? 2 : 4;                              // groups in flight
     constexpr bool kRound = !std::is_void<TI>::value;
     __shared__ v4f others[KW > 1 ? KW - 1 : 1][MF][RF][64];
-    __shared__ uint32_t rounded[kRound ? (kRoundMost + 16 * kMicroGroup) / 8 : 1];
-    __shared__ uint8_t rounded_scales[kRound ? (kRoundMost + 16 * kMicroGroup) / 32 : 4] __attribute__((aligned(4)));
+    __shared__ alignas(16) uint32_t rounded[kRound ? (kRoundMost + 16 * kMicroGroup) / 8 : 1];
+    __shared__ alignas(16) uint8_t rounded_scales[kRound ? (kRoundMost + 16 * kMicroGroup) / 32 : 4];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int64_t pitch = (int64_t)p.groups * 64, spitch = (int64_t)p.groups * 4;
     const uint8_t *a = p.a, *a_scales = p.a_scales;
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN * WM * WN > 16 ? WM * WN / 4 
         for (int st = 0; st + 1 < stages; ++st) multiply(st, std::true_type());
     multiply(stages - 1, std::false_type());
 
-    __syncthreads();
+    arrived<0>();                                                              // nothing is on its way to LDS, and no wave reads blocks from it any more
     float* const strip = space.strip[wv];
     constexpr int V = 16 / sizeof(TO), kAcross = 32 * FN / V;                  // elements of a store, stores of a row
     TO* const out = static_cast<TO*>(p.out) + (i0 + wi) * p.out_stride + j0 + wj;

@@ -258,6 +258,8 @@ void product_few_by_shape(same::ProductArgs& p, hipStream_t st)
 //   256 x 256                   from 256 such tiles on (4096 x 16,384 x 1024: 58, tiles of 128 85; 2048 x 4096 x 4096, 128 tiles: 33,
 //                               tiles of 128 27)
 //   64 x 64                     up to 160 tiles of 128 x 128 (512 x 4096 x 4096: 13.9, 16.5; 1024 x 4096 x 4096: 27, 18)
+constexpr int64_t kRowsAtOnce = (int64_t)1 << 28;
+
 template <class TO>
 void product_to(same::ProductArgs& p, int32_t type_a, hipStream_t st)
 {
@@ -409,17 +411,33 @@ int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float
     static_assert(SAME_LDA_ROUND_MAX == same::kRoundMost, "");
     if (a->rows == 0) return SAME_LDA_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    same::ProductArgs p = {static_cast<const uint8_t*>(a->data), a->scales, static_cast<const uint8_t*>(b->data), b->scales, a->rows, b->rows,
-                           (int32_t)same::micro_groups(a->width), scale, out->data, out->stride, 0, 0, 0, a->stride, a->width, 0};
-    const same_lda_rows whole = {a->data, nullptr, a->rows, a->stride, 8, a->type};
-    p.wide_a = chunks_fit(&whole, 8);
-    const same_lda_rows strip = {out->data, nullptr, out->rows, out->stride, 16 / element_bytes(out->type), out->type};   // alignment of rows, whatever their width
-    p.wide = chunks_fit(&strip, strip.width);
-    switch (out->type) {
-        case SAME_LDA_FLOAT:  product_to<float>(p, a->type, st); break;
-        case SAME_LDA_BFLOAT: product_to<__bf16>(p, a->type, st); break;
-        default:              product_to<_Float16>(p, a->type, st); break;
-    }
+    const same_lda_rows whole = {a->data, nullptr, a->rows, a->stride, 8, a->type};                                      // alignment of rows, whatever their width
+    const same_lda_rows strip = {out->data, nullptr, out->rows, out->stride, 16 / element_bytes(out->type), out->type};
+    const int64_t pitch_a = a->type == SAME_LDA_MICRO ? same::micro_code_pitch(a->width) : 0, pitch_b = same::micro_code_pitch(b->width);
+    // at most 2^28 rows of either operand in a launch: grids stay below 2^32 threads (the output's size bounds the tiles)
+    for (int64_t i = 0; i < a->rows; i += kRowsAtOnce)
+        for (int64_t j = 0; j < b->rows; j += kRowsAtOnce) {
+            same::ProductArgs p = {};
+            p.a = static_cast<const uint8_t*>(a->data) + i * pitch_a;                                                    // (a matrix of numbers: i = 0)
+            p.a_scales = a->scales + i * (pitch_a / 16);
+            p.b = static_cast<const uint8_t*>(b->data) + j * pitch_b;
+            p.b_scales = b->scales + j * (pitch_b / 16);
+            p.rows_a = at_most(a->rows - i, kRowsAtOnce);
+            p.rows_b = at_most(b->rows - j, kRowsAtOnce);
+            p.groups = (int32_t)same::micro_groups(a->width);
+            p.scale = scale;
+            p.out = static_cast<char*>(out->data) + (i * out->stride + j) * element_bytes(out->type);
+            p.out_stride = out->stride;
+            p.wide = chunks_fit(&strip, strip.width);
+            p.stride_a = a->stride;
+            p.width = a->width;
+            p.wide_a = chunks_fit(&whole, 8);
+            switch (out->type) {
+                case SAME_LDA_FLOAT:  product_to<float>(p, a->type, st); break;
+                case SAME_LDA_BFLOAT: product_to<__bf16>(p, a->type, st); break;
+                default:              product_to<_Float16>(p, a->type, st); break;
+            }
+        }
     return launched("micro_product");
 }
 

@@ -188,8 +188,8 @@ def test_embed_grad_is_exact_on_integers_and_on_one_word():
     for n, V, width in [(200_003, 5000, 20), (70_001, 300_000, 3), (70_001, 270_000, 2), (4_300_001, 600, 2)]:
         g = torch.randint(-8, 9, (n, width), device=DEV, dtype=torch.float32)
         t = (torch.rand(n, device=DEV, dtype=torch.float64) ** 6 * V).long()
-        want = torch.zeros(V, width, dtype=torch.float64, device=DEV).index_add_(0, t, g.double())
-        assert torch.equal(binding.embed_grad(g, t, V).double(), want)
+        want = torch.zeros(V, width, dtype=torch.float64).index_add_(0, t.cpu(), g.double().cpu())
+        assert torch.equal(binding.embed_grad(g, t, V).double().cpu(), want)
 
 
 def test_embed_grad_without_tokens_or_words():
@@ -449,7 +449,7 @@ def test_offsets_beyond_32_bits():
 
 
 def test_product_of_many_short_rows():
-    n = 70_000_000                                                    # codes beyond 2^32 bytes, an output wider than 2^26
+    n = (1 << 28) + 70                                                # codes beyond 2^32 bytes, more rows than one launch takes
     codes = torch.zeros(n, 64, dtype=torch.uint8, device=DEV)
     codes[n - 1, 0] = 0x22
     q = binding.MicroMatrix(codes, torch.full((n, 4), 127, dtype=torch.uint8, device=DEV), 128)
