@@ -293,7 +293,7 @@ def micro(codes, scales, width):
 
 
 PRODUCTS = [(1, 1, 1), (1, 100, 33), (1, 1000, 256), (2, 17, 129), (5, 300, 1000), (13, 501, 640), (16, 16, 128), (16, 4096, 512), (17, 65, 129), (33, 1, 4096), (64, 64, 256),
-            (100, 1030, 200), (128, 128, 384), (130, 257, 384), (255, 300, 1024), (300, 513, 2048), (512, 520, 640), (1025, 300, 256), (20, 33_000, 1030), (31, 4500, 1024), (40, 36_000, 700), (70, 700, 384), (1300, 1500, 640), (2100, 5000, 100)]
+            (100, 1030, 200), (128, 128, 384), (130, 257, 384), (255, 300, 1024), (300, 513, 2048), (512, 520, 640), (1025, 300, 256), (20, 33_000, 1030), (31, 4500, 1024), (40, 36_000, 700), (25, 300, 500), (70, 700, 384), (1300, 1500, 640), (2100, 5000, 100)]
 
 
 @pytest.mark.parametrize("M, N, K", PRODUCTS)
