@@ -6,6 +6,8 @@ off by at most m u times the sum of their magnitudes (to first order; 1.01 cover
 summed in pieces, so m counts the terms of a piece and the pieces.  Then one product and one rounding: u + eps/2.
 Products of four-bit numbers are exact in binary32, and every addition of the matrix instruction is taken to be off by a whole
 step: 2 u per term.  Rounding to four bits and reading back are exact."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -100,6 +102,9 @@ def test_embed_shapes_of_tokens_and_the_longest_and_shortest_lists():
     assert out.shape == (2, 3, 5) and out.dtype == torch.bfloat16 and out[1, 0, 4] == 68 and torch.all(out[1, 1] == 0)
     assert binding.embed(T, t[:0]).shape == (0, 3, 5)
     assert torch.equal(binding.embed(T, torch.tensor(4, device=DEV)), T[4])
+    g = torch.arange(30, dtype=torch.float32, device=DEV).view(2, 3, 5)
+    assert torch.equal(binding.embed_grad(g, t, 7), binding.embed_grad(g.view(6, 5), t.view(6), 7))
+    assert torch.equal(binding.embed_grad(g.transpose(0, 1), t.t(), 7), binding.embed_grad(g, t, 7))     # not contiguous: copied
     big = torch.randint(0, 7, (3_000_001,), device=DEV)
     assert torch.equal(binding.embed(T, big), T[big])
     assert torch.all(binding.embed(T[:0], t) == 0)                # a table without rows: no id names one
@@ -118,6 +123,18 @@ def test_padding_never_reads_the_table_nor_the_gradient():
     assert torch.equal(torch.isfinite(binding.embed(x, torch.tensor([2, 1, 0], device=DEV))).cpu(), torch.tensor([[True, False], [False, True], [False, True]]))
     s = binding.embed_grad(x, torch.tensor([0, 0, 1], device=DEV), 2)
     assert torch.isnan(s[0, 0]) and s[0, 1] == 3.0 and s[1, 1] == float("-inf")
+    for n in (3000, 12_000, 40_000):                              # every way to the sums: most rows stand for no word
+        t = torch.randint(0, 300, (n,), device=DEV)
+        t[::3], t[1::3] = -1, 300 + 300 * torch.randint(0, 1 << 40, (len(t[1::3]),), device=DEV)
+        t[1], t[4] = 1 << 33, -(1 << 40)
+        g = torch.full((n, 24), float("nan"), device=DEV)
+        known = (t >= 0) & (t < 300)
+        g[known] = torch.randint(-8, 9, (int(known.sum()), 24), device=DEV).float()
+        want = torch.zeros(300, 24, dtype=torch.float64).index_add_(0, t[known].cpu(), g[known].double().cpu())
+        assert torch.equal(binding.embed_grad(g, t, 300).double().cpu(), want)
+        none = torch.full((n,), -1, device=DEV)
+        assert torch.all(binding.embed_grad(g, none, 300) == 0.0)
+        assert torch.all(binding.embed_grad(g, none, out=torch.full((300, 24), 2.0, device=DEV), accumulate=True) == 2.0)
 
 
 # ---- gradient
@@ -156,11 +173,11 @@ def test_embed_grad_matches_the_oracle(n, V, width, kind):
 
 @pytest.mark.parametrize("out", TYPES)
 @pytest.mark.parametrize("grad", TYPES)
-@pytest.mark.parametrize("width", [5, 16, 66, 512])
+@pytest.mark.parametrize("n, width", [(1500, 5), (1500, 16), (1500, 66), (1500, 512), (17_000, 5), (17_000, 16), (17_000, 66), (9000, 1032)])
 @pytest.mark.parametrize("accumulate", [False, True])
-def test_embed_grad_types_strides_and_accumulation(grad, out, width, accumulate):
+def test_embed_grad_types_strides_and_accumulation(grad, out, n, width, accumulate):
     rng = np.random.default_rng(width)
-    n, V = 1500, 23
+    V = 23
     G = numbers_of(rng, n, width, TYPES[grad]) * 0.25
     t = words(rng, n, V, "skewed")
     t[t == 20] = 19
@@ -381,14 +398,19 @@ def everything(T, t, g, x):
     return e, dT, q.codes, q.scales, binding.embed(q, t, dtype=torch.bfloat16), binding.micro_product(x, q), binding.micro_dequantize(q)
 
 
-def inputs(seed, n=3000, V=500, E=96):
+def inputs(seed, n, rows, V=700, E=416):
     rng = np.random.default_rng(seed)
     return (numbers_of(rng, V, E, torch.float32).to(DEV), torch.from_numpy(words(rng, n, V, "skewed")).to(DEV), numbers_of(rng, n, E, torch.float32).to(DEV),
-            numbers_of(rng, 7, E, torch.bfloat16).to(DEV))
+            numbers_of(rng, rows, E, torch.bfloat16).to(DEV))
 
 
-def test_other_streams_at_once_give_the_same():
-    sets = [inputs(s) for s in range(3)]
+# the gradient in one launch and by a sort, the product that rounds by itself, in small tiles and in large ones
+CALLS = [(3000, 7), (40_000, 70), (12_000, 5000)]
+
+
+@pytest.mark.parametrize("n, rows", CALLS)
+def test_other_streams_at_once_give_the_same(n, rows):
+    sets = [inputs(s, n, rows) for s in range(3)]
     want = [everything(*s) for s in sets]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in sets]
@@ -401,8 +423,36 @@ def test_other_streams_at_once_give_the_same():
         assert all(torch.equal(a, b) for a, b in zip(w, g))
 
 
-def test_captured_calls_replay_on_new_inputs():
-    a, b = inputs(1), inputs(2)
+def test_threads_at_once_give_the_same():
+    sets = [inputs(s, 20_000, 40) for s in range(4)]
+    want = [everything(*s) for s in sets]
+    torch.cuda.synchronize()
+    got = [None] * len(sets)
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(5):
+                got[k] = everything(*sets[k])
+                try:
+                    binding.micro_product(sets[k][3], binding.micro_quantize(sets[k][0][:, :100 + k]))
+                except binding.SameLdaError as e:                     # the text is the calling thread's
+                    assert f"and of {100 + k} elements" in str(e)
+                else:
+                    raise AssertionError
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(sets))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for w, g in zip(want, got):
+        assert all(torch.equal(a, b) for a, b in zip(w, g))
+
+
+@pytest.mark.parametrize("n, rows", CALLS)
+def test_captured_calls_replay_on_new_inputs(n, rows):
+    a, b = inputs(1, n, rows), inputs(2, n, rows)
     held = [x.clone() for x in a]
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
