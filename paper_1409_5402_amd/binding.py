@@ -381,13 +381,18 @@ class MicroMatrix:
         return MicroMatrix(self.codes[rows], self.scales[rows], self.width)
 
 
+def _type_of(dtype) -> int:
+    kind = _types.get(dtype)
+    if kind is None:
+        raise TypeError(f"{dtype} is not one of float32, bfloat16 and float16")
+    return kind
+
+
 def _rows(x) -> bytes:
     """A matrix as a same_lda_rows."""
     if type(x) is MicroMatrix:
         return _pack_rows(x.codes.data_ptr(), x.scales.data_ptr(), x.rows, x.width, x.width, MICRO)
-    kind = _types.get(x.dtype)
-    if kind is None:
-        raise TypeError(f"{x.dtype} is not one of float32, bfloat16 and float16")
+    kind = _type_of(x.dtype)
     if x.dim() != 2:
         raise ValueError(f"a matrix has two dimensions, not {x.dim()}")
     rows, width = x.shape
@@ -425,12 +430,15 @@ def _token_ids(tokens):
     return tokens if tokens.is_contiguous() else tokens.contiguous()
 
 
-def _output(out, shape, dtype, default, device):
+def _output(out, shape, rows, width, dtype, default, device):
+    """The output of a call, made here where none is given, and its same_lda_rows as `rows` rows of `width`."""
     if out is None:
-        return _torch.empty(shape, dtype=dtype or default, device=device)
+        kind = _type_of(dtype or default)
+        out = _torch.empty(shape, dtype=dtype or default, device=device)
+        return out, _pack_rows(out.data_ptr(), 0, rows, width, width, kind)
     if out.shape != shape or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype or out.dtype}")
-    return out
+    return out, _rows(out if out.dim() == 2 else out.view(-1, width))
 
 
 def embed(table, tokens, scale=1.0, dtype=None, out=None):
@@ -439,9 +447,9 @@ def embed(table, tokens, scale=1.0, dtype=None, out=None):
     shape tokens.shape + (width,) whose leading dimensions can be viewed as one."""
     ids = _token_ids(tokens)
     index = _gpu(ids, table, out)
-    out = _output(out, (*tokens.shape, table.shape[1]), dtype, _torch.float32 if type(table) is MicroMatrix else table.dtype, ids.device)
-    flat = out if out.dim() == 2 else out.view(-1, out.shape[-1])
-    _run(index, _library.same_lda_embed, _rows(table), ids.data_ptr() if ids.numel() else _EMPTY, ids.element_size(), scale, _rows(flat))
+    t, n, width = _rows(table), ids.numel(), table.shape[1]
+    out, o = _output(out, (*tokens.shape, width), n, width, dtype, _torch.float32 if type(table) is MicroMatrix else table.dtype, ids.device)
+    _run(index, _library.same_lda_embed, t, ids.data_ptr() if n else _EMPTY, ids.element_size(), scale, o)
     return out
 
 
@@ -458,8 +466,10 @@ def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumul
     if out is None and (accumulate or rows is None):
         raise ValueError("accumulate needs out" if accumulate else "rows or out must say how many rows the table has")
     index = _gpu(ids, grad, out)
-    out = _output(out, (out.shape[0] if rows is None else int(rows), grad.shape[-1]), dtype, grad.dtype, ids.device)
-    g, o = _rows(grad if grad.dim() == 2 else grad.reshape(-1, grad.shape[-1])), _rows(out)
+    width = grad.shape[-1]
+    rows = out.shape[0] if rows is None else int(rows)
+    g = _rows(grad if grad.dim() == 2 else grad.reshape(-1, width))
+    out, o = _output(out, (rows, width), rows, width, dtype, grad.dtype, ids.device)
     n = c_size_t()
     if _library.same_lda_embed_grad_workspace(g, o, byref(n)):
         raise SameLdaError(-1, _library.same_lda_last_error(None).decode())
@@ -483,6 +493,8 @@ def micro_quantize(x, out=None) -> MicroMatrix:
         out.codes = _torch.empty((rows, 64 * groups), dtype=_torch.uint8, device=device)
         out.scales = _torch.empty((rows, 4 * groups), dtype=_torch.uint8, device=device)
         out.width, out.rows = width, rows
+    elif type(out) is not MicroMatrix:
+        raise TypeError("out is a MicroMatrix")
     _run(index, _library.same_lda_micro_quantize, r, _rows(out))
     return out
 
@@ -490,8 +502,8 @@ def micro_quantize(x, out=None) -> MicroMatrix:
 def micro_dequantize(q, dtype=None, out=None):
     """The numbers that a MicroMatrix stands for, in `dtype` (default: float32)."""
     index = _gpu(q, out)
-    out = _output(out, q.shape, dtype, _torch.float32, q.device)
-    _run(index, _library.same_lda_embed, _rows(q), None, 8, 1.0, _rows(out))
+    out, o = _output(out, q.shape, q.rows, q.width, dtype, _torch.float32, q.codes.device)
+    _run(index, _library.same_lda_embed, _rows(q), None, 8, 1.0, o)
     return out
 
 
@@ -501,6 +513,7 @@ def micro_product(a, b, scale=1.0, dtype=None, out=None):
     if type(a) is not MicroMatrix and (a.shape[0] > 16 or a.numel() > 16384):
         a = micro_quantize(a)
     index = _gpu(a, b, out)
-    out = _output(out, (a.shape[0], b.rows), dtype, _torch.float32, b.codes.device)
-    _run(index, _library.same_lda_micro_product, _rows(a), _rows(b), scale, _rows(out))
+    x, rows = _rows(a), a.shape[0]
+    out, o = _output(out, (rows, b.rows), rows, b.rows, dtype, _torch.float32, b.codes.device)
+    _run(index, _library.same_lda_micro_product, x, _rows(b), scale, o)
     return out

@@ -110,6 +110,22 @@ def test_embed_shapes_of_tokens_and_the_longest_and_shortest_lists():
     assert torch.all(binding.embed(T[:0], t) == 0)                # a table without rows: no id names one
 
 
+def test_refusals_on_the_device():
+    """What the binding refuses with tensors on a GPU: types, shapes, places."""
+    T, t = torch.zeros(4, 8, device=DEV), torch.zeros(3, dtype=torch.int64, device=DEV)
+    q = binding.micro_quantize(T)
+    for error, call in [(TypeError, lambda: binding.embed(T, t, dtype=torch.float64)), (TypeError, lambda: binding.embed(T.double(), t)),
+                        (ValueError, lambda: binding.embed(T, t.cpu())), (ValueError, lambda: binding.embed(T.cpu(), t)), (ValueError, lambda: binding.embed(T, t, out=T)),
+                        (ValueError, lambda: binding.embed(T, t, dtype=torch.float16, out=T[:3])), (ValueError, lambda: binding.embed(T.t(), t)),
+                        (binding.SameLdaError, lambda: binding.embed(T, t, float("nan"))), (ValueError, lambda: binding.embed_grad(T[:3], t, 5, out=T)),
+                        (ValueError, lambda: binding.embed_grad(T, t, 5)), (binding.SameLdaError, lambda: binding.embed_grad(T[:3], t, 5, float("inf"))),
+                        (TypeError, lambda: binding.micro_dequantize(q, dtype=torch.int32)), (TypeError, lambda: binding.micro_quantize(T, out=T)),
+                        (binding.SameLdaError, lambda: binding.micro_quantize(T[:, :4], out=q)), (binding.SameLdaError, lambda: binding.micro_product(q, binding.micro_quantize(T[:, :7].contiguous()))),
+                        (ValueError, lambda: binding.micro_product(q, q, out=T)), (ValueError, lambda: binding.micro_product(T.cpu(), q))]:
+        with pytest.raises(error):
+            call()
+
+
 def test_padding_never_reads_the_table_nor_the_gradient():
     T = torch.full((5, 64), float("nan"), device=DEV)
     T[2] = 1.0
