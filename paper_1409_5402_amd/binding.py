@@ -327,8 +327,9 @@ class SameLDA:
 
 
 # ---- Word tables as an embedding.  These functions take torch tensors on one GPU, run on torch's current stream of that
-# GPU and return at once; what a call allocates (outputs, scratch) comes from torch's allocator.  A call's own time on the host
-# counts where tokens come one by one, so operands are checked and passed on in few steps.
+# GPU and return at once; what a call allocates (outputs, scratch) comes from torch's allocator.  Nothing is recorded for torch's
+# autograd: embed_grad is the backward pass of embed.  A call's own time on the host counts where tokens come one by one, so
+# operands are checked and passed on in few steps.
 
 MICRO = 3
 _pack_rows = struct.Struct("PPqqii").pack          # same_lda_rows, passed by the address of its bytes

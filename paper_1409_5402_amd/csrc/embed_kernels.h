@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a)
 // kFewTiles tiles the placement adds them up for itself); placement, which adds up the digits before its own.
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr uint32_t kFewTiles = 64;
+constexpr uint32_t kFewTiles = 64;                               // 50,000 tokens x 64: 52 us; beyond it does not pay, 100,000: 60 us by itself, 55 in a launch
 
 __device__ __forceinline__ int32_t word_of(const Tokens& tokens, int64_t i, int64_t rows)
 {
@@ -355,6 +355,8 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int64_t w, int c, f
     store_chunk<TO, V>(to, acc);
 }
 
+// Memory bound where tokens are many: a million rows of 256 binary32 take 243 us, 4.6 TB/s of what has to be read and written;
+// 65,537 rows of 1024 bf16 37 us, 5.3 TB/s.
 template <class TI, class TO, int V, bool kNarrow>
 __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
 {
