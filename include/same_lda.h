@@ -299,13 +299,14 @@ int same_lda_micro_size(int64_t rows, int32_t width, size_t* code_bytes, size_t*
  * that holds an infinity or a NaN becomes NaN as a whole (s = 255, codes 0).                                       */
 int same_lda_micro_quantize(const same_lda_rows* x, const same_lda_rows* micro_out, void* hip_stream);
 
+#define SAME_LDA_ROUND_ROWS 64
+#define SAME_LDA_ROUND_MAX 16384
 /* out[i][j] = scale * sum_k a[i][k] * b[j][k], both microscaled and of one width, in binary32, rounded once to the output's
  * type: with rows of topic weights and the rows of phi, the predictive weight of every word (same_lda_sddmm is the
  * same product at the nonzeros only, of unrounded matrices).
- *   a            microscaled, or up to 16 rows and SAME_LDA_ROUND_MAX elements of any type: then the product is that of
- *                what same_lda_micro_quantize would make of them, in the one call
+ *   a            microscaled, or up to SAME_LDA_ROUND_ROWS rows and SAME_LDA_ROUND_MAX elements of any type: then the
+ *                product is that of what same_lda_micro_quantize would make of them, in the one call
  *   out          [a->rows][b->rows]                                                                               */
-#define SAME_LDA_ROUND_MAX 16384
 int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out,
                            void* hip_stream);
 

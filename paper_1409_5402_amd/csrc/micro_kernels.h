@@ -104,7 +104,7 @@ struct alignas(4) ScaleWords {
 // With TI a type of numbers the rows of a are such numbers, few enough (kRoundMost of them) for every workgroup to round them for itself:
 // one launch in place of two (16 x 40,000 x 1024, the most: 13.4 us, rounded before 14.2; with the 53,248 of 13 x 50,021 x 4096 it
 // would be 44, 34).
-constexpr int kRoundMost = 16384;
+constexpr int kRoundMost = 16384, kRoundRows = 64;
 
 template <class TO, int MF, int RF, int KW, class TI>
 __global__ __launch_bounds__(256) void micro_product_few_kernel(ProductArgs p)
@@ -112,8 +112,8 @@ __global__ __launch_bounds__(256) void micro_product_few_kernel(ProductArgs p)
     constexpr int kUnroll = MF * RF >= 8 ? 2 : 4;                              // groups in flight
     constexpr bool kRound = !std::is_void<TI>::value;
     __shared__ v4f others[KW > 1 ? KW - 1 : 1][MF][RF][64];
-    __shared__ alignas(16) uint32_t rounded[kRound ? (kRoundMost + 16 * kMicroGroup) / 8 : 1];
-    __shared__ alignas(16) uint8_t rounded_scales[kRound ? (kRoundMost + 16 * kMicroGroup) / 32 : 4];
+    __shared__ alignas(16) uint32_t rounded[kRound ? (kRoundMost + 16 * MF * kMicroGroup) / 8 : 1];
+    __shared__ alignas(16) uint8_t rounded_scales[kRound ? (kRoundMost + 16 * MF * kMicroGroup) / 32 : 4];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int64_t pitch = (int64_t)p.groups * 64, spitch = (int64_t)p.groups * 4;
     const uint8_t *a = p.a, *a_scales = p.a_scales;

@@ -249,6 +249,16 @@ void product_few_by_shape(same::ProductArgs& p, hipStream_t st)
     else                             product_few<TO, MF, 4, 4, TI>(p, st);
 }
 
+// Rows of numbers, rounded in the call: one launch in place of two (32 x 2000 x 256: 6.5 us, 14.2).  Beyond 16 rows they are short, and not
+// shared out.
+template <class TO, class TI>
+void product_rounded(same::ProductArgs& p, hipStream_t st)
+{
+    if (p.rows_a <= 16)      product_few_by_shape<TO, 1, TI>(p, st);
+    else if (p.rows_a <= 32) product_few<TO, 2, 1, 1, TI>(p, st);
+    else                     product_few<TO, 4, 1, 1, TI>(p, st);
+}
+
 // Which kernel (us at rows of a x rows of b x width, the first number the chosen one's):
 //   up to 16 rows of a          straight from memory; above, tiles, but up to 32 rows of a by a table below 32 MB of longer rows
 //                               (32 x 5000 x 4096: 9.2, tiles 12.6; 32 x 50,021 x 4096: tiles 34, 44; 32 x 100,000 x 256: tiles 7.0, 10.1)
@@ -264,9 +274,9 @@ template <class TO>
 void product_to(same::ProductArgs& p, int32_t type_a, hipStream_t st)
 {
     switch (type_a) {
-        case SAME_LDA_FLOAT:  return product_few_by_shape<TO, 1, float>(p, st);
-        case SAME_LDA_BFLOAT: return product_few_by_shape<TO, 1, __bf16>(p, st);
-        case SAME_LDA_HALF:   return product_few_by_shape<TO, 1, _Float16>(p, st);
+        case SAME_LDA_FLOAT:  return product_rounded<TO, float>(p, st);
+        case SAME_LDA_BFLOAT: return product_rounded<TO, __bf16>(p, st);
+        case SAME_LDA_HALF:   return product_rounded<TO, _Float16>(p, st);
     }
     if (p.rows_a <= 16) return product_few_by_shape<TO, 1>(p, st);
     if (p.rows_a <= 32 && p.groups > 2 && p.rows_b * p.groups * 64 < (int64_t)1 << 25) return product_few_by_shape<TO, 2>(p, st);
@@ -405,10 +415,10 @@ int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float
         return fail_without_handle(SAME_LDA_EINVAL, "micro_product: %lld rows by %lld rows do not give %lld x %d", (long long)a->rows, (long long)b->rows,
                                    (long long)out->rows, out->width);
     if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "micro_product: the scale must be finite");
-    if (a->type != SAME_LDA_MICRO && (a->rows > 16 || a->rows * a->width > SAME_LDA_ROUND_MAX))
-        return fail_without_handle(SAME_LDA_EINVAL, "micro_product: a must be microscaled beyond 16 rows and %d elements (got %lld x %d)", SAME_LDA_ROUND_MAX,
-                                   (long long)a->rows, a->width);
-    static_assert(SAME_LDA_ROUND_MAX == same::kRoundMost, "");
+    if (a->type != SAME_LDA_MICRO && (a->rows > SAME_LDA_ROUND_ROWS || a->rows * a->width > SAME_LDA_ROUND_MAX))
+        return fail_without_handle(SAME_LDA_EINVAL, "micro_product: a must be microscaled beyond %d rows or %d elements (got %lld x %d)", SAME_LDA_ROUND_ROWS,
+                                   SAME_LDA_ROUND_MAX, (long long)a->rows, a->width);
+    static_assert(SAME_LDA_ROUND_MAX == same::kRoundMost && SAME_LDA_ROUND_ROWS == same::kRoundRows, "");
     if (a->rows == 0) return SAME_LDA_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const same_lda_rows whole = {a->data, nullptr, a->rows, a->stride, 8, a->type};                                      // alignment of rows, whatever their width

@@ -82,7 +82,7 @@ def test_shapes_types_tokens_and_scales_are_refused():
     refused(L.same_lda_micro_quantize(ref(a), ref(rows(type=M, rows=5)), None), "into")
     refused(L.same_lda_micro_quantize(ref(a), ref(rows(type=M, width=9)), None), "into")
     refused(L.same_lda_micro_product(ref(m), ref(a), 1.0, ref(rows(width=4)), None), "must be microscaled")
-    refused(L.same_lda_micro_product(ref(rows(rows=17)), ref(m), 1.0, ref(rows(rows=17, width=4)), None), "must be microscaled")
+    refused(L.same_lda_micro_product(ref(rows(rows=65)), ref(m), 1.0, ref(rows(rows=65, width=4)), None), "must be microscaled")
     refused(L.same_lda_micro_product(ref(rows(rows=2, width=8193)), ref(rows(type=M, width=8193)), 1.0, ref(rows(rows=2, width=4)), None), "must be microscaled")
     refused(L.same_lda_micro_product(ref(m), ref(rows(type=M, width=9)), 1.0, ref(rows(width=4)), None), "elements")
     refused(L.same_lda_micro_product(ref(m), ref(m), 1.0, ref(rows(width=5)), None), "do not give")
