@@ -76,33 +76,33 @@ constexpr int64_t kComputeUnits = 256;
 constexpr int64_t kMaxGroups = (int64_t)1 << 22;     // workgroups of a launch (256 threads each: below 2^32 threads)
 
 template <class TI, class TO, int V>
-int embed_launch(same::EmbedArgs& a, int32_t width, hipStream_t st)
+int embed_launch(const char* call, same::EmbedArgs& a, int32_t width, hipStream_t st)
 {
     a.chunks = width / V;
     a.lanes_log2 = lanes_log2_for(a.chunks);
     const int64_t per = (int64_t)256 >> a.lanes_log2;
     const int64_t groups = at_most(a.n > 2 * per * kComputeUnits ? (a.n + 2 * per - 1) / (2 * per) : (a.n + per - 1) / per, kMaxGroups);   // two tokens in turn where they are many
     hipLaunchKernelGGL((same::embed_kernel<TI, TO, V>), dim3((unsigned)groups), dim3(256), 0, st, a);
-    return launched("embed");
+    return launched(call);
 }
 
 // The widest chunks that both sides are aligned for: 16 bytes of the narrower type, two elements, or one.
 template <class TI, class TO>
-int embed_by_width(same::EmbedArgs& a, const same_lda_rows* table, const same_lda_rows* out, hipStream_t st)
+int embed_by_width(const char* call, same::EmbedArgs& a, const same_lda_rows* table, const same_lda_rows* out, hipStream_t st)
 {
     constexpr int kWide = sizeof(TI) == 4 && sizeof(TO) == 4 ? 4 : 8;
-    if (out->width % kWide == 0 && chunks_fit(table, kWide) && chunks_fit(out, kWide)) return embed_launch<TI, TO, kWide>(a, out->width, st);
-    if (out->width % 2 == 0 && chunks_fit(table, 2) && chunks_fit(out, 2)) return embed_launch<TI, TO, 2>(a, out->width, st);
-    return embed_launch<TI, TO, 1>(a, out->width, st);
+    if (out->width % kWide == 0 && chunks_fit(table, kWide) && chunks_fit(out, kWide)) return embed_launch<TI, TO, kWide>(call, a, out->width, st);
+    if (out->width % 2 == 0 && chunks_fit(table, 2) && chunks_fit(out, 2)) return embed_launch<TI, TO, 2>(call, a, out->width, st);
+    return embed_launch<TI, TO, 1>(call, a, out->width, st);
 }
 
 template <class TI>
-int embed_to(same::EmbedArgs& a, const same_lda_rows* table, const same_lda_rows* out, hipStream_t st)
+int embed_to(const char* call, same::EmbedArgs& a, const same_lda_rows* table, const same_lda_rows* out, hipStream_t st)
 {
     switch (out->type) {
-        case SAME_LDA_FLOAT:  return embed_by_width<TI, float>(a, table, out, st);
-        case SAME_LDA_BFLOAT: return embed_by_width<TI, __bf16>(a, table, out, st);
-        default:              return embed_by_width<TI, _Float16>(a, table, out, st);
+        case SAME_LDA_FLOAT:  return embed_by_width<TI, float>(call, a, table, out, st);
+        case SAME_LDA_BFLOAT: return embed_by_width<TI, __bf16>(call, a, table, out, st);
+        default:              return embed_by_width<TI, _Float16>(call, a, table, out, st);
     }
 }
 
@@ -131,7 +131,7 @@ GradSpace grad_space(const same_lda_rows* grad, int64_t rows)
 {
     const int64_t n = grad->rows, width = grad->width;
     GradSpace s = {};
-    if (few_tokens(n, rows, grad)) return s;
+    if (n == 0 || few_tokens(n, rows, grad)) return s;
     size_t at = 0;
     const auto part = [&at](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     int bits = 1;
@@ -316,10 +316,10 @@ int same_lda_embed(const same_lda_rows* table, const void* tokens, int32_t token
                          out->rows, scale, out->data, out->stride, 0, 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     switch (table->type) {
-        case SAME_LDA_FLOAT:  return embed_to<float>(a, table, out, st);
-        case SAME_LDA_BFLOAT: return embed_to<__bf16>(a, table, out, st);
-        case SAME_LDA_HALF:   return embed_to<_Float16>(a, table, out, st);
-        default:              return embed_to<uint8_t>(a, table, out, st);
+        case SAME_LDA_FLOAT:  return embed_to<float>("embed", a, table, out, st);
+        case SAME_LDA_BFLOAT: return embed_to<__bf16>("embed", a, table, out, st);
+        case SAME_LDA_HALF:   return embed_to<_Float16>("embed", a, table, out, st);
+        default:              return embed_to<uint8_t>("embed", a, table, out, st);
     }
 }
 
@@ -346,6 +346,11 @@ int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t t
     if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes || (uintptr_t)workspace % 16))
         return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: needs %zu bytes of workspace aligned to 16 (got %zu)", s.bytes, workspace ? workspace_bytes : (size_t)0);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (n == 0) {                                                    // a table of zeros: the lookup of rows that no table holds
+        const same_lda_rows none = {nullptr, nullptr, 0, 0, table_grad->width, SAME_LDA_FLOAT};
+        same::EmbedArgs zeros = {nullptr, nullptr, 0, 0, {nullptr, 0}, rows, 1.0f, table_grad->data, table_grad->stride, 0, 0};
+        return embed_to<float>("embed_grad", zeros, &none, table_grad, st);
+    }
     char* const w = static_cast<char*>(workspace);
     same::GradArgs a = {grad->data, grad->stride, nullptr, nullptr, rows, scale, accumulate, table_grad->data, table_grad->stride,
                         nullptr, s.ranges, grad->width, 0, 0, {tokens, token_bytes == 8}, (int32_t)n, 0, 0};
