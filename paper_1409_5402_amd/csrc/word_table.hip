@@ -120,11 +120,12 @@ constexpr int64_t kSmallTiles = 1 << 22;                             // up to th
 
 // One launch without a sort: up to 8192 tokens with two workgroups per compute unit, or 16,384 with one where rows of the gradient
 // are short (16,384 tokens into 2000 x 64 f32: 27 us, sorted 42; into 30,000 x 1024 bf16: 59, 60; into 2000 x 1024 f32, where the
-// most frequent word keeps one compute unit busy: 56, 44); and a grid below 2^32 threads.
+// most frequent word keeps one compute unit busy: 56, 44); and a grid below 2^32 threads: 1024 for every 256 words begun, and
+// every 64 chunks of a row.
 constexpr int kFewerTokens = 8192;
 bool few_tokens(int64_t n, int64_t rows, const same_lda_rows* grad)
 {
-    return n <= ((int64_t)grad->width * element_bytes(grad->type) <= 2048 ? same::kFewTokens : kFewerTokens) && rows * ((grad->width + 63) / 64) < (int64_t)1 << 30;
+    return n <= ((int64_t)grad->width * element_bytes(grad->type) <= 2048 ? same::kFewTokens : kFewerTokens) && (rows + 256) * ((grad->width + 63) / 64) < (int64_t)1 << 30;
 }
 
 GradSpace grad_space(const same_lda_rows* grad, int64_t rows)

@@ -29,3 +29,14 @@ def test_gradient_of_no_tokens_fills_rows_only(width, stride, offset, dtype):
         binding.embed_grad(torch.zeros(0, width, dtype=grad, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV), out=out)
         assert torch.all(out == 0.0)
     check()
+
+
+def test_gradient_of_few_tokens_into_the_longest_tables():
+    """The last table that a launch of a workgroup per 256 words takes, and the first ones that go by way of the sort."""
+    for rows in ((1 << 30) - 257, (1 << 30) - 1, 1 << 30):
+        t = torch.tensor([rows - 1, 0, rows, rows - 1, -1, 77], device=DEV)
+        g = torch.tensor([[1.0], [2.0], [50.0], [4.0], [60.0], [8.0]], device=DEV)
+        out = torch.ones((rows, 1), dtype=torch.bfloat16, device=DEV)
+        binding.embed_grad(g, t, out=out)
+        assert out[rows - 1].item() == 5.0 and out[0].item() == 2.0 and out[77].item() == 8.0 and out.count_nonzero().item() == 3
+        del out

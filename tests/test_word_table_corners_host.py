@@ -17,3 +17,13 @@ def test_a_gradient_of_no_tokens_needs_no_workspace():
     for v, w in [(1, 1), ((1 << 30) - 1, 1), (1 << 30, 1), ((1 << 31) - 1, 1), (1 << 25, 4096), ((1 << 31) - 1, 1 << 20)]:
         for type in (F, B, H):
             assert workspace(0, v, w, type) == 0
+
+
+def test_a_gradient_in_one_launch_stays_below_the_largest_grid():
+    """Up to 8192 tokens need no workspace where they are taken in one launch, with 1024 threads for every 256 words and 64 chunks of a
+    row at least; a launch has fewer than 2^32."""
+    for v in [(1 << 30) - 1024, (1 << 30) - 257, (1 << 30) - 256, (1 << 30) - 255, (1 << 30) - 1, 1 << 30, (1 << 29) - 1, (1 << 29) - 128, (1 << 28) - 1, (1 << 28) - 257, (1 << 22) - 1]:
+        for w in (1, 64, 65, 128, 129, 256, 1 << 14, 1 << 20):
+            if workspace(5, v, w) == 0:
+                assert -(-v // 256) * -(-w // 64) * 1024 < 1 << 32, (v, w)
+    assert workspace(8192, 4_000_000, 64) == 0 and workspace(5, (1 << 30) - 1024, 1) == 0          # and is not left without need
