@@ -394,11 +394,13 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
 }
 
 // The rows of the long runs that start in the ranges of a workgroup, one range per group of lanes: the partial sums of a run in
-// order.  A run of more than kLongJoin of them is left to the whole workgroup: its groups sum consecutive parts, then the
-// parts' sums are added in pairs, pairs of pairs and so on.  Groups are of few lanes (kJoinLanesLog2): the hottest word's partial sums (2 MB of a million
-// tokens of natural text at 256 elements) are then read by as many compute units as there are groups to a row.
+// order.  A run of more than kLongJoin of them is left to the whole workgroup: kJoinParts of its groups sum consecutive parts, then the
+// parts' sums are added in pairs, pairs of pairs and so on.  Groups are of few lanes (kJoinLanesLog2 at most): the hottest word's
+// partial sums (2 MB of a million tokens of natural text at 256 elements) are then read by as many compute units as there are groups to
+// a row.  The number of parts is that of the widest groups, so that narrower ones (rows of few chunks) give the same sums.
 constexpr int kLongJoin = 32;
 constexpr int kJoinLanesLog2 = 3;
+constexpr int kJoinParts = 1024 >> kJoinLanesLog2;
 
 // acc += rows first .. behind - 1 of the partial sums of a run: row 0 is `head`, row k is 2 (item + k)
 template <int V>
@@ -420,8 +422,8 @@ __global__ __launch_bounds__(1024) void embed_grad_join_kernel(GradArgs a)
     __shared__ int32_t later[1024 / kLongJoin + 2];                 // ranges that a long join starts in: at least kLongJoin apart
     __shared__ int32_t n_later;
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2, groups = 1024 >> a.lanes_log2;
-    const int column = blockIdx.y * lanes + lane;
-    const int c = column < a.chunks ? column : a.chunks - 1;
+    const int64_t column = ((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * lanes + lane;
+    const int c = column < a.chunks ? (int)column : a.chunks - 1;
     const int64_t n = a.start[a.rows];
     if (threadIdx.x == 0) n_later = 0;
     __syncthreads();
@@ -446,11 +448,11 @@ __global__ __launch_bounds__(1024) void embed_grad_join_kernel(GradArgs a)
         const int64_t it = later[q], from = it * kLongRun;
         const int32_t w = a.sorted[from + kLongRun - 1].word;              // the run goes on behind its first range
         const int64_t s = a.start[w], e = a.start[w + 1];
-        const int64_t rows = (e - 1) / kLongRun - it + 1, each = (rows + groups - 1) / groups;
+        const int64_t rows = (e - 1) / kLongRun - it + 1, each = (rows + kJoinParts - 1) / kJoinParts;
         const int64_t lo = group * each, hi = lo + each < rows ? lo + each : rows;
         float acc[V] = {};
-        add_partials<V>(acc, a, it, s == from ? 2 * it : 2 * it + 1, lo, hi, c);
-for (int o = groups >> 1; o > 0; o >>= 1) {
+        if (group < kJoinParts) add_partials<V>(acc, a, it, s == from ? 2 * it : 2 * it + 1, lo, hi, c);
+        for (int o = kJoinParts >> 1; o > 0; o >>= 1) {
             if (group >= o && group < 2 * o)
 #pragma unroll
                 for (int j = 0; j < V; ++j) part[j * 512 + threadIdx.x - (o << a.lanes_log2)] = acc[j];

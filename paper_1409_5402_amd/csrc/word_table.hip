@@ -190,10 +190,10 @@ int grad_launch(same::GradArgs& a, hipStream_t st)
     const dim3 grid((unsigned)at_most((a.ranges + a.rows + per - 1) / per, most), across);
     if (a.lanes_log2 < 4) hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V, true>), grid, dim3(256), 0, st, a);
     else                  hipLaunchKernelGGL((same::embed_grad_kernel<TI, TO, V, false>), grid, dim3(256), 0, st, a);
-    if (a.lanes_log2 > same::kJoinLanesLog2 && a.chunks <= 65535 << same::kJoinLanesLog2) a.lanes_log2 = same::kJoinLanesLog2;
+    if (a.lanes_log2 > same::kJoinLanesLog2) a.lanes_log2 = same::kJoinLanesLog2;
     const int64_t items = (int64_t)1024 >> a.lanes_log2;             // ranges of a workgroup
-    hipLaunchKernelGGL((same::embed_grad_join_kernel<TO, V>), dim3((unsigned)((a.ranges + items - 1) / items), (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2)),
-                       dim3(1024), 0, st, a);
+    const unsigned columns = (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2), deep = (columns + 65534) / 65535;   // 65,535 of them side by side
+    hipLaunchKernelGGL((same::embed_grad_join_kernel<TO, V>), dim3((unsigned)((a.ranges + items - 1) / items), (columns + deep - 1) / deep, deep), dim3(1024), 0, st, a);
     return launched("embed_grad");
 }
 
