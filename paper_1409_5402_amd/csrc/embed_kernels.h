@@ -467,19 +467,25 @@ __global__ __launch_bounds__(1024) void embed_grad_join_kernel(GradArgs a)
 }
 
 // Few tokens: one launch.  A workgroup owns up to `words` words, reads the whole list, keeps the places of its words' tokens in order
-// and sorts them by word in LDS.  A word's row is then summed by a group of lanes, or by all groups where its run is long.
+// and sorts them by word in LDS.  A word's row is then summed by a group of lanes, or, of a run of more than kLongRun tokens, by all
+// groups: the run is cut into 256 pieces, of 16 tokens at least, every kColumns-th piece is added up in order, then these sums in
+// pairs, pairs of pairs and so on.  A group takes a piece at a time and kColumns is the least number of groups that a workgroup has, so
+// the additions are the same for every number of groups, and a term passes 64 + 16 + 4 of them at most.  (One part per group was
+// 73 us for 16,384 tokens of one word x 64 f32, this is 78; batches of natural text take the same time within 5 %.)
 // The words go to the workgroups in turn, 2^unit_log2 at a time (128 bytes of the table): with consecutive words the
 // workgroup of the most frequent ones had most of the tokens (8192 tokens, 30,000 x 1024 bf16: 103 us, in turn 37).
 constexpr int kFewTokens = 16384;                                   // 1024 for each of the kRows of the kernel that takes the most
 constexpr int kFewWords = 256;                                      // most words of a workgroup
+constexpr int kColumns = 16;
 
+// (two workgroups per compute unit where 64 registers are enough, which is where V < 8)
 template <class TI, class TO, int V, int kRows>
-__global__ __launch_bounds__(1024) void embed_grad_few_kernel(GradArgs a)
+__global__ __launch_bounds__(1024, V < 8 && kRows == 8 ? 8 : 4) void embed_grad_few_kernel(GradArgs a)
 {
     constexpr int kTokens = 1024 * kRows;
     __shared__ union {
-        uint32_t list[kTokens];                                  // number of the word in the upper half, place in the lower
-        float part[512 * V];
+        uint32_t list[kTokens];                                     // number of the word in the upper half, place in the lower
+        float part[1024 * V];
     } lds;
     __shared__ uint16_t sorted[kTokens];                         // places, by word
     __shared__ uint32_t cnt[16][kFewWords];                         // per wave and word: tokens, then the next position among the sorted
@@ -606,18 +612,35 @@ __global__ __launch_bounds__(1024) void embed_grad_few_kernel(GradArgs a)
     __syncthreads();
     for (int q = 0; q < n_long; ++q) {                              // in any order: each is a sum of its own
         const int word = long_words[q];
-        const uint32_t p0 = first[word], run = first[word + 1] - p0, part = (run + groups - 1) / groups;
-        const uint32_t lo = p0 + (uint32_t)group * part, hi = lo + part < p0 + run ? lo + part : p0 + run;
-        float acc[V] = {};
-        sum(acc, lo, hi);
-        for (int o = groups >> 1; o > 0; o >>= 1) {
+        const uint32_t p0 = first[word], behind = first[word + 1], each = max(8u * ((behind - p0 + 2047u) / 2048u), 16u);   // 8 at a time
+        const uint32_t pieces = (behind - p0 + each - 1u) / each;
+        float acc[V] = {};                                          // of the first kColumns groups: a column each
+        for (uint32_t k0 = 0; k0 < pieces; k0 += groups) {
+            const uint32_t p = p0 + (k0 + (uint32_t)group) * each;
+            float piece[V] = {};
+            sum(piece, p, p + each < behind ? p + each : behind);
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] += piece[j];
+            if (groups > kColumns) {
+                if (group >= kColumns)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) lds.part[j * 1024 + threadIdx.x] = piece[j];
+                __syncthreads();
+                if (group < kColumns)
+                    for (int o = kColumns; o < groups && k0 + (uint32_t)o < pieces; o += kColumns)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) acc[j] += lds.part[j * 1024 + threadIdx.x + (o << a.lanes_log2)];
+                __syncthreads();
+            }
+        }
+        for (int o = kColumns >> 1; o > 0; o >>= 1) {
             if (group >= o && group < 2 * o)
 #pragma unroll
-                for (int j = 0; j < V; ++j) lds.part[j * 512 + threadIdx.x - (o << a.lanes_log2)] = acc[j];
+                for (int j = 0; j < V; ++j) lds.part[j * 1024 + threadIdx.x] = acc[j];
             __syncthreads();
             if (group < o)
 #pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] += lds.part[j * 512 + threadIdx.x];
+                for (int j = 0; j < V; ++j) acc[j] += lds.part[j * 1024 + threadIdx.x + (o << a.lanes_log2)];
             __syncthreads();
         }
         if (group == 0 && mine) write_row<TO, V>(a, word_at(word), c, acc, true);
