@@ -281,9 +281,11 @@ int same_lda_embed(const same_lda_rows* table, const void* tokens, int32_t token
 /* The gradient of that lookup with respect to the table:
  *   table_grad[w] = scale * sum of grad[i] over the tokens i with tokens[i] = w         (accumulate = 0)
  *   table_grad[w] += the same, for the words that have a token; others are not touched  (accumulate != 0)
- * The tokens are sorted by word and every row is one sum in binary32 in an order that depends on the tokens alone, so equal
- * calls give equal bits; the sum is rounded once to the type of table_grad.  Tokens that stand for no word add nothing:
- * their rows of grad are not read.
+ * The tokens are sorted by word and every row is one sum in binary32, in an order that depends on the tokens, the shapes
+ * and the type of grad, but not on addresses, strides, the tokens' type or that of table_grad: equal numbers give equal
+ * bits.  Up to 64 terms of a word are added one by one, more are cut into pieces of at most 64, so that none of its t
+ * terms passes more than 100 + t / 8192 additions; the sum is rounded once to the type of table_grad.  Tokens that stand
+ * for no word add nothing: their rows of grad are not read.
  *   workspace    as many bytes as same_lda_embed_grad_workspace says for the same matrices (it reads their shapes), aligned
  *                to 16; its contents are scratch, in use until the call's kernels have ended                          */
 int same_lda_embed_grad_workspace(const same_lda_rows* grad, const same_lda_rows* table_grad, size_t* bytes);

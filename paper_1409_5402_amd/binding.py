@@ -460,7 +460,8 @@ _EMPTY = 16        # stands for the address of a list of no tokens: not null, ne
 def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumulate=False):
     """The gradient of ``embed(table, tokens, scale)`` with respect to a table of `rows` rows, from that of its result: `grad`
     of shape tokens.shape + (width,).  `dtype` (default: grad's) is the result's type.  `out`: where it is written, or added to with
-    ``accumulate=True``; `rows` is then out's.  Equal calls give equal bits."""
+    ``accumulate=True``; `rows` is then out's.  Equal numbers of
+    one type and shape give equal bits, whatever their strides."""
     ids = _token_ids(tokens)
     if grad.shape[:-1] != tokens.shape:
         raise ValueError(f"grad has shape {tuple(grad.shape)}, tokens {tuple(tokens.shape)}")

@@ -80,8 +80,9 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a)
 }
 
 // ---- Gradient.  The tokens are sorted by word, stable, with the padding behind the last word; the positions of one word are
-// then a run in ascending order, and its row of the gradient is one sum over the run in binary32, in an order that depends
-// on the tokens alone (no atomics: two calls give the same bits).
+// then a run in ascending order, and its row of the gradient is one sum over the run in binary32.  The order of its additions
+// depends on the tokens, and on whether they are taken in one launch (their number, the bytes of a row of grad, the table's size);
+// not on how rows are cut into chunks and lanes, which addresses and strides decide, and no atomics: equal numbers, equal bits.
 
 // Stable radix sort of the words by digits of `bits` bits (at most kDigitBits), least significant first.  A workgroup owns a
 // tile of 256 * R consecutive tokens.  Per pass: counts per (digit, tile); for every digit their exclusive sum over the tiles (up to
