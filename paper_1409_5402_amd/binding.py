@@ -403,6 +403,16 @@ def _rows(x) -> bytes:
     return _pack_rows(x.data_ptr(), 0, rows, stride if rows > 1 else width, width, kind)
 
 
+def _micro(name, x):
+    if type(x) is not MicroMatrix:
+        raise TypeError(f"{name} is a MicroMatrix (micro_quantize makes one), not a {type(x).__name__}")
+
+
+def _numbers(name, x):
+    if type(x) is MicroMatrix:
+        raise TypeError(f"{name} is a tensor, not a MicroMatrix")
+
+
 def _gpu(*operands) -> int:
     """The number of the GPU that all operands are on."""
     index = operands[0].get_device()
@@ -437,6 +447,7 @@ def _output(out, shape, rows, width, dtype, default, device):
         kind = _type_of(dtype or default)
         out = _torch.empty(shape, dtype=dtype or default, device=device)
         return out, _pack_rows(out.data_ptr(), 0, rows, width, width, kind)
+    _numbers("out", out)
     if out.shape != shape or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype or out.dtype}")
     return out, _rows(out if out.dim() == 2 else out.view(-1, width))
@@ -463,6 +474,7 @@ def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumul
     ``accumulate=True``; `rows` is then out's.  Equal numbers of
     one type and shape give equal bits, whatever their strides."""
     ids = _token_ids(tokens)
+    _numbers("grad", grad)
     if grad.shape[:-1] != tokens.shape:
         raise ValueError(f"grad has shape {tuple(grad.shape)}, tokens {tuple(tokens.shape)}")
     if out is None and (accumulate or rows is None):
@@ -485,6 +497,7 @@ def micro_quantize(x, out=None) -> MicroMatrix:
     """A matrix in microscaled four-bit floating point."""
     if _torch is None:
         _setup()
+    _numbers("x", x)
     index = _gpu(x, out)
     r = _rows(x)
     if out is None:
@@ -503,6 +516,7 @@ def micro_quantize(x, out=None) -> MicroMatrix:
 
 def micro_dequantize(q, dtype=None, out=None):
     """The numbers that a MicroMatrix stands for, in `dtype` (default: float32)."""
+    _micro("q", q)
     index = _gpu(q, out)
     out, o = _output(out, q.shape, q.rows, q.width, dtype, _torch.float32, q.codes.device)
     _run(index, _library.same_lda_embed, _rows(q), None, 8, 1.0, o)
@@ -520,6 +534,7 @@ def _rounded_in_the_call(a, b) -> bool:
 def micro_product(a, b, scale=1.0, dtype=None, out=None):
     """scale * a @ b.T in `dtype` (default: float32) for a MicroMatrix `b`; `a` is a MicroMatrix, or a matrix that is rounded to
     one first."""
+    _micro("b", b)
     if type(a) is not MicroMatrix and not _rounded_in_the_call(a, b):
         a = micro_quantize(a)
     index = _gpu(a, b, out)

@@ -40,3 +40,12 @@ def test_gradient_of_few_tokens_into_the_longest_tables():
         binding.embed_grad(g, t, out=out)
         assert out[rows - 1].item() == 5.0 and out[0].item() == 2.0 and out[77].item() == 8.0 and out.count_nonzero().item() == 3
         del out
+
+
+def test_microscaled_outputs_are_refused():
+    x, t = torch.zeros(4, 8, device=DEV), torch.zeros(4, dtype=torch.int64, device=DEV)
+    q = binding.micro_quantize(x)
+    for call in (lambda: binding.embed(x, t, out=q), lambda: binding.embed_grad(x, t, out=q), lambda: binding.micro_dequantize(q, out=q),
+                 lambda: binding.micro_product(x, q, out=binding.micro_quantize(torch.zeros(4, 4, device=DEV)))):
+        with pytest.raises(TypeError, match="MicroMatrix"):
+            call()

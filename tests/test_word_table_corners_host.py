@@ -1,6 +1,8 @@
 """Workspaces and refusals of the word-table operators at the borders of what they take: everything is found on the host."""
 import ctypes
 
+import pytest
+import torch
 
 from paper_1409_5402_amd import binding
 from test_word_tables_host import B, F, H, rows
@@ -27,3 +29,13 @@ def test_a_gradient_in_one_launch_stays_below_the_largest_grid():
             if workspace(5, v, w) == 0:
                 assert -(-v // 256) * -(-w // 64) * 1024 < 1 << 32, (v, w)
     assert workspace(8192, 4_000_000, 64) == 0 and workspace(5, (1 << 30) - 1024, 1) == 0          # and is not left without need
+
+
+def test_tensors_and_microscaled_matrices_are_told_apart():
+    """Where one is given for the other, the call says so."""
+    x, t = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+    q = binding.MicroMatrix(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 4, dtype=torch.uint8), 8)
+    for call in (lambda: binding.micro_product(x, x), lambda: binding.micro_product(q, x), lambda: binding.micro_product(torch.zeros(100, 8), x), lambda: binding.micro_dequantize(x),
+                 lambda: binding.embed_grad(q, t, 5), lambda: binding.micro_quantize(q)):
+        with pytest.raises(TypeError, match="MicroMatrix"):
+            call()
