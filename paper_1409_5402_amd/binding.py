@@ -470,19 +470,23 @@ _EMPTY = 16        # stands for the address of a list of no tokens: not null, ne
 
 def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumulate=False):
     """The gradient of ``embed(table, tokens, scale)`` with respect to a table of `rows` rows, from that of its result: `grad`
-    of shape tokens.shape + (width,).  `dtype` (default: grad's) is the result's type.  `out`: where it is written, or added to with
+    of shape tokens.shape + (width,), copied first where its rows are not contiguous or share memory (an expanded tensor).  `dtype` (default: grad's) is the result's type.  `out`: where it is written, or added to with
     ``accumulate=True``; `rows` is then out's.  Equal numbers of
     one type and shape give equal bits, whatever their strides."""
     ids = _token_ids(tokens)
     _numbers("grad", grad)
-    if grad.shape[:-1] != tokens.shape:
+    if grad.dim() != tokens.dim() + 1 or grad.shape[:-1] != tokens.shape:
         raise ValueError(f"grad has shape {tuple(grad.shape)}, tokens {tuple(tokens.shape)}")
     if out is None and (accumulate or rows is None):
         raise ValueError("accumulate needs out" if accumulate else "rows or out must say how many rows the table has")
     index = _gpu(ids, grad, out)
     width = grad.shape[-1]
     rows = out.shape[0] if rows is None else int(rows)
-    g = _rows(grad if grad.dim() == 2 else grad.reshape(-1, width))
+    flat = grad if grad.dim() == 2 else grad.reshape(ids.numel(), width)
+    stride, inner = flat.stride()
+    if inner != 1 and width > 1 or stride < width and len(flat) > 1:
+        flat = flat.contiguous()
+    g = _rows(flat)
     out, o = _output(out, (rows, width), rows, width, dtype, grad.dtype, ids.device)
     n = c_size_t()
     if _library.same_lda_embed_grad_workspace(g, o, byref(n)):

@@ -49,3 +49,18 @@ def test_microscaled_outputs_are_refused():
                  lambda: binding.micro_product(x, q, out=binding.micro_quantize(torch.zeros(4, 4, device=DEV)))):
         with pytest.raises(TypeError, match="MicroMatrix"):
             call()
+
+
+def test_gradient_of_rows_that_share_memory_or_are_not_contiguous():
+    """What torch's backward passes hand on: of a sum the expanded gradient, of a transposed result a transposed one."""
+    t = torch.tensor([[1, 2, 3], [3, -1, 0]], device=DEV)
+    row = torch.arange(1.0, 6.0, device=DEV)
+    for shape, ids in (((6, 5), t.view(6)), ((2, 3, 5), t)):
+        for g in (row.expand(shape), torch.tensor(1.0, device=DEV).expand(shape), torch.zeros(2, 1, 1, device=DEV).add(row[:2].view(2, 1, 1)).expand(2, 3, 5).reshape(shape),
+                  torch.randn(5, 6, device=DEV).t().reshape(shape) if len(shape) == 3 else torch.randn(5, 6, device=DEV).t(), torch.randn(6, 10, device=DEV)[:, ::2].view(shape)):
+            assert torch.equal(binding.embed_grad(g, ids, 4), binding.embed_grad(g.contiguous(), ids, 4))
+    one = torch.randn(1, 10, device=DEV)[:, ::2]
+    assert torch.equal(binding.embed_grad(one, torch.tensor([2], device=DEV), 3)[2], one[0])
+    x = torch.randn(4, 5, device=DEV, requires_grad=True)
+    (x[t.view(6).clamp(min=0)] * (t.view(6, 1) >= 0)).sum().backward()
+    assert torch.equal(binding.embed_grad(torch.ones((), device=DEV).expand(6, 5), t.view(6), 4), x.grad)

@@ -39,3 +39,10 @@ def test_tensors_and_microscaled_matrices_are_told_apart():
                  lambda: binding.embed_grad(q, t, 5), lambda: binding.micro_quantize(q)):
         with pytest.raises(TypeError, match="MicroMatrix"):
             call()
+
+
+def test_gradients_without_a_row_are_refused():
+    with pytest.raises(ValueError, match="grad has shape"):
+        binding.embed_grad(torch.tensor(1.0), torch.tensor(1), 5)
+    with pytest.raises(ValueError, match="grad has shape"):
+        binding.embed_grad(torch.zeros(4), torch.zeros(4, dtype=torch.int64), 5)
