@@ -213,6 +213,7 @@ class SameLDA:
                 raise ValueError(f"out must be a contiguous {dtype} tensor of shape {self._shape(which)}")
             nbytes = out.numel() * out.element_size()
             on_device = out.device.type == "cuda"
+            torch.autograd.graph.increment_version(out)                 # autograd may have kept what it held
             if on_device:
                 torch.cuda.current_stream(out.device).synchronize()     # what is still being done to out ends first
             self._check(self._lib.same_lda_get(self._h, which, out.data_ptr() if nbytes else None, nbytes, 1 if on_device else 0))
@@ -441,6 +442,11 @@ def _token_ids(tokens):
     return tokens if tokens.is_contiguous() else tokens.contiguous()
 
 
+def _rewritten(out):
+    """Tells autograd, as torch's own in-place operations do, that `out` will not hold what it may have kept of it for a backward pass."""
+    _torch.autograd.graph.increment_version(out)
+
+
 def _output(out, shape, rows, width, dtype, default, device):
     """The output of a call, made here where none is given, and its same_lda_rows as `rows` rows of `width`."""
     if out is None:
@@ -450,13 +456,15 @@ def _output(out, shape, rows, width, dtype, default, device):
     _numbers("out", out)
     if out.shape != shape or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype or out.dtype}")
+    _rewritten(out)
     return out, _rows(out if out.dim() == 2 else out.view(-1, width))
 
 
 def embed(table, tokens, scale=1.0, dtype=None, out=None):
     """scale * table[tokens]: the rows of `table` (a matrix, or a MicroMatrix) for int32 or int64 `tokens` of any shape, in
     `dtype` (default: the table's, float32 for a MicroMatrix).  An id outside the table (padding) gives zeros.  `out`: a tensor of
-    shape tokens.shape + (width,) whose leading dimensions can be viewed as one."""
+    shape tokens.shape + (width,) whose leading dimensions can be viewed as one.  The result has no gradient function, also of a table that
+    requires a gradient: a step calls embed_grad for it."""
     ids = _token_ids(tokens)
     index = _gpu(ids, table, out)
     t, n, width = _rows(table), ids.numel(), table.shape[1]
@@ -498,7 +506,7 @@ def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumul
 
 
 def micro_quantize(x, out=None) -> MicroMatrix:
-    """A matrix in microscaled four-bit floating point."""
+    """A matrix in microscaled four-bit floating point (for autograd a constant)."""
     if _torch is None:
         _setup()
     _numbers("x", x)
@@ -514,12 +522,14 @@ def micro_quantize(x, out=None) -> MicroMatrix:
         out.width, out.rows = width, rows
     elif type(out) is not MicroMatrix:
         raise TypeError("out is a MicroMatrix")
+    else:
+        _rewritten((out.codes, out.scales))
     _run(index, _library.same_lda_micro_quantize, r, _rows(out))
     return out
 
 
 def micro_dequantize(q, dtype=None, out=None):
-    """The numbers that a MicroMatrix stands for, in `dtype` (default: float32)."""
+    """The numbers that a MicroMatrix stands for, in `dtype` (default: float32; for autograd a constant)."""
     _micro("q", q)
     index = _gpu(q, out)
     out, o = _output(out, q.shape, q.rows, q.width, dtype, _torch.float32, q.codes.device)
@@ -537,7 +547,7 @@ def _rounded_in_the_call(a, b) -> bool:
 
 def micro_product(a, b, scale=1.0, dtype=None, out=None):
     """scale * a @ b.T in `dtype` (default: float32) for a MicroMatrix `b`; `a` is a MicroMatrix, or a matrix that is rounded to
-    one first."""
+    one first.  The result has no gradient function, also where `a` requires a gradient."""
     _micro("b", b)
     if type(a) is not MicroMatrix and not _rounded_in_the_call(a, b):
         a = micro_quantize(a)

@@ -1,7 +1,9 @@
 """Calls at the borders of what the word-table operators take."""
+import numpy as np
 import pytest
 import torch
 
+from helpers import csc_from_dense
 from paper_1409_5402_amd import binding
 from test_gpu_word_tables import DEV, TYPES, guarded
 
@@ -64,3 +66,33 @@ def test_gradient_of_rows_that_share_memory_or_are_not_contiguous():
     x = torch.randn(4, 5, device=DEV, requires_grad=True)
     (x[t.view(6).clamp(min=0)] * (t.view(6, 1) >= 0)).sum().backward()
     assert torch.equal(binding.embed_grad(torch.ones((), device=DEV).expand(6, 5), t.view(6), 4), x.grad)
+
+
+def test_autograd_sees_constants_and_rewritten_outputs():
+    """Results have no gradient function, as the docstrings say; what a call writes into an `out` that a backward pass has kept ends that
+    pass with torch's error, not with a wrong gradient."""
+    T = torch.randn(6, 8, device=DEV, requires_grad=True)
+    t = torch.tensor([1, 5, 0], device=DEV)
+    q = binding.micro_quantize(T)
+    for y in (binding.embed(T, t), binding.embed_grad(T, torch.arange(6, device=DEV), 6), binding.micro_product(T, q), binding.micro_dequantize(q)):
+        assert y.grad_fn is None and not y.requires_grad
+    for call in (lambda out: binding.embed(T, t, out=out), lambda out: binding.embed_grad(T, torch.arange(6, device=DEV), out=out[:6]), lambda out: binding.embed_grad(T, torch.arange(6, device=DEV), out=out, accumulate=True),
+                 lambda out: binding.micro_dequantize(q[:3], out=out), lambda out: binding.micro_product(T[:3], binding.micro_quantize(torch.ones(8, 8, device=DEV)), out=out)):
+        out = torch.randn(3, 8, device=DEV)
+        x = torch.ones(3, 8, device=DEV, requires_grad=True)
+        y = (x * out).sum()                                                    # keeps out for x's gradient
+        call(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    with torch.inference_mode():
+        out = torch.empty(3, 8, device=DEV)
+    binding.embed(T, t, out=out)
+    assert torch.equal(out, T.detach()[t])
+    X = csc_from_dense(np.array([[1, 2, 0], [0, 3, 1]]))
+    model = binding.SameLDA(X.D, X.V, X.colptr, X.rowidx, X.val, 4, 0.1, 0.01, seed=1, m0=5)
+    phi = torch.ones(3, 4, device=DEV)
+    y = (torch.ones(3, 4, device=DEV, requires_grad=True) * phi).sum()
+    model.get(binding.PHI, out=phi)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    model.close()
