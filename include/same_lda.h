@@ -305,7 +305,8 @@ int same_lda_micro_quantize(const same_lda_rows* x, const same_lda_rows* micro_o
 #define SAME_LDA_ROUND_MAX 16384
 /* out[i][j] = scale * sum_k a[i][k] * b[j][k], both microscaled and of one width, in binary32, rounded once to the output's
  * type: with rows of topic weights and the rows of phi, the predictive weight of every word (same_lda_sddmm is the
- * same product at the nonzeros only, of unrounded matrices).
+ * same product at the nonzeros only, of unrounded matrices).  What four bits cost: an element is off by up to a quarter
+ * of its block's largest, and the predictive weights of Dirichlet models by 5 to 20 % on average.
  *   a            microscaled, or up to SAME_LDA_ROUND_ROWS rows and SAME_LDA_ROUND_MAX elements of any type: then the
  *                product is that of what same_lda_micro_quantize would make of them, in the one call
  *   out          [a->rows][b->rows]                                                                               */
