@@ -118,14 +118,21 @@ struct GradSpace {
 constexpr int kTileRows = 16, kSmallTileRows = 4;                    // rows of 256 tokens in a tile of the sort
 constexpr int64_t kSmallTiles = 1 << 22;                             // up to this many tokens the tiles are small
 
-// One launch without a sort: up to 8192 tokens with two workgroups per compute unit, or 16,384 with one where rows of the gradient
-// are short (16,384 tokens into 2000 x 64 f32: 27 us, sorted 42; into 30,000 x 1024 bf16: 59, 60; into 2000 x 1024 f32, where the
-// most frequent word keeps one compute unit busy: 56, 44); and a grid below 2^32 threads: 1024 for every 256 words begun, and
-// every 64 chunks of a row.
+// One launch without a sort (us, sorted after it):
+//   up to 8192 tokens     8192 into 30,000 x 1024 bf16 35, 53; into 2000 x 1024 f32 31, 36; into a million words x 16 f32 59, 58
+//   up to 16,384 tokens   where rows of the gradient are short (into 2000 x 64 f32 26, 37; into 30,000 x 1024 bf16 59, 57; into 2000 x
+//                         1024 f32, where the most frequent word keeps one compute unit busy, 63, 40); beyond 2^18 words not of 512 bytes
+//                         and less, for a compute unit takes one workgroup of 256 words at a time then, each reads the whole list,
+//                         and writing such rows does not hide it (f32, into 200,000 x 16 40, 45; 400,000 x 16 66, 55; 400,000 x
+//                         128 89, 80; 400,000 x 192 116, 129; a million x 16 143, 61)
+// and a grid below 2^32 threads: 1024 for every 256 words begun, and every 64 chunks of a row.
 constexpr int kFewerTokens = 8192;
+constexpr int64_t kScannedWords = 1 << 18;
 bool few_tokens(int64_t n, int64_t rows, const same_lda_rows* grad)
 {
-    return n <= ((int64_t)grad->width * element_bytes(grad->type) <= 2048 ? same::kFewTokens : kFewerTokens) && (rows + 256) * ((grad->width + 63) / 64) < (int64_t)1 << 30;
+    const int64_t row_bytes = (int64_t)grad->width * element_bytes(grad->type);
+    const bool more = row_bytes <= 2048 && (rows <= kScannedWords || row_bytes > 512);
+    return n <= (more ? same::kFewTokens : kFewerTokens) && (rows + 256) * ((grad->width + 63) / 64) < (int64_t)1 << 30;
 }
 
 GradSpace grad_space(const same_lda_rows* grad, int64_t rows)
