@@ -274,8 +274,10 @@ void product_rounded(same::ProductArgs& p, hipStream_t st)
 //                               (100 x 100,000 x 256: 10.6, large tiles 13.9; 2000 x 30,000 x 256: 50.0, 53.7; 16-bit sums, whose
 //                               rows of 64 are half as long, 4096 x 20,000 x 200: large tiles 45, 53)
 //   256 x 256                   from 256 such tiles on (4096 x 16,384 x 1024: 58, tiles of 128 85; 2048 x 4096 x 4096, 128 tiles: 33,
-//                               tiles of 128 27)
-//   64 x 64                     up to 160 tiles of 128 x 128 (512 x 4096 x 4096: 13.9, 16.5; 1024 x 4096 x 4096: 27, 18)
+//                               tiles of 128 27) for more than 640 rows of a (16-bit sums, 700 x 100,000 x 1024: 70, 80; 600 x 70,000 x
+//                               1024: tiles of 128 47, 56; 17 x 70,000 x 4096: 72, of 64 32)
+//   64 x 64                     up to 64 rows of a, and up to 160 tiles of 128 x 128 (512 x 4096 x 4096: 13.9, 16.5; 1024 x 4096 x 4096: 27, 18;
+//                               64 x 70,000 x 4096: 31, 45; 64 x 600,000 x 128, a single stage: 20, 35)
 constexpr int64_t kRowsAtOnce = (int64_t)1 << 28;
 
 template <class TO>
@@ -291,13 +293,13 @@ void product_to(same::ProductArgs& p, int32_t type_a, hipStream_t st)
     const int64_t tiles = ((p.rows_a + 127) / 128) * ((p.rows_b + 127) / 128);
     const int64_t large = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
     if (p.groups <= 2) {
-        if (tiles <= (sizeof(TO) == 4 ? 4096 : 2048)) product_tiles<TO, 1, 1, 2, 2, 1, 2>(p, st);
+        if (p.rows_a <= 64 || tiles <= (sizeof(TO) == 4 ? 4096 : 2048)) product_tiles<TO, 1, 1, 2, 2, 1, 2>(p, st);
         else                      product_tiles<TO, 2, 2, 2, 2, 1, 2>(p, st);
     } else if (p.groups == 3) {
         product_tiles<TO, 2, 2, 2, 2, 2, 2>(p, st);
-    } else if (large >= 256 && p.groups >= 8) {
+    } else if (p.rows_a > 640 && large >= 256 && p.groups >= 8) {
         product_tiles<TO, 4, 2, 2, 4, 2, 4>(p, st);
-    } else if (tiles <= 160) {
+    } else if (p.rows_a <= 64 || tiles <= 160) {
         product_tiles<TO, 1, 1, 2, 2, 2, 8>(p, st);
     } else {
         product_tiles<TO, 2, 2, 2, 2, 2, 4>(p, st);
