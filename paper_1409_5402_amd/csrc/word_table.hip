@@ -247,12 +247,14 @@ void product_few(same::ProductArgs& p, hipStream_t st)
     hipLaunchKernelGGL((same::micro_product_few_kernel<TO, MF, RF, KW, TI>), dim3((unsigned)at_most((p.tiles_b + 4 / KW - 1) / (4 / KW), kMaxGroups)), dim3(256), 0, st, p);
 }
 
-// Of long rows the four waves of a workgroup take a part each.  16 rows of the table per wave, or 64 where that still leaves 512
-// workgroups: 13 rows by 50,021 x 4096 take 60 us with 16 rows and whole rows per wave, 30 us with 64 and a quarter.
+// Of rows of ten groups and more the four waves of a workgroup take a part each (1 x 60,000 x 1280: whole rows per wave 9.7 us, a quarter
+// 10.7; 16 rows 13.5, 11.9; 16 x 20,000 7.7, 6.4; with eight and nine groups a part is too short: 1 x 100,000 x 1024 11.8, 17;
+// 16 x 60,000 x 1152 8.7, 9.9).  16 rows of the table per wave, or 64 where that still leaves 512 workgroups (16 x 50,000 x 4096: 27,
+// with 16 rows 32; 13 x 28,000, fewer: with 16 rows 17.5, 15.5; a single row would do better with 16, 1 x 50,000 x 4096 21, 25).
 template <class TO, int MF, class TI = void>
 void product_few_by_shape(same::ProductArgs& p, hipStream_t st)
 {
-    if (p.groups < 8)                product_few<TO, MF, 1, 1, TI>(p, st);
+    if (p.groups < 10)               product_few<TO, MF, 1, 1, TI>(p, st);
     else if (p.rows_b < 64 * 512)    product_few<TO, MF, 1, 4, TI>(p, st);
     else                             product_few<TO, MF, 4, 4, TI>(p, st);
 }
