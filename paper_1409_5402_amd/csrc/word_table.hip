@@ -249,14 +249,15 @@ void product_few(same::ProductArgs& p, hipStream_t st)
 
 // Of rows of ten groups and more the four waves of a workgroup take a part each (1 x 60,000 x 1280: whole rows per wave 9.7 us, a quarter
 // 10.7; 16 rows 13.5, 11.9; 16 x 20,000 7.7, 6.4; with eight and nine groups a part is too short: 1 x 100,000 x 1024 11.8, 17;
-// 16 x 60,000 x 1152 8.7, 9.9).  16 rows of the table per wave, or 64 where that still leaves 512 workgroups (16 x 50,000 x 4096: 27,
-// with 16 rows 32; 13 x 28,000, fewer: with 16 rows 17.5, 15.5; a single row would do better with 16, 1 x 50,000 x 4096 21, 25).
+// 16 x 60,000 x 1152 8.7, 9.9; up to 4096 rows it is the shorter wait all the same, 17 x 3000 x 1024 4.1, 4.8).  16 rows of the
+// table per wave, or 64 where that still leaves 512 workgroups (16 x 50,000 x 4096: 27, with 16 rows 32; 16 x 20,000 x 4096: with 16
+// rows 14.5, 15.3; a single row would do better with 16 everywhere, 1 x 50,000 x 4096 21, 25).
 template <class TO, int MF, class TI = void>
 void product_few_by_shape(same::ProductArgs& p, hipStream_t st)
 {
-    if (p.groups < 10)               product_few<TO, MF, 1, 1, TI>(p, st);
-    else if (p.rows_b < 64 * 512)    product_few<TO, MF, 1, 4, TI>(p, st);
-    else                             product_few<TO, MF, 4, 4, TI>(p, st);
+    if (p.groups < (p.rows_b > 4096 ? 10 : 8)) product_few<TO, MF, 1, 1, TI>(p, st);
+    else if (p.rows_b < 64 * 512)              product_few<TO, MF, 1, 4, TI>(p, st);
+    else                                       product_few<TO, MF, 4, 4, TI>(p, st);
 }
 
 // Rows of numbers, rounded in the call: one launch in place of two (32 x 2000 x 256: 6.5 us, 14.2).  Beyond 16 rows they are short, and not
@@ -270,8 +271,11 @@ void product_rounded(same::ProductArgs& p, hipStream_t st)
 }
 
 // Which kernel (us at rows of a x rows of b x width, the first number the chosen one's):
-//   up to 16 rows of a          straight from memory; above, tiles, but up to 32 rows of a by a table below 32 MB of longer rows
-//                               (32 x 5000 x 4096: 9.2, tiles 12.6; 32 x 50,021 x 4096: tiles 34, 44; 32 x 100,000 x 256: tiles 7.0, 10.1)
+//   up to 16 rows of a          straight from memory; above, tiles, but up to 32 rows of a by a table of up to 8192 longer rows (17 x 8000 x
+//                               4096: 8.2, tiles 10.6; 32 x 8000 x 4096: 9.8, 10.5; 32 x 12,000 x 4096: tiles 11.0, 13.5; 32 x 20,000 x
+//                               1024: tiles 6.3, 10.1; 32 x 100,000 x 256: tiles 7.0, 10.1), 16,384 of four groups (17 x 12,000 x 512:
+//                               4.0, 4.8; 32 x 20,000 x 512: tiles 5.1, 5.8), or any number of three, for which there are only tiles
+//                               of 128 rows (17 x 180,000 x 384: 13, 27)
 //   rows of one or two groups   a single stage, four workgroups per compute unit; tiles of 64 x 64 where those of 128 x 128 are few
 //                               (100 x 100,000 x 256: 10.6, large tiles 13.9; 2000 x 30,000 x 256: 50.0, 53.7; 16-bit sums, whose
 //                               rows of 64 are half as long, 4096 x 20,000 x 200: large tiles 45, 53)
@@ -291,7 +295,7 @@ void product_to(same::ProductArgs& p, int32_t type_a, hipStream_t st)
         case SAME_LDA_HALF:   return product_rounded<TO, _Float16>(p, st);
     }
     if (p.rows_a <= 16) return product_few_by_shape<TO, 1>(p, st);
-    if (p.rows_a <= 32 && p.groups > 2 && p.rows_b * p.groups * 64 < (int64_t)1 << 25) return product_few_by_shape<TO, 2>(p, st);
+    if (p.rows_a <= 32 && (p.groups == 3 || (p.groups > 3 && p.rows_b <= (p.groups == 4 ? 16384 : 8192)))) return product_few_by_shape<TO, 2>(p, st);
     const int64_t tiles = ((p.rows_a + 127) / 128) * ((p.rows_b + 127) / 128);
     const int64_t large = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
     if (p.groups <= 2) {

@@ -21,7 +21,8 @@ def numbers_on_device(codes, scales, width):
 # tiles of 256 x 256 (8, 9, 33 and 64 groups of 128 elements), of 128 x 128 in two stages and in one, of 64 x 64; remainders of rows,
 # of columns and of groups
 FORMS = [(4096, 4096, 1024), (4100, 4152, 1100), (3900, 4300, 4224), (4096, 4096, 8192), (4352, 3841, 1152), (1500, 3000, 640), (1536, 2048, 900), (2050, 33_000, 200), (2100, 33_000, 100), (520, 712, 1500),
-         (512, 512, 384), (17, 70_000, 1100), (64, 40_000, 2048), (40, 300_000, 100), (64, 140_000, 256), (300, 30_000, 1024)]
+         (512, 512, 384), (17, 70_000, 1100), (64, 40_000, 2048), (40, 300_000, 100), (64, 140_000, 256), (300, 30_000, 1024), (20, 8192, 1152), (31, 8300, 1300), (25, 16_385, 512),
+         (16, 4100, 1024), (9, 4096, 1152), (3, 40_000, 1280), (32, 180_000, 384)]
 
 
 @pytest.mark.parametrize("M, N, K", FORMS)
