@@ -404,14 +404,8 @@ def _rows(x) -> bytes:
     return _pack_rows(x.data_ptr(), 0, rows, stride if rows > 1 else width, width, kind)
 
 
-def _micro(name, x):
-    if type(x) is not MicroMatrix:
-        raise TypeError(f"{name} is a MicroMatrix (micro_quantize makes one), not a {type(x).__name__}")
-
-
-def _numbers(name, x):
-    if type(x) is MicroMatrix:
-        raise TypeError(f"{name} is a tensor, not a MicroMatrix")
+def _not_micro(name, x):
+    return TypeError(f"{name} is a MicroMatrix (micro_quantize makes one), not a {type(x).__name__}")
 
 
 def _gpu(*operands) -> int:
@@ -453,7 +447,8 @@ def _output(out, shape, rows, width, dtype, default, device):
         kind = _type_of(dtype or default)
         out = _torch.empty(shape, dtype=dtype or default, device=device)
         return out, _pack_rows(out.data_ptr(), 0, rows, width, width, kind)
-    _numbers("out", out)
+    if type(out) is MicroMatrix:
+        raise TypeError("out is a tensor, not a MicroMatrix")
     if out.shape != shape or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype or out.dtype}")
     _rewritten(out)
@@ -482,19 +477,22 @@ def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumul
     ``accumulate=True``; `rows` is then out's.  Equal numbers of
     one type and shape give equal bits, whatever their strides."""
     ids = _token_ids(tokens)
-    _numbers("grad", grad)
-    if grad.dim() != tokens.dim() + 1 or grad.shape[:-1] != tokens.shape:
+    if type(grad) is MicroMatrix:
+        raise TypeError("grad is a tensor, not a MicroMatrix")
+    shape = grad.shape
+    if not shape or shape[:-1] != tokens.shape:
         raise ValueError(f"grad has shape {tuple(grad.shape)}, tokens {tuple(tokens.shape)}")
     if out is None and (accumulate or rows is None):
         raise ValueError("accumulate needs out" if accumulate else "rows or out must say how many rows the table has")
     index = _gpu(ids, grad, out)
-    width = grad.shape[-1]
+    width = shape[-1]
     rows = out.shape[0] if rows is None else int(rows)
-    flat = grad if grad.dim() == 2 else grad.reshape(ids.numel(), width)
-    stride, inner = flat.stride()
-    if inner != 1 and width > 1 or stride < width and len(flat) > 1:
+    flat = grad if len(shape) == 2 else grad.reshape(ids.numel(), width)
+    try:
+        g = _rows(flat)
+    except ValueError:                                 # rows that share memory or are not contiguous
         flat = flat.contiguous()
-    g = _rows(flat)
+        g = _rows(flat)
     out, o = _output(out, (rows, width), rows, width, dtype, grad.dtype, ids.device)
     n = c_size_t()
     if _library.same_lda_embed_grad_workspace(g, o, byref(n)):
@@ -509,7 +507,8 @@ def micro_quantize(x, out=None) -> MicroMatrix:
     """A matrix in microscaled four-bit floating point (for autograd a constant)."""
     if _torch is None:
         _setup()
-    _numbers("x", x)
+    if type(x) is MicroMatrix:
+        raise TypeError("x is a tensor, not a MicroMatrix")
     index = _gpu(x, out)
     r = _rows(x)
     if out is None:
@@ -530,7 +529,8 @@ def micro_quantize(x, out=None) -> MicroMatrix:
 
 def micro_dequantize(q, dtype=None, out=None):
     """The numbers that a MicroMatrix stands for, in `dtype` (default: float32; for autograd a constant)."""
-    _micro("q", q)
+    if type(q) is not MicroMatrix:
+        raise _not_micro("q", q)
     index = _gpu(q, out)
     out, o = _output(out, q.shape, q.rows, q.width, dtype, _torch.float32, q.codes.device)
     _run(index, _library.same_lda_embed, _rows(q), None, 8, 1.0, o)
@@ -548,7 +548,8 @@ def _rounded_in_the_call(a, b) -> bool:
 def micro_product(a, b, scale=1.0, dtype=None, out=None):
     """scale * a @ b.T in `dtype` (default: float32) for a MicroMatrix `b`; `a` is a MicroMatrix, or a matrix that is rounded to
     one first.  The result has no gradient function, also where `a` requires a gradient."""
-    _micro("b", b)
+    if type(b) is not MicroMatrix:
+        raise _not_micro("b", b)
     if type(a) is not MicroMatrix and not _rounded_in_the_call(a, b):
         a = micro_quantize(a)
     index = _gpu(a, b, out)
