@@ -539,8 +539,8 @@ def micro_dequantize(q, dtype=None, out=None):
 
 def _rounded_in_the_call(a, b) -> bool:
     """Whether micro_product leaves the rounding of a matrix to the library's call: one launch in place of two, where it takes
-    the rows, and above 16 of them by tables that are small (us in the call and before it: 32 x 2000 x 256 6.5, 14.2;
-    32 x 100,000 x 256 11.5, 14.5; 64 x 100,000 x 256 21.5, 14.0; 17 x 50,000 x 900 22.5, 15.0)."""
+    the rows, and above 16 of them by tables that are small (us in the call and before it: 32 x 2000 x 256 7.2, 15.1;
+    64 x 60,000 x 256 12.6, 14.8; 64 x 70,000 x 256 13.2, 14.8; 64 x 100,000 x 256 18.1, 14.8; 17 x 50,000 x 900 13.1, 14.7)."""
     rows = a.shape[0]
     return rows <= 64 and a.numel() <= 16384 and (rows <= 16 or -(-rows // 16) * b.rows * b.width <= 1 << 26)
 

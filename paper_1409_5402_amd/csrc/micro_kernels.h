@@ -102,8 +102,8 @@ struct alignas(4) ScaleWords {
 
 // 13 x 50,021 x 4096 takes 26 us, 4.2 TB/s; 1 x 100,000 x 256 5.4 us, a launch and the way to memory.
 // With TI a type of numbers the rows of a are such numbers, few enough (kRoundMost of them) for every workgroup to round them for itself:
-// one launch in place of two (16 x 40,000 x 1024, the most: 13.4 us, rounded before 14.2; with the 53,248 of 13 x 50,021 x 4096 it
-// would be 44, 34).
+// one launch in place of two (the most, as calls: 16 x 40,000 x 1024 9.0 us, rounded before 14.6; 2 x 20,000 x 8192 19.2, 19.8; with the
+// 53,248 of 13 x 50,021 x 4096 it would be 44, 34).
 constexpr int kRoundMost = 16384, kRoundRows = 64;
 
 template <class TO, int MF, int RF, int KW, class TI>
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(256) void micro_product_few_kernel(ProductArgs p)
 // consecutive rows that are read at one block then lie in different banks.  A row's scales are fetched for kScaleGroups
 // groups at once: what a compute unit's loads cost is the lines that they touch, and with 8 bytes per row and stage the
 // scales touched as many as the codes (65 x 50,021 x 4096: 36.6 us, with kScaleGroups = 4 33.5 us).
-// 8192 x 8192 x 8192 to bf16 takes 275 us, 4.0 PFLOP/s (tiles of 256 x 256 by eight waves): its loads alone take 231 us and its
+// 8192 x 8192 x 8192 to bf16 takes 275 to 282 us, 4.0 PFLOP/s (tiles of 256 x 256 by eight waves): its loads alone take 231 us and its
 // products alone 211 (6.4 PFLOP/s is what the instructions reach by themselves on random numbers, 9.2 on zeros).  2048 x 100,000
 // x 256 to binary32 takes 166 us, 5.0 TB/s; a kernel that only stores the same tiles takes 127.
 constexpr int kStageGroups = 2;

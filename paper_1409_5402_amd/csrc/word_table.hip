@@ -181,7 +181,8 @@ int grad_launch(same::GradArgs& a, hipStream_t st)
     const unsigned across = (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2);
     const int64_t most = kMaxGroups / across;                        // across <= SAME_LDA_WIDTH_MAX / 64
     if (!a.start) {                                                  // few tokens
-        // two workgroups per compute unit, for each reads the whole list; more where a workgroup's words would be more than fit
+        // 512 workgroups, for each reads the whole list; more where a workgroup's words would be more than fit.  A compute unit holds two
+        // of them up to 8192 tokens and V < 8; otherwise (some 100 registers, or 114 KB of LDS) one, and the grid runs in two rounds
         if (a.lanes_log2 < 2) a.lanes_log2 = 2;                      // 256 groups at most, and words
         const int64_t groups = (int64_t)1024 >> a.lanes_log2;
         a.unit_log2 = 0;
@@ -260,7 +261,7 @@ void product_few_by_shape(same::ProductArgs& p, hipStream_t st)
     else                                       product_few<TO, MF, 4, 4, TI>(p, st);
 }
 
-// Rows of numbers, rounded in the call: one launch in place of two (32 x 2000 x 256: 6.5 us, 14.2).  Beyond 16 rows they are short, and not
+// Rows of numbers, rounded in the call: one launch in place of two (32 x 2000 x 256: 7.2 us, 15.1, as calls).  Beyond 16 rows they are short, and not
 // shared out.
 template <class TO, class TI>
 void product_rounded(same::ProductArgs& p, hipStream_t st)
@@ -277,8 +278,9 @@ void product_rounded(same::ProductArgs& p, hipStream_t st)
 //                               4.0, 4.8; 32 x 20,000 x 512: tiles 5.1, 5.8), or any number of three, for which there are only tiles
 //                               of 128 rows (17 x 180,000 x 384: 13, 27)
 //   rows of one or two groups   a single stage, four workgroups per compute unit; tiles of 64 x 64 where those of 128 x 128 are few
-//                               (100 x 100,000 x 256: 10.6, large tiles 13.9; 2000 x 30,000 x 256: 50.0, 53.7; 16-bit sums, whose
-//                               rows of 64 are half as long, 4096 x 20,000 x 200: large tiles 45, 53)
+//                               (100 x 131,072 x 256: 13, large tiles 16; 128 x 393,216 x 256, at 3072 of them, 39, 39; 128 x 524,288 x 256,
+//                               at 4096, 79, 73; 16-bit sums, whose rows of 64 are half as long: at 1536 2000 x 12,288 x 256 16, 17, 2048 x
+//                               12,288 x 256 14, 13; at 2048 100 x 262,144 x 256 19, 23, 2048 x 16,384 x 256 18, 15; at 4096 33, 30)
 //   256 x 256                   from 256 such tiles on (4096 x 16,384 x 1024: 58, tiles of 128 85; 2048 x 4096 x 4096, 128 tiles: 33,
 //                               tiles of 128 27) for more than 640 rows of a (16-bit sums, 700 x 100,000 x 1024: 70, 80; 600 x 70,000 x
 //                               1024: tiles of 128 47, 56; 17 x 70,000 x 4096: 72, of 64 32)
