@@ -42,3 +42,13 @@ def test_every_form_and_output_type_is_exact(M, N, K):
             assert torch.equal(got, rounded), (dtype, stride, torch.nonzero(got != rounded)[:5])
             check()
             del got
+
+
+@pytest.mark.parametrize("M, N, K", [(16, 4096, 1024), (16, 5000, 1024), (9, 40_000, 1152), (1, 33_000, 1025), (12, 4200, 1280), (3, 33_000, 5000), (16, 70_000, 500)])
+def test_rounding_in_the_call_gives_the_same_bits(M, N, K):
+    """Whole rows per wave, quarters, 16 and 64 rows of the table: the form does not depend on where `a` is rounded."""
+    rng = np.random.default_rng(M + N + K)
+    b = micro(*random_micro(rng, N, K, 120, 130), K)
+    for dtype in TYPES.values():
+        x = torch.from_numpy(rng.normal(size=(M, K))).to(dtype).to(DEV)
+        assert torch.equal(binding.micro_product(x, b, 0.5, dtype=dtype), binding.micro_product(binding.micro_quantize(x), b, 0.5, dtype=dtype))
