@@ -277,13 +277,15 @@ void product_rounded(same::ProductArgs& p, hipStream_t st)
 //                               1024: tiles 6.3, 10.1; 32 x 100,000 x 256: tiles 7.0, 10.1), 16,384 of four groups (17 x 12,000 x 512:
 //                               4.0, 4.8; 32 x 20,000 x 512: tiles 5.1, 5.8), or any number of three, for which there are only tiles
 //                               of 128 rows (17 x 180,000 x 384: 13, 27)
-//   rows of one or two groups   a single stage, four workgroups per compute unit; tiles of 64 x 64 where those of 128 x 128 are few
-//                               (100 x 131,072 x 256: 13, large tiles 16; 128 x 393,216 x 256, at 3072 of them, 39, 39; 128 x 524,288 x 256,
-//                               at 4096, 79, 73; 16-bit sums, whose rows of 64 are half as long: at 1536 2000 x 12,288 x 256 16, 17, 2048 x
-//                               12,288 x 256 14, 13; at 2048 100 x 262,144 x 256 19, 23, 2048 x 16,384 x 256 18, 15; at 4096 33, 30)
+//   rows of one or two groups   a single stage, four workgroups per compute unit; tiles of 64 x 64 where those of 128 x 128 are few (here
+//                               of 64, then of 128: 100 x 131,072 x 256 13, 16; 2048 x 28,672 x 256, at 3584, 39, 40; 128 x 524,288 x 256,
+//                               at 4096, 79, 73; to 16 bits, where rows of 64 are half as long: at 1536 2000 x 12,288 x 256 16, 17 and 2048 x
+//                               12,288 x 256 14, 13; at 2048 100 x 262,144 x 256 19, 23 and 2048 x 16,384 x 256 18, 15; at 4096 2000 x
+//                               32,768 x 256 33, 30: full tiles of 128 would pay from half as many on)
 //   256 x 256                   from 256 such tiles on (4096 x 16,384 x 1024: 58, tiles of 128 85; 2048 x 4096 x 4096, 128 tiles: 33,
 //                               tiles of 128 27) for more than 640 rows of a (16-bit sums, 700 x 100,000 x 1024: 70, 80; 600 x 70,000 x
-//                               1024: tiles of 128 47, 56; 17 x 70,000 x 4096: 72, of 64 32)
+//                               1024: tiles of 128 47, 56; 17 x 70,000 x 4096: 72, of 64 32) of eight groups and more (4096 x 8192 x 1024
+//                               30, 34; of seven the same, of four 22, 24)
 //   64 x 64                     up to 64 rows of a, and up to 160 tiles of 128 x 128 (512 x 4096 x 4096: 13.9, 16.5; 1024 x 4096 x 4096: 27, 18;
 //                               64 x 70,000 x 4096: 31, 45; 64 x 600,000 x 128, a single stage: 20, 35)
 constexpr int64_t kRowsAtOnce = (int64_t)1 << 28;
@@ -302,7 +304,7 @@ void product_to(same::ProductArgs& p, int32_t type_a, hipStream_t st)
     const int64_t large = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
     if (p.groups <= 2) {
         if (p.rows_a <= 64 || tiles <= (sizeof(TO) == 4 ? 4096 : 2048)) product_tiles<TO, 1, 1, 2, 2, 1, 2>(p, st);
-        else                      product_tiles<TO, 2, 2, 2, 2, 1, 2>(p, st);
+        else product_tiles<TO, 2, 2, 2, 2, 1, 2>(p, st);
     } else if (p.groups == 3) {
         product_tiles<TO, 2, 2, 2, 2, 2, 2>(p, st);
     } else if (p.rows_a > 640 && large >= 256 && p.groups >= 8) {
