@@ -252,6 +252,9 @@ int same_lda_synchronize(same_lda_t* h);
 #define SAME_LDA_BFLOAT  1   /* bfloat16                                                                           */
 #define SAME_LDA_HALF    2   /* binary16                                                                           */
 #define SAME_LDA_MICRO   3   /* microscaled four-bit floating point, see below                                     */
+#define SAME_LDA_GROUPS_OF_32   32   /* four-bit integers with a step and a base per group of so many elements,     */
+#define SAME_LDA_GROUPS_OF_64   64   /* see below                                                                  */
+#define SAME_LDA_GROUPS_OF_128 128
 #define SAME_LDA_WIDTH_MAX (1 << 20)   /* elements of a row (of the output of a product: 2^31 - 1)                 */
 
 /* A matrix of `rows` rows of `width` elements; the elements of a row are contiguous, rows are `stride` elements
@@ -260,10 +263,15 @@ int same_lda_synchronize(same_lda_t* h);
  * the code 0 .. 7 in the low three bits of a half byte (the even element in the low half), the sign above them.
  * A block has a scale byte s: its elements count 2^(s-127) times (s = 255: all are NaN).  Rows are filled up with
  * zero blocks to a multiple of 128 elements and follow each other without gaps: 64 bytes of codes (data, aligned to
- * 16) and 4 of scales (aligned to 4) per 128 elements; stride is not used.                                        */
+ * 16) and 4 of scales (aligned to 4) per 128 elements; stride is not used.
+ * SAME_LDA_GROUPS_OF_32, _64, _128: an element is q s + b, q in 0 .. 15, the step s and the base b of its group of 32, 64 or
+ * 128 consecutive elements of a row in bfloat16.  Rows are filled up with codes 0 to a multiple of 128 elements and follow each
+ * other without gaps: 64 bytes of codes (data, aligned to 16) per 128 elements, 4 bytes per group (scales, aligned to 4; s, then
+ * b); stride is not used.  Of 128 elements the 32-bit word 4 h + j (little endian) has the eight from 32 j + 8 h on: element 2 t of them is the
+ * half byte t counted from the lowest, element 2 t + 1 the half byte 4 + t.                                       */
 typedef struct {
     void*    data;
-    uint8_t* scales;      /* SAME_LDA_MICRO only */
+    uint8_t* scales;      /* SAME_LDA_MICRO and SAME_LDA_GROUPS_OF_* only */
     int64_t  rows;        /* below 2^31          */
     int64_t  stride;
     int32_t  width;
@@ -274,7 +282,7 @@ typedef struct {
  *   tokens       [out->rows] int32 or int64 (token_bytes = 4 or 8); an id outside [0, table->rows) stands for no word
  *                (padding): its row is zeros.  Null: row i of the table, for all of them (out->rows == table->rows): the
  *                way to read a microscaled matrix back.
- *   table        any type; out: any but SAME_LDA_MICRO                                                            */
+ *   table        any type; out: SAME_LDA_FLOAT, _BFLOAT or _HALF                                                  */
 int same_lda_embed(const same_lda_rows* table, const void* tokens, int32_t token_bytes, float scale,
                    const same_lda_rows* out, void* hip_stream);
 
@@ -292,6 +300,35 @@ int same_lda_embed_grad_workspace(const same_lda_rows* grad, const same_lda_rows
 int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale,
                         int32_t accumulate, const same_lda_rows* table_grad, void* workspace, size_t workspace_bytes,
                         void* hip_stream);
+
+/* Dropout.  An element of a matrix is kept, times 1 / (1 - p), or zero, whatever it held.  Which ones are kept follows from the seed, the step
+ * and the place (row, column) in the call's matrix alone: nothing is stored, and a backward pass repeats the forward pass's
+ * choice from the same same_lda_drop.  An element has 32 random bits and is kept where they are below (1 - p) 2^32 rounded to an integer;
+ * they come from Philox4x32-10 under the seed, in a part of its counters that the sweeps do not use: of columns 8 c .. 8 c + 7 of row i the
+ * blocks at (c, i, step mod 2^32, 2^30 + floor(step / 2^32)) and at the same with 2^27 added to the last word; column 8 c + e has
+ * half e mod 2 (0: the lower 16 bits) of word floor(e / 2) of either block, that of the first block as its upper bits. */
+typedef struct {
+    double         p;        /* probability that an element becomes zero, in [0, 1]                             */
+    uint64_t       seed;
+    uint64_t       step;     /* below 2^56; another one for every call whose choice is to be another             */
+    const int64_t* step_at;  /* device, or null: the number there is added to step (modulo 2^56) when the kernel runs, so that
+                                a captured call draws anew in every replay that finds another number there      */
+} same_lda_drop;
+
+/* out[i][j] = x[i][j] / (1 - p) where kept, else 0: the factor and the product in binary32, rounded once to the output's type.  The
+ * gradient is the same call on the gradient of out.  out may be x itself (the same data, stride and type).        */
+int same_lda_dropout(const same_lda_rows* x, const same_lda_drop* drop, const same_lda_rows* out, void* hip_stream);
+
+/* same_lda_embed followed by same_lda_dropout, rounded once: scale / (1 - p) in binary32 takes the place of the scale.  Rows of ids that
+ * stand for no word are zeros.                                                                                    */
+int same_lda_embed_dropout(const same_lda_rows* table, const void* tokens, int32_t token_bytes, float scale, const same_lda_drop* drop,
+                           const same_lda_rows* out, void* hip_stream);
+
+/* The gradient of same_lda_embed_dropout with respect to the table: same_lda_embed_grad (its workspace, its order of
+ * additions) of the elements of grad that the lookup kept, with scale / (1 - p).  What dropped elements hold does not count. */
+int same_lda_embed_dropout_grad(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale, const same_lda_drop* drop,
+                                int32_t accumulate, const same_lda_rows* table_grad, void* workspace, size_t workspace_bytes,
+                                void* hip_stream);
 
 /* Bytes of the codes and of the scales of a microscaled matrix. */
 int same_lda_micro_size(int64_t rows, int32_t width, size_t* code_bytes, size_t* scale_bytes);
@@ -312,6 +349,24 @@ int same_lda_micro_quantize(const same_lda_rows* x, const same_lda_rows* micro_o
  *   out          [a->rows][b->rows]                                                                               */
 int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out,
                            void* hip_stream);
+
+/* Bytes of the codes and of the scales of a matrix in groups of `group` = 32, 64 or 128 elements. */
+int same_lda_group_size(int64_t rows, int32_t width, int32_t group, size_t* code_bytes, size_t* scale_bytes);
+
+/* x in grouped integers.  Of a group's least and largest number b is the least rounded down to bfloat16 (not below its least finite
+ * number, which leaves s below 0 where all are below that), s = (largest - b) / 15 rounded to binary32 and on to bfloat16 (the next lower one where b + 15 s would be beyond binary32), and
+ * an element is the nearest of b, b + s, .. b + 15 s, ties to the even q (s = 0: q = 0).  A group that holds an infinity or a NaN
+ * becomes NaN as a whole (s, b NaN, codes 0).  Where numbers are of one sign this form has 16 sizes, the microscaled one
+ * eight.                                                                                                          */
+int same_lda_group_quantize(const same_lda_rows* x, const same_lda_rows* group_out, void* hip_stream);
+
+/* out[i][j] = scale * sum_k a[i][k] * (q_jk s_jk + b_jk): rows of numbers as they are, by a matrix in grouped integers of the same
+ * width.  Sums are binary32; of binary32 rows all 24 bits count.  The result is rounded once to the output's type.  Groups
+ * are summed as s sum a q + b sum a, so a row of a that is not finite, or one for which the sum of (15 |s| + |b|) |a| is beyond
+ * binary32, gives numbers that may be infinite or NaN.
+ *   a            any number of rows, SAME_LDA_FLOAT, _BFLOAT or _HALF
+ *   out          [a->rows][b->rows]                                                                               */
+int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* hip_stream);
 
 /* Text of the last failure of this handle (when h is NULL: of the last failed call without a handle, same_lda_init
  * among them, on the calling thread).  The pointer stays valid until the next failing call.                        */

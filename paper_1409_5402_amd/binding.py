@@ -7,6 +7,7 @@ There is no fallback: if the library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 import struct
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
@@ -25,7 +26,8 @@ _DTYPES = {THETA: np.float32, PHI: np.float32, NDK: np.uint32, NWK: np.uint32, N
 EXPORTS = ["same_lda_init", "same_lda_sweep", "same_lda_sweep_poisson", "same_lda_sweep_sampled", "same_lda_loglik", "same_lda_free",
            "same_lda_set_batch", "same_lda_stage_batch", "same_lda_commit_batch", "same_lda_debug_draw_poisson", "same_lda_sddmm",
            "same_lda_vb_exp_elog_beta", "same_lda_vb_estep",
-           "same_lda_embed", "same_lda_embed_grad_workspace", "same_lda_embed_grad", "same_lda_micro_size", "same_lda_micro_quantize", "same_lda_micro_product",
+           "same_lda_embed", "same_lda_embed_grad_workspace", "same_lda_embed_grad", "same_lda_dropout", "same_lda_embed_dropout", "same_lda_embed_dropout_grad",
+           "same_lda_group_size", "same_lda_group_quantize", "same_lda_group_product", "same_lda_micro_size", "same_lda_micro_quantize", "same_lda_micro_product",
            "same_lda_get", "same_lda_set", "same_lda_get_pass", "same_lda_set_pass", "same_lda_task_count",
            "same_lda_debug_draw", "same_lda_debug_draw_noalloc", "same_lda_debug_chunk_limit", "same_lda_set_timing", "same_lda_get_timing", "same_lda_selftest",
            "same_lda_synchronize",
@@ -86,6 +88,12 @@ def load(path: str | None = None) -> ctypes.CDLL:
         L.same_lda_embed.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_void_p, c_void_p]
         L.same_lda_embed_grad_workspace.argtypes = [c_void_p, c_void_p, POINTER(c_size_t)]
         L.same_lda_embed_grad.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.same_lda_dropout.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
+        L.same_lda_embed_dropout.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_void_p, c_void_p, c_void_p]
+        L.same_lda_embed_dropout_grad.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.same_lda_group_size.argtypes = [c_int64, c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
+        L.same_lda_group_quantize.argtypes = [c_void_p, c_void_p, c_void_p]
+        L.same_lda_group_product.argtypes = [c_void_p, c_void_p, c_float, c_void_p, c_void_p]
         L.same_lda_micro_size.argtypes = [c_int64, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
         L.same_lda_micro_quantize.argtypes = [c_void_p, c_void_p, c_void_p]
         L.same_lda_micro_product.argtypes = [c_void_p, c_void_p, c_float, c_void_p, c_void_p]
@@ -334,6 +342,7 @@ class SameLDA:
 
 MICRO = 3
 _pack_rows = struct.Struct("PPqqii").pack          # same_lda_rows, passed by the address of its bytes
+_pack_drop = struct.Struct("dQQP").pack            # same_lda_drop
 _torch = None
 _types = {}                                        # element types by torch's
 _library = None
@@ -383,6 +392,86 @@ class MicroMatrix:
         return MicroMatrix(self.codes[rows], self.scales[rows], self.width)
 
 
+class GroupMatrix:
+    """A matrix in grouped four-bit integers, q s + b: ``codes`` [rows, 64 * g] in uint8 and ``scales`` [rows, 128 * g / group, 2] in
+    bfloat16 (s and b of every group of `group` = 32, 64 or 128 elements), contiguous tensors on one GPU with g = ceil(width / 128), in
+    the layout that include/same_lda.h describes."""
+
+    __slots__ = ("codes", "scales", "width", "group", "rows")
+
+    def __init__(self, codes, scales, width, group):
+        if _torch is None:
+            _setup()
+        width, group = int(width), int(group)
+        if group not in (32, 64, 128):
+            raise ValueError(f"groups hold 32, 64 or 128 elements, not {group}")
+        blocks = -(-width // 128)
+        rows, n = codes.shape[0], blocks * (128 // group)
+        if (width < 1 or codes.dtype != _torch.uint8 or scales.dtype != _torch.bfloat16 or codes.shape != (rows, 64 * blocks) or scales.shape != (rows, n, 2)
+                or not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device):
+            raise ValueError(f"rows of {width} elements in groups of {group} need contiguous uint8 codes [rows, {64 * blocks}] and bfloat16 scales [rows, {n}, 2] on one device")
+        self.codes, self.scales, self.width, self.group, self.rows = codes, scales, width, group, rows
+
+    @property
+    def shape(self):
+        return (self.rows, self.width)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def get_device(self):
+        return self.codes.get_device()
+
+    def __getitem__(self, rows):
+        """A range of rows (a slice without a step), not copied."""
+        if not isinstance(rows, slice) or rows.step not in (None, 1):
+            raise TypeError("a grouped matrix is sliced by ranges of rows")
+        return GroupMatrix(self.codes[rows], self.scales[rows], self.width, self.group)
+
+
+_CODED = (MicroMatrix, GroupMatrix)
+
+
+class Dropout:
+    """Which elements of a matrix are kept: each with probability 1 - p, by its place, the seed and the step alone, so a backward pass that is
+    given the same Dropout repeats the forward pass's choice.  `step`: an integer in [0, 2^56), another one for every call whose
+    choice is to be another; or a tensor of one int64 element on the GPU, read when the kernel runs (a captured graph that counts it up
+    draws anew in every replay)."""
+
+    __slots__ = ("p", "seed", "step", "_packed")
+
+    def __init__(self, p, seed, step=0):
+        p = float(p)
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"the probability {p} is not in [0, 1]")
+        at = 0
+        if _is_torch(step):
+            import torch
+            if step.dtype != torch.int64 or step.numel() != 1:
+                raise TypeError(f"a step in a tensor is one int64 element, not {step.numel()} of {step.dtype}")
+            at, count = step.data_ptr(), 0
+        else:
+            count = operator.index(step)
+            if not 0 <= count < 1 << 56:
+                raise ValueError(f"the step {count} is not in [0, 2^56)")
+        seed = operator.index(seed)
+        if not 0 <= seed < 1 << 64:
+            raise ValueError(f"the seed {seed} is not in [0, 2^64)")
+        self.p, self.seed, self.step = p, seed, step
+        self._packed = _pack_drop(p, seed, count, at)
+
+    def _on(self):
+        """The operand among a call's that must be on its GPU: the step's tensor, if it is one."""
+        return None if type(self.step) is int or not _is_torch(self.step) else self.step
+
+
+def _drop(drop) -> bytes:
+    if type(drop) is not Dropout:
+        raise TypeError(f"drop is a Dropout, not a {type(drop).__name__}")
+    return drop._packed
+
+
 def _type_of(dtype) -> int:
     kind = _types.get(dtype)
     if kind is None:
@@ -394,6 +483,8 @@ def _rows(x) -> bytes:
     """A matrix as a same_lda_rows."""
     if type(x) is MicroMatrix:
         return _pack_rows(x.codes.data_ptr(), x.scales.data_ptr(), x.rows, x.width, x.width, MICRO)
+    if type(x) is GroupMatrix:
+        return _pack_rows(x.codes.data_ptr(), x.scales.data_ptr(), x.rows, x.width, x.width, x.group)
     kind = _type_of(x.dtype)
     if x.dim() != 2:
         raise ValueError(f"a matrix has two dimensions, not {x.dim()}")
@@ -447,59 +538,96 @@ def _output(out, shape, rows, width, dtype, default, device):
         kind = _type_of(dtype or default)
         out = _torch.empty(shape, dtype=dtype or default, device=device)
         return out, _pack_rows(out.data_ptr(), 0, rows, width, width, kind)
-    if type(out) is MicroMatrix:
-        raise TypeError("out is a tensor, not a MicroMatrix")
+    if type(out) in _CODED:
+        raise TypeError(f"out is a tensor, not a {type(out).__name__}")
     if out.shape != shape or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out has shape {tuple(out.shape)} and type {out.dtype}, not {tuple(shape)} and {dtype or out.dtype}")
     _rewritten(out)
     return out, _rows(out if out.dim() == 2 else out.view(-1, width))
 
 
-def embed(table, tokens, scale=1.0, dtype=None, out=None):
-    """scale * table[tokens]: the rows of `table` (a matrix, or a MicroMatrix) for int32 or int64 `tokens` of any shape, in
-    `dtype` (default: the table's, float32 for a MicroMatrix).  An id outside the table (padding) gives zeros.  `out`: a tensor of
+def embed(table, tokens, scale=1.0, dtype=None, out=None, drop=None):
+    """scale * table[tokens]: the rows of `table` (a matrix, a MicroMatrix or a GroupMatrix) for int32 or int64 `tokens` of any shape, in
+    `dtype` (default: the table's, float32 for one in four bits).  An id outside the table (padding) gives zeros.  `drop`: a Dropout of the
+    result, whose row i is that of the i-th token.  `out`: a tensor of
     shape tokens.shape + (width,) whose leading dimensions can be viewed as one.  The result has no gradient function, also of a table that
     requires a gradient: a step calls embed_grad for it."""
     ids = _token_ids(tokens)
     index = _gpu(ids, table, out)
     t, n, width = _rows(table), ids.numel(), table.shape[1]
-    out, o = _output(out, (*tokens.shape, width), n, width, dtype, _torch.float32 if type(table) is MicroMatrix else table.dtype, ids.device)
-    _run(index, _library.same_lda_embed, t, ids.data_ptr() if n else _EMPTY, ids.element_size(), scale, o)
+    if drop is not None:
+        d = _drop(drop)
+        _gpu(ids, drop._on())
+    out, o = _output(out, (*tokens.shape, width), n, width, dtype, _torch.float32 if type(table) in _CODED else table.dtype, ids.device)
+    if drop is None:
+        _run(index, _library.same_lda_embed, t, ids.data_ptr() if n else _EMPTY, ids.element_size(), scale, o)
+    else:
+        _run(index, _library.same_lda_embed_dropout, t, ids.data_ptr() if n else _EMPTY, ids.element_size(), scale, d, o)
     return out
+
+
+def dropout(x, drop, dtype=None, out=None):
+    """x / (1 - p) where `drop` (a Dropout) keeps an element, else 0, for a tensor of one dimension or more as the matrix of its last dimension's
+    rows; in `dtype` (default: x's).  The gradient is the same call on the result's gradient.  `out` may be x itself; its leading
+    dimensions can be viewed as one.  For autograd the result is a constant."""
+    if _torch is None:
+        _setup()
+    if type(x) in _CODED:
+        raise TypeError(f"x is a tensor, not a {type(x).__name__}")
+    d = _drop(drop)
+    if not x.dim() or not x.shape[-1]:
+        raise ValueError(f"x has shape {tuple(x.shape)}, which holds no rows")
+    index = _gpu(x, out, drop._on())
+    width = x.shape[-1]
+    flat, r = _flat_rows(x, x.numel() // width, width)
+    out, o = _output(out, x.shape, x.numel() // width, width, dtype, x.dtype, x.device)
+    _run(index, _library.same_lda_dropout, r, d, o)
+    return out
+
+
+def _flat_rows(x, rows, width):
+    """x as a matrix and its same_lda_rows, copied where its rows are not contiguous or share memory (an expanded tensor)."""
+    flat = x if x.dim() == 2 else x.reshape(rows, width)
+    try:
+        return flat, _rows(flat)
+    except ValueError:
+        flat = flat.contiguous()
+        return flat, _rows(flat)
 
 
 _EMPTY = 16        # stands for the address of a list of no tokens: not null, never read
 
 
-def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumulate=False):
+def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumulate=False, drop=None):
     """The gradient of ``embed(table, tokens, scale)`` with respect to a table of `rows` rows, from that of its result: `grad`
     of shape tokens.shape + (width,), copied first where its rows are not contiguous or share memory (an expanded tensor).  `dtype` (default: grad's) is the result's type.  `out`: where it is written, or added to with
-    ``accumulate=True``; `rows` is then out's.  Equal numbers of
+    ``accumulate=True``; `rows` is then out's.  `drop`: the Dropout of the lookup.  Equal numbers of
     one type and shape give equal bits, whatever their strides."""
     ids = _token_ids(tokens)
-    if type(grad) is MicroMatrix:
-        raise TypeError("grad is a tensor, not a MicroMatrix")
+    if type(grad) in _CODED:
+        raise TypeError(f"grad is a tensor, not a {type(grad).__name__}")
     shape = grad.shape
     if not shape or shape[:-1] != tokens.shape:
         raise ValueError(f"grad has shape {tuple(grad.shape)}, tokens {tuple(tokens.shape)}")
     if out is None and (accumulate or rows is None):
         raise ValueError("accumulate needs out" if accumulate else "rows or out must say how many rows the table has")
     index = _gpu(ids, grad, out)
+    if drop is not None:
+        d = _drop(drop)
+        _gpu(ids, drop._on())
     width = shape[-1]
     rows = out.shape[0] if rows is None else int(rows)
-    flat = grad if len(shape) == 2 else grad.reshape(ids.numel(), width)
-    try:
-        g = _rows(flat)
-    except ValueError:                                 # rows that share memory or are not contiguous
-        flat = flat.contiguous()
-        g = _rows(flat)
+    flat, g = _flat_rows(grad, ids.numel(), width)
     out, o = _output(out, (rows, width), rows, width, dtype, grad.dtype, ids.device)
     n = c_size_t()
     if _library.same_lda_embed_grad_workspace(g, o, byref(n)):
         raise SameLdaError(-1, _library.same_lda_last_error(None).decode())
     space = _torch.empty(n.value, dtype=_torch.uint8, device=ids.device) if n.value else None
-    _run(index, _library.same_lda_embed_grad, g, ids.data_ptr() if ids.numel() else _EMPTY, ids.element_size(), scale, 1 if accumulate else 0, o,
-         space.data_ptr() if n.value else None, n.value)
+    t, at = ids.data_ptr() if ids.numel() else _EMPTY, space.data_ptr() if n.value else None
+    if drop is None:
+        _run(index, _library.same_lda_embed_grad, g, t, ids.element_size(), scale, 1 if accumulate else 0, o, at, n.value)
+    else:
+        _run(index, _library.same_lda_embed_dropout_grad, g, t, ids.element_size(), scale, d, 1 if accumulate else 0, o, at, n.value)
     return out
 
 
@@ -507,8 +635,8 @@ def micro_quantize(x, out=None) -> MicroMatrix:
     """A matrix in microscaled four-bit floating point (for autograd a constant)."""
     if _torch is None:
         _setup()
-    if type(x) is MicroMatrix:
-        raise TypeError("x is a tensor, not a MicroMatrix")
+    if type(x) in _CODED:
+        raise TypeError(f"x is a tensor, not a {type(x).__name__}")
     index = _gpu(x, out)
     r = _rows(x)
     if out is None:
@@ -550,10 +678,63 @@ def micro_product(a, b, scale=1.0, dtype=None, out=None):
     one first.  The result has no gradient function, also where `a` requires a gradient."""
     if type(b) is not MicroMatrix:
         raise _not_micro("b", b)
+    if type(a) is GroupMatrix:
+        raise TypeError("a is a tensor or a MicroMatrix, not a GroupMatrix")
     if type(a) is not MicroMatrix and not _rounded_in_the_call(a, b):
         a = micro_quantize(a)
     index = _gpu(a, b, out)
     x, rows = _rows(a), a.shape[0]
     out, o = _output(out, (rows, b.rows), rows, b.rows, dtype, _torch.float32, b.codes.device)
     _run(index, _library.same_lda_micro_product, x, _rows(b), scale, o)
+    return out
+
+
+def group_quantize(x, group=64, out=None) -> GroupMatrix:
+    """A matrix in grouped four-bit integers, with a step and a base for every `group` = 32, 64 or 128 elements of a row (for
+    autograd a constant).  `out`: a GroupMatrix that is written; the group is then out's."""
+    if _torch is None:
+        _setup()
+    if type(x) in _CODED:
+        raise TypeError(f"x is a tensor, not a {type(x).__name__}")
+    index = _gpu(x, out)
+    r = _rows(x)
+    if out is None:
+        if group not in (32, 64, 128):
+            raise ValueError(f"groups hold 32, 64 or 128 elements, not {group}")
+        rows, width = x.shape
+        blocks = -(-width // 128)
+        device = x.device
+        out = GroupMatrix.__new__(GroupMatrix)
+        out.codes = _torch.empty((rows, 64 * blocks), dtype=_torch.uint8, device=device)
+        out.scales = _torch.empty((rows, blocks * (128 // group), 2), dtype=_torch.bfloat16, device=device)
+        out.width, out.group, out.rows = width, int(group), rows
+    elif type(out) is not GroupMatrix:
+        raise TypeError("out is a GroupMatrix")
+    else:
+        _rewritten((out.codes, out.scales))
+    _run(index, _library.same_lda_group_quantize, r, _rows(out))
+    return out
+
+
+def group_dequantize(q, dtype=None, out=None):
+    """The numbers that a GroupMatrix stands for, in `dtype` (default: float32; for autograd a constant)."""
+    if type(q) is not GroupMatrix:
+        raise TypeError(f"q is a GroupMatrix (group_quantize makes one), not a {type(q).__name__}")
+    index = _gpu(q, out)
+    out, o = _output(out, q.shape, q.rows, q.width, dtype, _torch.float32, q.codes.device)
+    _run(index, _library.same_lda_embed, _rows(q), None, 8, 1.0, o)
+    return out
+
+
+def group_product(a, b, scale=1.0, dtype=None, out=None):
+    """scale * a @ b.T in `dtype` (default: a's) for a GroupMatrix `b` and a matrix `a`, which is not rounded.  The result has no
+    gradient function, also where `a` requires a gradient."""
+    if type(b) is not GroupMatrix:
+        raise TypeError(f"b is a GroupMatrix (group_quantize makes one), not a {type(b).__name__}")
+    if type(a) in _CODED:
+        raise TypeError(f"a is a tensor, not a {type(a).__name__}")
+    index = _gpu(a, b, out)
+    x, rows = _rows(a), a.shape[0]
+    out, o = _output(out, (rows, b.rows), rows, b.rows, dtype, a.dtype, b.codes.device)
+    _run(index, _library.same_lda_group_product, x, _rows(b), scale, o)
     return out

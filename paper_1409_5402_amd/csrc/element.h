@@ -34,4 +34,58 @@ __device__ __forceinline__ void store_chunk(T* __restrict__ p, const float (&x)[
     *reinterpret_cast<Chunk<T, V>*>(p) = c;
 }
 
+// Eight elements at the alignment of one: whole vectors all the same, global memory is read and written at any address.
+typedef uint32_t v4u32 __attribute__((ext_vector_type(4)));
+typedef v4u32 v4u32_anywhere __attribute__((aligned(2)));
+
+template <class T>
+struct Eight {
+    T v[8];
+    static constexpr int kVectors = sizeof(T) / 2;
+    __device__ __forceinline__ void load(const T* p)
+    {
+        v4u32 x[kVectors];
+#pragma unroll
+        for (int q = 0; q < kVectors; ++q) x[q] = reinterpret_cast<const v4u32_anywhere*>(p)[q];
+        __builtin_memcpy(v, x, sizeof v);
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+        v4u32 x[kVectors];
+        __builtin_memcpy(x, v, sizeof v);
+#pragma unroll
+        for (int q = 0; q < kVectors; ++q) reinterpret_cast<v4u32_anywhere*>(p)[q] = x[q];
+    }
+};
+
+// The first `count` of eight elements, zeros behind them.
+template <class T>
+__device__ __forceinline__ void load_eight(float (&x)[8], const T* p, int count)
+{
+    Eight<T> c;
+    if (count >= 8) {
+        c.load(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c.v[j] = j < count ? p[j] : (T)0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = to_float(c.v[j]);
+}
+
+template <class T>
+__device__ __forceinline__ void store_eight(T* p, const float (&x)[8], int count)
+{
+    Eight<T> c;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c.v[j] = (T)x[j];
+    if (count >= 8) {
+        c.store(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < count) p[j] = c.v[j];
+    }
+}
+
 }  // namespace same
