@@ -12,25 +12,44 @@ using same::fail_without_handle;
 
 namespace {
 
-template <class TI, class TO>
-void product_launch(const same::GroupProductArgs& p, int group_log2, hipStream_t st)
+template <class TI, int P, bool kStack, int kGroupLog2, int KB>
+void product_few(same::GroupProductArgs& p, int blocks, hipStream_t st)
 {
-    const int64_t tiles = ((p.rows_a + 15) / 16) * ((p.rows_b + 15) / 16);
-    const dim3 grid((unsigned)at_most((tiles + 3) / 4, kMaxGroups));
-    switch (group_log2) {
-        case 5:  hipLaunchKernelGGL((same::group_product_kernel<TI, TO, 5>), grid, dim3(256), 0, st, p); break;
-        case 6:  hipLaunchKernelGGL((same::group_product_kernel<TI, TO, 6>), grid, dim3(256), 0, st, p); break;
-        default: hipLaunchKernelGGL((same::group_product_kernel<TI, TO, 7>), grid, dim3(256), 0, st, p); break;
+    int kw = 1;
+    while (kw * KB < blocks) kw *= 2;                                    // at most 8
+    p.waves_per_row = kw;
+    const int waves = kw < 4 ? 4 : kw, streams = waves / kw;
+    const int64_t turns = ((p.rows_b + 15) / 16 + streams - 1) / streams;
+    hipLaunchKernelGGL((same::group_product_few_kernel<TI, P, kStack, kGroupLog2, KB>), dim3((unsigned)at_most(turns, kComputeUnits * 8 / waves)), dim3(64 * waves), 0, st, p);
+}
+
+template <class TI, int P, bool kStack, int kGroupLog2>
+void product_few_by_width(same::GroupProductArgs& p, int blocks, hipStream_t st)
+{
+    if (blocks == 1) product_few<TI, P, kStack, kGroupLog2, 1>(p, blocks, st);
+    else if (blocks <= 2 || blocks == 16) product_few<TI, P, kStack, kGroupLog2, 2>(p, blocks, st);
+    else product_few<TI, P, kStack, kGroupLog2, 4>(p, blocks, st);
+}
+
+template <class TI, int kGroupLog2>
+void product_launch(same::GroupProductArgs& p, hipStream_t st)
+{
+    const int blocks = (p.width + 127) / 128;
+    if (p.rows_a <= 16 && blocks <= 32) {
+        if constexpr (sizeof(TI) == 4) return p.rows_a <= 4 ? product_few_by_width<TI, 1, true, kGroupLog2>(p, blocks, st) : product_few_by_width<TI, 3, false, kGroupLog2>(p, blocks, st);
+        else return product_few_by_width<TI, 1, false, kGroupLog2>(p, blocks, st);
     }
+    const int64_t tiles = ((p.rows_a + 15) / 16) * ((p.rows_b + 15) / 16);
+    hipLaunchKernelGGL((same::group_product_kernel<TI, kGroupLog2>), dim3((unsigned)at_most((tiles + 3) / 4, kMaxGroups)), dim3(256), 0, st, p);
 }
 
 template <class TI>
-void product_to(const same::GroupProductArgs& p, int group_log2, int32_t type, hipStream_t st)
+void product_to(same::GroupProductArgs& p, int group_log2, hipStream_t st)
 {
-    switch (type) {
-        case SAME_LDA_FLOAT:  return product_launch<TI, float>(p, group_log2, st);
-        case SAME_LDA_BFLOAT: return product_launch<TI, __bf16>(p, group_log2, st);
-        default:              return product_launch<TI, _Float16>(p, group_log2, st);
+    switch (group_log2) {
+        case 5:  return product_launch<TI, 5>(p, st);
+        case 6:  return product_launch<TI, 6>(p, st);
+        default: return product_launch<TI, 7>(p, st);
     }
 }
 
@@ -84,12 +103,24 @@ int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float
     if (a->rows == 0) return SAME_LDA_OK;
     const int group_log2 = __builtin_ctz((unsigned)b->type);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const same::GroupProductArgs p = {a->data, a->rows, a->stride, a->width, static_cast<const uint8_t*>(b->data), b->scales, b->rows,
-                                      same::micro_code_pitch(b->width), same::group_scale_pitch(b->width, group_log2), scale, out->data, out->stride};
+    same::GroupProductArgs p = {};
+    p.a = a->data;
+    p.rows_a = a->rows;
+    p.stride_a = a->stride;
+    p.width = a->width;
+    p.type_out = out->type;
+    p.codes = static_cast<const uint8_t*>(b->data);
+    p.scales = b->scales;
+    p.rows_b = b->rows;
+    p.pitch = same::micro_code_pitch(b->width);
+    p.scale_pitch = same::group_scale_pitch(b->width, group_log2);
+    p.scale = scale;
+    p.out = out->data;
+    p.out_stride = out->stride;
     switch (a->type) {
-        case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, out->type, st); break;
-        case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, out->type, st); break;
-        default:              product_to<_Float16>(p, group_log2, out->type, st); break;
+        case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, st); break;
+        case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, st); break;
+        default:              product_to<_Float16>(p, group_log2, st); break;
     }
     return launched("group_product");
 }

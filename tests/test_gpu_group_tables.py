@@ -218,6 +218,15 @@ def test_product_of_long_rows_and_many(M, N, K, dtype, group):
     product_case(np.random.default_rng(M + N), M, N, K, dtype, group, "f32")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M", [1, 8, 9, 16])
+@pytest.mark.parametrize("K", [257, 384, 511, 513, 1030, 1537, 2049, 3000, 3968, 4095, 4097])
+def test_product_of_few_rows_of_every_length(K, M, dtype):
+    """Every way in which few rows are shared out between waves, the last of them with a part or none of a row."""
+    for N, group in ((1, 32), (40, 64), (131, 128)):
+        product_case(np.random.default_rng(K + M), M, N, K, dtype, group, "f32")
+
+
 @pytest.mark.parametrize("M, N, K", [(1, 100, 700), (4, 90, 384), (7, 130, 1100), (16, 257, 4224), (33, 200, 900), (200, 300, 640)])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("group", GROUPS)
