@@ -58,17 +58,45 @@ struct Eight {
     }
 };
 
-// The first `count` of eight elements, zeros behind them.
+// Elements at .. at + 7 of a row, zeros behind its end, in two steps: a whole load, of the row's last eight elements where the chunk crosses
+// its end, and moving those into place.  Many loads are then on their way together.
 template <class T>
-__device__ __forceinline__ void load_eight(float (&x)[8], const T* p, int count)
+__device__ __forceinline__ Eight<T> eight_at(const T* row, int at, int width)
 {
     Eight<T> c;
-    if (count >= 8) {
-        c.load(p);
+    if (width >= 8) {
+        c.load(row + (at < width - 8 ? at : width - 8));
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) c.v[j] = j < count ? p[j] : (T)0.0f;
+        for (int j = 0; j < 8; ++j) {
+            const T x = row[at + j < width ? at + j : width - 1];
+            c.v[j] = at + j < width ? x : (T)0.0f;
+        }
     }
+    return c;
+}
+
+template <class T>
+__device__ __forceinline__ void cut_eight(Eight<T>& c, int at, int width)
+{
+    const int over = at + 8 - width;
+    if (over <= 0 || width < 8) return;
+#pragma unroll
+    for (int by = 1; by <= 4; by *= 2)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const T other = j + by < 8 ? c.v[j + by < 8 ? j + by : 7] : (T)0.0f;
+            c.v[j] = over & by ? other : c.v[j];
+        }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c.v[j] = over >= 8 ? (T)0.0f : c.v[j];
+}
+
+template <class T>
+__device__ __forceinline__ void load_eight(float (&x)[8], const T* row, int at, int width)
+{
+    Eight<T> c = eight_at(row, at, width);
+    cut_eight(c, at, width);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = to_float(c.v[j]);
 }

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void group_quantize_kernel(GroupQuantizeArgs a
         const int64_t row = all >> 32 ? at / pieces : (int64_t)((uint32_t)at / (uint32_t)pieces);             // a division of 64 bits takes as long as the rest
         const int c = (int)(at - row * pieces), count = a.width - 8 * c;
         float x[8];
-        load_eight<TI>(x, static_cast<const TI*>(a.x) + row * a.stride + (int64_t)c * 8, count);
+        load_eight<TI>(x, static_cast<const TI*>(a.x) + row * a.stride, 8 * c, a.width);
         float least = __builtin_inff(), most = -__builtin_inff();
         int bad = 0;
 #pragma unroll
@@ -157,73 +157,194 @@ __device__ __forceinline__ void three_pieces(v4u32 (&out)[3], const float (&from
         }
 }
 
-// Eight numbers of a row as operands of the matrix instruction, in the codes' order: themselves, or three operands that add up to them.
+// Eight numbers as operands of the matrix instruction, in the codes' order: themselves, or three operands that add up to them.
 template <class TI, int P>
-__device__ __forceinline__ void pieces_of(v4u32 (&out)[P], const TI* p, int count)
+__device__ __forceinline__ void pieces_of(v4u32 (&out)[P], const Eight<TI>& c)
 {
     if constexpr (P == 1) {
-        Eight<TI> c;
-        if (count >= 8) {
-            c.load(p);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) c.v[j] = j < count ? p[j] : (TI)0.0f;
-        }
         v4u32 x;
         __builtin_memcpy(&x, c.v, 16);
         out[0] = {__builtin_amdgcn_perm(x[2], x[0], 0x05040100u), __builtin_amdgcn_perm(x[2], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[1], 0x05040100u),
                   __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
     } else {
-        float x[8];
-        load_eight<float>(x, p, count);
-        three_pieces(out, x);
+        three_pieces(out, c.v);
     }
 }
 
-// A wave takes 16 rows of a by 16 of b.
-template <class TI, int kGroupLog2>
-__global__ __launch_bounds__(256) void group_product_kernel(GroupProductArgs p)
+// An operand of ones: with it as the first, an instruction adds up the rows of the second, lane l the row l % 16.
+template <bool kHalf>
+__device__ __forceinline__ v4u32 all_ones()
+{
+    constexpr uint32_t one = kHalf ? 0x3C003C00u : 0x3F803F80u;
+    return {one, one, one, one};
+}
+
+// Any number of rows.  A workgroup of four waves takes 16 MT rows of a by 16 NT (4 / WK) of b: its rows of a go by way of LDS, cut into
+// pieces and with their sums S, a block of 128 elements ahead; the codes come straight from memory into the registers of the one wave that
+// has these rows of b, a block ahead too.  WK waves share out the blocks of a row of b and their sums are added in order at the end: more
+// waves where rows of b are few.
+template <class TI, int kGroupLog2, int MT, int NT, int WK>
+__global__ __launch_bounds__(256, 2) void group_product_kernel(GroupProductArgs p)
 {
     constexpr bool kHalf = kHalfMatrix<TI>;
-    constexpr int P = sizeof(TI) == 4 ? 3 : 1, kSteps = 1 << (kGroupLog2 - 5), kPer = 128 >> kGroupLog2;   // instructions per group, groups of 128 elements
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, r = lane & 15, h = lane >> 4;
-    const int64_t tiles_b = (p.rows_b + 15) / 16, tiles_a = (p.rows_a + 15) / 16, blocks = (p.width + 127) / 128;
-    const v4u32 ones = kHalf ? v4u32{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u} : v4u32{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-    for (int64_t tile = (int64_t)blockIdx.x * 4 + wv; tile < tiles_a * tiles_b; tile += (int64_t)gridDim.x * 4) {
-        const int64_t i0 = tile / tiles_b * 16, j0 = tile % tiles_b * 16;
-        const int64_t i = i0 + r < p.rows_a ? i0 + r : p.rows_a - 1, j = j0 + r < p.rows_b ? j0 + r : p.rows_b - 1;   // rows behind the last are computed from it and not written
-        const TI* const x = static_cast<const TI*>(p.a) + i * p.stride_a;
-        const uint8_t* const codes = p.codes + j * p.pitch + 16 * h;
-        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(p.scales + j * p.scale_pitch);
-        v4f32 acc = {};
-        for (int64_t k = 0; k < blocks; ++k) {
-            const v4u32 w = *reinterpret_cast<const v4u32*>(codes + k * 64);
+    constexpr int P = sizeof(TI) == 4 ? 3 : 1, kPer = 128 >> kGroupLog2, kSteps = 4 / kPer;   // groups of a block, instructions per group
+    constexpr int WN = 4 / WK, kUnits = MT * WK, kOwn = (kUnits + 3) / 4;             // 16 rows of a by a block each
+    __shared__ union {
+        struct {
+            v4u32 x[2][WK][MT][4][P][64];                                             // as the lanes of the matrix instruction take them
+            float sum[2][WK][kPer][16 * MT];
+        } in;
+        float out[WK > 1 ? WK - 1 : 1][WK > 1 ? MT * NT * 4 : 1][WK > 1 ? 64 * WN : 1];
+    } lds;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
+    const int wn = wv % WN, wk = wv / WN;
+    // the tiles of the same rows of b on one of the eight dies, one after the other: they find the codes in its cache
+    const int64_t tiles_a = (p.rows_a + 16 * MT - 1) / (16 * MT), turn = blockIdx.x / 8, tile_b = turn / tiles_a * 8 + blockIdx.x % 8;
+    const int64_t i0 = (turn % tiles_a) * (16 * MT), j0 = tile_b * (16 * NT * WN) + wn * (16 * NT);
+    if (tile_b * (16 * NT * WN) >= p.rows_b) return;                                  // the whole workgroup
+    const int blocks = (p.width + 127) / 128, trips = (blocks + WK - 1) / WK;
+
+    const uint8_t* codes[NT];
+    const uint8_t* scales[NT];
 #pragma unroll
-            for (int g = 0; g < kPer; ++g) {
-                v4f32 d = {}, s = {};
+    for (int n = 0; n < NT; ++n) {
+        const int64_t j = j0 + 16 * n + r < p.rows_b ? j0 + 16 * n + r : p.rows_b - 1;   // rows behind the last are computed from it and not written
+        codes[n] = p.codes + j * p.pitch + 16 * h;
+        scales[n] = p.scales + j * p.scale_pitch;
+    }
+    struct Codes {
+        v4u32 w[NT];
+        uint32_t sb[NT][kPer];
+    };
+    const auto load_codes = [&](Codes& c, int trip) {                                 // blocks behind the row's end: those of its last, times zeros
+        const int k = trip * WK + wk < blocks ? trip * WK + wk : blocks - 1;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            c.w[n] = *reinterpret_cast<const v4u32*>(codes[n] + (int64_t)k * 64);
+            struct alignas(4) Words { uint32_t v[kPer]; };
+            const Words s = *reinterpret_cast<const Words*>(scales[n] + (int64_t)k * (4 * kPer));
+#pragma unroll
+            for (int g = 0; g < kPer; ++g) c.sb[n][g] = s.v[g];
+        }
+    };
+    Eight<TI> raw[kOwn][4];
+    const TI* rows[kOwn];
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) {
+        const int64_t i = i0 + 16 * ((wv + 4 * o) % MT) + r;
+        rows[o] = static_cast<const TI*>(p.a) + (i < p.rows_a ? i : p.rows_a - 1) * p.stride_a;
+    }
+    const auto load_rows = [&](int trip) {
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o)
+            if (wv + 4 * o < kUnits)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) raw[o][t] = eight_at(rows[o], (trip * WK + (wv + 4 * o) / MT) * 128 + 32 * t + 8 * h, p.width);
+    };
+    const auto put_rows = [&](int trip) {
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+            const int u = wv + 4 * o;
+            if (u >= kUnits) continue;
+            v4f32 total[kPer] = {};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                cut_eight(raw[o][t], (trip * WK + u / MT) * 128 + 32 * t + 8 * h, p.width);
+                v4u32 c[P];
+                pieces_of<TI, P>(c, raw[o][t]);
+#pragma unroll
+                for (int q = 0; q < P; ++q) {
+                    lds.in.x[trip & 1][u / MT][u % MT][t][q][lane] = c[q];
+                    total[t / kSteps] = mfma_16<kHalf>(all_ones<kHalf>(), c[q], total[t / kSteps]);
+                }
+            }
+            if (h == 0)
+#pragma unroll
+                for (int g = 0; g < kPer; ++g) lds.in.sum[trip & 1][u / MT][g][16 * (u % MT) + r] = total[g][0];
+        }
+    };
+    v4f32 acc[MT][NT] = {};
+    const auto multiply = [&](const Codes& c, int trip) {
+        const auto& x = lds.in.x[trip & 1][wk];
+#pragma unroll
+        for (int g = 0; g < kPer; ++g) {
+            v4u32 part[kSteps][MT][P];
+            v4f32 s[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                s[m] = *reinterpret_cast<const v4f32*>(&lds.in.sum[trip & 1][wk][g][16 * m + 4 * h]);
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+                    for (int q = 0; q < P; ++q) part[t][m][q] = x[m][g * kSteps + t][q][lane];
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                v4f32 d[MT] = {};
 #pragma unroll
                 for (int t = 0; t < kSteps; ++t) {
-                    const int at = (int)k * 128 + 32 * (g * kSteps + t) + 8 * h;
-                    v4u32 xs[P];
-                    pieces_of<TI, P>(xs, x + at, p.width - at);
-                    const v4u32 b = codes_up<kHalf>(w[g * kSteps + t]);
+                    const v4u32 b = codes_up<kHalf>(c.w[n][g * kSteps + t]);
 #pragma unroll
-                    for (int q = 0; q < P; ++q) {
-                        d = mfma_16<kHalf>(xs[q], b, d);
-                        s = mfma_16<kHalf>(xs[q], ones, s);
-                    }
+                    for (int q = P - 1; q >= 0; --q)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) d[m] = mfma_16<kHalf>(part[t][m][q], b, d[m]);
                 }
-                const uint32_t sb = scales[k * kPer + g];
-                const float step = from_bfloat_bits(sb & 0xFFFFu), base = __uint_as_float(sb & 0xFFFF0000u);
+                const float step = from_bfloat_bits(c.sb[n][g] & 0xFFFFu), base = __uint_as_float(c.sb[n][g] & 0xFFFF0000u);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) acc[q] = __builtin_fmaf(step, d[q], __builtin_fmaf(base, s[q], acc[q]));
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[m][n][q] = __builtin_fmaf(step, d[m][q], __builtin_fmaf(base, s[m][q], acc[m][n][q]));
             }
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (i0 + 4 * h + q < p.rows_a && j0 + r < p.rows_b)
-                store_number(p, i0 + 4 * h + q, j0 + r, p.scale * acc[q]);
+    };
+    Codes even, odd;
+    load_rows(0);
+    load_codes(even, 0);
+    put_rows(0);
+    __syncthreads();
+    for (int trip = 0;;) {
+        if (trip + 1 < trips) load_rows(trip + 1);
+        load_codes(odd, trip + 1);
+        multiply(even, trip);
+        if (++trip >= trips) break;
+        put_rows(trip);                                                               // where the trip before last read, which a barrier ended
+        __syncthreads();
+        if (trip + 1 < trips) load_rows(trip + 1);
+        load_codes(even, trip + 1);
+        multiply(odd, trip);
+        if (++trip >= trips) break;
+        put_rows(trip);
+        __syncthreads();
     }
+    if constexpr (WK > 1) {
+        __syncthreads();
+        if (wk > 0)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) lds.out[wk - 1][(m * NT + n) * 4 + q][wn * 64 + lane] = acc[m][n][q];
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int w = 0; w + 1 < WK; ++w)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[m][n][q] += lds.out[w][(m * NT + n) * 4 + q][wn * 64 + lane];
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t i = i0 + 16 * m + 4 * h + q;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                if (i < p.rows_a && j0 + 16 * n + r < p.rows_b) store_number(p, i, j0 + 16 * n + r, p.scale * acc[m][n][q]);
+        }
 }
 
 // Few rows of a, up to 16.  A wave keeps its part of them, KB blocks of 128 elements, in registers and goes through the rows of b, 16 at
@@ -247,56 +368,6 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
     const int kw = p.waves_per_row, streams = (int)(blockDim.x >> 6) / kw, stream = wv / kw, mine = wv - stream * kw;
     const int blocks = (p.width + 127) / 128, first = mine * KB;
 
-    // the wave's part of a: lane l has the elements 32 t + 8 h .. + 7 of row l % 16 of every block
-    v4u32 x[KB][4][kKept], sums[kSets][3];
-    {
-        const int m = kStack ? r & 3 : r;
-        const TI* const row = static_cast<const TI*>(p.a) + (m < p.rows_a ? m : p.rows_a - 1) * p.stride_a;
-        float total[kSets * 8];
-#pragma unroll
-        for (int g = 0; g < kSets * 8; ++g) total[g] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < KB; ++k)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int at = (first + k) * 128 + 32 * t + 8 * h;
-                float y[8];
-                load_eight<TI>(y, row + at, p.width - at);
-                if constexpr (kStack) {
-                    v4u32 c[3];
-                    three_pieces(c, y);
-                    const v4u32 zero = {};
-                    x[k][t][0] = r < 4 ? c[0] : r < 8 ? c[1] : r < 12 ? c[2] : zero;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] = __uint_as_float(j < 4 ? x[k][t][0][j & 3] << 16 : x[k][t][0][j & 3] & 0xFFFF0000u);
-                } else if constexpr (P == 3) {
-                    v4u32 c[3];
-                    three_pieces(c, y);
-#pragma unroll
-                    for (int q = 0; q < kKept; ++q) x[k][t][q] = c[q];
-                    if constexpr (kAside) aside[wv][k * 4 + t][lane] = c[2];
-                } else {
-                    pieces_of<TI, 1>(x[k][t], row + at, p.width - at);
-                }
-                total[k * kPer + t / kSteps] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
-            }
-#pragma unroll
-        for (int g = 0; g < KB * kPer; ++g) {
-            total[g] += __shfl_xor(total[g], 16);
-            total[g] += __shfl_xor(total[g], 32);
-        }
-#pragma unroll
-        for (int e = 0; e < kSets; ++e) {
-            const float* const of = total + 8 * e;
-            const float y[8] = {of[0], of[2], of[4], of[6], of[1], of[3], of[5], of[7]};          // three_pieces pairs j with j + 4
-            three_pieces(sums[e], y);
-#pragma unroll
-            for (int q = 0; q < 3; ++q)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sums[e][q][j] = h == 0 ? sums[e][q][j] : 0u;
-        }
-    }
-
     const int64_t tiles = (p.rows_b + 15) / 16, turns = (tiles + streams - 1) / streams;
     struct Codes {
         v4u32 w[KB];
@@ -318,6 +389,56 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
             for (int g = 0; g < kPer; ++g) c.sb[k * kPer + g] = s.v[g];
         }
     };
+    // kRing turns are on their way or at work; what is asked for behind the last one is its last row again
+    constexpr int kRing = kAside ? 2 : 4;
+    Codes ring[kRing];
+    // the wave's part of a: lane l has the elements 32 t + 8 h .. + 7 of row l % 16 of every block
+    v4u32 x[KB][4][kKept], sums[kSets][3];
+    {
+        const int m = kStack ? r & 3 : r;
+        const TI* const row = static_cast<const TI*>(p.a) + (m < p.rows_a ? m : p.rows_a - 1) * p.stride_a;
+        Eight<TI> raw[KB][4];
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) raw[k][t] = eight_at(row, (first + k) * 128 + 32 * t + 8 * h, p.width);
+        load(ring[0], blockIdx.x);                                             // behind the rows of a, which are waited for first
+        v4f32 total[kSets * 8];
+#pragma unroll
+        for (int g = 0; g < kSets * 8; ++g) total[g] = v4f32{};
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                cut_eight(raw[k][t], (first + k) * 128 + 32 * t + 8 * h, p.width);
+                v4u32 c[sizeof(TI) == 4 ? 3 : 1];
+                pieces_of(c, raw[k][t]);
+                if constexpr (kStack) {
+                    const v4u32 zero = {};
+                    c[0] = r < 4 ? c[0] : r < 8 ? c[1] : r < 12 ? c[2] : zero;
+                }
+                v4f32& sum = total[k * kPer + t / kSteps];
+#pragma unroll
+                for (int q = 0; q < P; ++q) sum = mfma_16<kHalf>(all_ones<kHalf>(), c[q], sum);
+#pragma unroll
+                for (int q = 0; q < kKept; ++q) x[k][t][q] = c[q];
+                if constexpr (kAside) aside[wv][k * 4 + t][lane] = c[2];
+            }
+#pragma unroll
+        for (int e = 0; e < kSets; ++e) {
+            const v4f32* const of = total + 8 * e;
+            const float y[8] = {of[0][0], of[2][0], of[4][0], of[6][0], of[1][0], of[3][0], of[5][0], of[7][0]};          // three_pieces pairs j with j + 4
+            three_pieces(sums[e], y);
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sums[e][q][j] = h == 0 ? sums[e][q][j] : 0u;
+        }
+    }
+
+#pragma unroll
+    for (int u = 1; u + 1 < kRing; ++u) load(ring[u], blockIdx.x + (int64_t)u * gridDim.x);
+
     int buffer = 0;
     const auto multiply = [&](const Codes& c, int64_t turn) {
         v4f32 acc = {};
@@ -370,28 +491,26 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
             const int i = e >> 4, j = e & 15;
             if (i < p.rows_a && tile * 16 + j < p.rows_b) {
                 float all = 0.0f;
-                for (int w = stream * kw; w < (stream + 1) * kw; ++w) {
-                    if constexpr (kStack) all += (part[buffer][w][i + 8][j] + part[buffer][w][i + 4][j]) + part[buffer][w][i][j];
-                    else                  all += part[buffer][w][i][j];
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {                                  // all on their way at once
+                    const int of = stream * kw + (w < kw ? w : 0);
+                    float y = part[buffer][of][i][j];
+                    if constexpr (kStack) y += part[buffer][of][i + 4][j] + part[buffer][of][i + 8][j];
+                    all += w < kw ? y : 0.0f;
                 }
                 store_number(p, i, tile * 16 + j, p.scale * all);
             }
         }
         buffer ^= 1;                                                           // the next turn's sums go elsewhere; the one after it is behind a barrier
     };
-    Codes even, odd;
-    int64_t turn = blockIdx.x;
-    if (turn >= turns) return;
-    load(even, turn);
-    for (;;) {
-        const int64_t next = turn + gridDim.x, after = next + gridDim.x;
-        load(odd, next < turns ? next : turn);
-        multiply(even, turn);
-        if (next >= turns) break;
-        load(even, after < turns ? after : next);
-        multiply(odd, next);
-        if (after >= turns) break;
-        turn = after;
+    for (int64_t turn = blockIdx.x;;) {
+#pragma unroll
+        for (int u = 0; u < kRing; ++u) {
+            load(ring[(u + kRing - 1) % kRing], turn + (int64_t)(kRing - 1) * gridDim.x);
+            multiply(ring[u], turn);
+            turn += gridDim.x;
+            if (turn >= turns) return;
+        }
     }
 }
 

@@ -12,6 +12,8 @@ using same::fail_without_handle;
 
 namespace {
 
+constexpr int64_t kRowsOfA = (int64_t)1 << 24, kRowsOfB = (int64_t)1 << 28;
+
 template <class TI, int P, bool kStack, int kGroupLog2, int KB>
 void product_few(same::GroupProductArgs& p, int blocks, hipStream_t st)
 {
@@ -31,6 +33,13 @@ void product_few_by_width(same::GroupProductArgs& p, int blocks, hipStream_t st)
     else product_few<TI, P, kStack, kGroupLog2, 4>(p, blocks, st);
 }
 
+template <class TI, int kGroupLog2, int MT, int NT, int WK>
+void product_tiles(const same::GroupProductArgs& p, hipStream_t st)
+{
+    const int64_t across = 16 * NT * (4 / WK), tiles_a = (p.rows_a + 16 * MT - 1) / (16 * MT), tiles_b = ((p.rows_b + across - 1) / across + 7) / 8 * 8;
+    hipLaunchKernelGGL((same::group_product_kernel<TI, kGroupLog2, MT, NT, WK>), dim3((unsigned)(tiles_a * tiles_b)), dim3(256), 0, st, p);
+}
+
 template <class TI, int kGroupLog2>
 void product_launch(same::GroupProductArgs& p, hipStream_t st)
 {
@@ -39,8 +48,10 @@ void product_launch(same::GroupProductArgs& p, hipStream_t st)
         if constexpr (sizeof(TI) == 4) return p.rows_a <= 4 ? product_few_by_width<TI, 1, true, kGroupLog2>(p, blocks, st) : product_few_by_width<TI, 3, false, kGroupLog2>(p, blocks, st);
         else return product_few_by_width<TI, 1, false, kGroupLog2>(p, blocks, st);
     }
-    const int64_t tiles = ((p.rows_a + 15) / 16) * ((p.rows_b + 15) / 16);
-    hipLaunchKernelGGL((same::group_product_kernel<TI, kGroupLog2>), dim3((unsigned)at_most((tiles + 3) / 4, kMaxGroups)), dim3(256), 0, st, p);
+    constexpr int kTall = sizeof(TI) == 4 ? 2 : 4;                       // of 16 rows of a
+    if (p.rows_a <= 16)      product_tiles<TI, kGroupLog2, 1, 2, 4>(p, st);
+    else if (p.rows_a <= 32) product_tiles<TI, kGroupLog2, 2, 2, sizeof(TI) == 4 ? 2 : 4>(p, st);
+    else                     product_tiles<TI, kGroupLog2, kTall, 4, 1>(p, st);
 }
 
 template <class TI>
@@ -103,25 +114,29 @@ int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float
     if (a->rows == 0) return SAME_LDA_OK;
     const int group_log2 = __builtin_ctz((unsigned)b->type);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    same::GroupProductArgs p = {};
-    p.a = a->data;
-    p.rows_a = a->rows;
-    p.stride_a = a->stride;
-    p.width = a->width;
-    p.type_out = out->type;
-    p.codes = static_cast<const uint8_t*>(b->data);
-    p.scales = b->scales;
-    p.rows_b = b->rows;
-    p.pitch = same::micro_code_pitch(b->width);
-    p.scale_pitch = same::group_scale_pitch(b->width, group_log2);
-    p.scale = scale;
-    p.out = out->data;
-    p.out_stride = out->stride;
-    switch (a->type) {
-        case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, st); break;
-        case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, st); break;
-        default:              product_to<_Float16>(p, group_log2, st); break;
-    }
+    // slices of either operand: grids stay below 2^32 threads (the output's size bounds the tiles)
+    for (int64_t i = 0; i < a->rows; i += kRowsOfA)
+        for (int64_t j = 0; j < b->rows; j += kRowsOfB) {
+            same::GroupProductArgs p = {};
+            p.rows_a = at_most(a->rows - i, kRowsOfA);
+            p.rows_b = at_most(b->rows - j, kRowsOfB);
+            p.a = static_cast<const char*>(a->data) + i * a->stride * element_bytes(a->type);
+            p.stride_a = a->stride;
+            p.width = a->width;
+            p.type_out = out->type;
+            p.pitch = same::micro_code_pitch(b->width);
+            p.scale_pitch = same::group_scale_pitch(b->width, group_log2);
+            p.codes = static_cast<const uint8_t*>(b->data) + j * p.pitch;
+            p.scales = b->scales + j * p.scale_pitch;
+            p.scale = scale;
+            p.out = static_cast<char*>(out->data) + (i * out->stride + j) * element_bytes(out->type);
+            p.out_stride = out->stride;
+            switch (a->type) {
+                case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, st); break;
+                case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, st); break;
+                default:              product_to<_Float16>(p, group_log2, st); break;
+            }
+        }
     return launched("group_product");
 }
 
