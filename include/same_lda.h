@@ -365,8 +365,12 @@ int same_lda_group_quantize(const same_lda_rows* x, const same_lda_rows* group_o
  * are summed as s sum a q + b sum a, so a row of a that is not finite, or one for which the sum of (15 |s| + |b|) |a| is beyond
  * binary32, gives numbers that may be infinite or NaN.
  *   a            any number of rows, SAME_LDA_FLOAT, _BFLOAT or _HALF
- *   out          [a->rows][b->rows]                                                                               */
-int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* hip_stream);
+ *   out          [a->rows][b->rows]
+ *   workspace    as many bytes as same_lda_group_product_workspace says for the same matrices (none for few rows), aligned to 16; its
+ *                contents are scratch, in use until the call's kernels have ended                                  */
+int same_lda_group_product_workspace(const same_lda_rows* a, const same_lda_rows* b, size_t* bytes);
+int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* workspace,
+                           size_t workspace_bytes, void* hip_stream);
 
 /* Text of the last failure of this handle (when h is NULL: of the last failed call without a handle, same_lda_init
  * among them, on the calling thread).  The pointer stays valid until the next failing call.                        */

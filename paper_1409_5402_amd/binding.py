@@ -27,7 +27,7 @@ EXPORTS = ["same_lda_init", "same_lda_sweep", "same_lda_sweep_poisson", "same_ld
            "same_lda_set_batch", "same_lda_stage_batch", "same_lda_commit_batch", "same_lda_debug_draw_poisson", "same_lda_sddmm",
            "same_lda_vb_exp_elog_beta", "same_lda_vb_estep",
            "same_lda_embed", "same_lda_embed_grad_workspace", "same_lda_embed_grad", "same_lda_dropout", "same_lda_embed_dropout", "same_lda_embed_dropout_grad",
-           "same_lda_group_size", "same_lda_group_quantize", "same_lda_group_product", "same_lda_micro_size", "same_lda_micro_quantize", "same_lda_micro_product",
+           "same_lda_group_size", "same_lda_group_quantize", "same_lda_group_product_workspace", "same_lda_group_product", "same_lda_micro_size", "same_lda_micro_quantize", "same_lda_micro_product",
            "same_lda_get", "same_lda_set", "same_lda_get_pass", "same_lda_set_pass", "same_lda_task_count",
            "same_lda_debug_draw", "same_lda_debug_draw_noalloc", "same_lda_debug_chunk_limit", "same_lda_set_timing", "same_lda_get_timing", "same_lda_selftest",
            "same_lda_synchronize",
@@ -93,7 +93,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
         L.same_lda_embed_dropout_grad.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
         L.same_lda_group_size.argtypes = [c_int64, c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
         L.same_lda_group_quantize.argtypes = [c_void_p, c_void_p, c_void_p]
-        L.same_lda_group_product.argtypes = [c_void_p, c_void_p, c_float, c_void_p, c_void_p]
+        L.same_lda_group_product_workspace.argtypes = [c_void_p, c_void_p, POINTER(c_size_t)]
+        L.same_lda_group_product.argtypes = [c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
         L.same_lda_micro_size.argtypes = [c_int64, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
         L.same_lda_micro_quantize.argtypes = [c_void_p, c_void_p, c_void_p]
         L.same_lda_micro_product.argtypes = [c_void_p, c_void_p, c_float, c_void_p, c_void_p]
@@ -736,5 +737,12 @@ def group_product(a, b, scale=1.0, dtype=None, out=None):
     index = _gpu(a, b, out)
     x, rows = _rows(a), a.shape[0]
     out, o = _output(out, (rows, b.rows), rows, b.rows, dtype, a.dtype, b.codes.device)
-    _run(index, _library.same_lda_group_product, x, _rows(b), scale, o)
+    t, space, size = _rows(b), None, 0
+    if rows > 16 or b.width > 4096:                    # fewer and shorter rows need none
+        n = c_size_t()
+        if _library.same_lda_group_product_workspace(x, t, byref(n)):
+            raise SameLdaError(-1, _library.same_lda_last_error(None).decode())
+        size = n.value
+        space = _torch.empty(size, dtype=_torch.uint8, device=b.codes.device) if size else None
+    _run(index, _library.same_lda_group_product, x, t, scale, o, space.data_ptr() if size else None, size)
     return out

@@ -3,8 +3,11 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "element.h"
 #include "group_format.h"
+#include "to_lds.h"
 
 namespace same {
 
@@ -179,30 +182,87 @@ __device__ __forceinline__ v4u32 all_ones()
     return {one, one, one, one};
 }
 
-// Any number of rows.  A workgroup of four waves takes 16 MT rows of a by 16 NT (4 / WK) of b: its rows of a go by way of LDS, cut into
-// pieces and with their sums S, a block of 128 elements ahead; the codes come straight from memory into the registers of the one wave that
-// has these rows of b, a block ahead too.  WK waves share out the blocks of a row of b and their sums are added in order at the end: more
-// waves where rows of b are few.
-template <class TI, int kGroupLog2, int MT, int NT, int WK>
-__global__ __launch_bounds__(256, 2) void group_product_kernel(GroupProductArgs p)
+// Any number of rows, in two launches.  The first one lays the rows of a down as the lanes of the matrix instruction take them, cut into pieces
+// and filled up with zeros: per 16 rows and block of 128 elements 4 P operands of 1 KB; and the sums S of their groups, 32 groups to the
+// three operands of a bfloat16 instruction.
+struct GroupRowsArgs {
+    const void* a;
+    int64_t rows_a, stride_a;
+    int32_t width;
+    int32_t blocks, filled;          // of 128 elements in a row; with those that are zeros
+    v4u32* operands;                 // [16 rows][filled][4][P][64]
+    uint16_t* sums;                  // [16 rows][sets of 32 groups][3][64][8]
+};
+
+template <class TI, int kGroupLog2>
+__global__ __launch_bounds__(256) void group_rows_kernel(GroupRowsArgs a)
 {
     constexpr bool kHalf = kHalfMatrix<TI>;
-    constexpr int P = sizeof(TI) == 4 ? 3 : 1, kPer = 128 >> kGroupLog2, kSteps = 4 / kPer;   // groups of a block, instructions per group
-    constexpr int WN = 4 / WK, kUnits = MT * WK, kOwn = (kUnits + 3) / 4;             // 16 rows of a by a block each
+    constexpr int P = sizeof(TI) == 4 ? 3 : 1, kPer = 128 >> kGroupLog2, kSteps = 4 / kPer, kAll = 32 / kPer;   // groups of a block, instructions per group, blocks of a set
+    const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const int64_t tile = blockIdx.x;
+    const int64_t i = tile * 16 + r < a.rows_a ? tile * 16 + r : a.rows_a - 1;         // rows behind the last one: it again
+    const TI* const row = static_cast<const TI*>(a.a) + i * a.stride_a;
+    const int sets = (a.blocks + kAll - 1) / kAll, most = a.filled > sets * kAll ? a.filled : sets * kAll;
+    for (int k = blockIdx.y * 4 + (threadIdx.x >> 6); k < most; k += gridDim.y * 4) {
+        Eight<TI> raw[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) raw[t] = eight_at(row, k * 128 + 32 * t + 8 * h, a.width);
+        v4f32 total[kPer] = {};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            cut_eight(raw[t], k * 128 + 32 * t + 8 * h, a.width);
+            v4u32 c[P];
+            pieces_of<TI, P>(c, raw[t]);
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                if (k < a.filled) a.operands[((tile * a.filled + k) * (4 * P) + t * P + q) * 64 + lane] = c[q];
+                total[t / kSteps] = mfma_16<kHalf>(all_ones<kHalf>(), c[q], total[t / kSteps]);
+            }
+        }
+        if (h == 0 && k < sets * kAll)
+#pragma unroll
+            for (int g = 0; g < kPer; ++g) {
+                const int in = (k % kAll) * kPer + g;                                  // of the set: element in % 8 of lane (in / 8, r)
+                uint16_t* const to = a.sums + (((tile * sets + k / kAll) * 3 * 64 + (in / 8) * 16 + r) * 8 + in % 8);
+                float y = total[g][0];
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    const uint32_t bits = __float_as_uint(y);
+                    to[q * 64 * 8] = (uint16_t)(bits >> 16);
+                    y -= __uint_as_float(bits & 0xFFFF0000u);
+                }
+            }
+    }
+}
+
+// The second one: a workgroup of four waves takes 16 MT rows of a by 16 NT (4 / WK) of b.  The operands of a come to LDS a block ahead; the
+// codes come straight into the registers of the one wave that has these rows of b, a block ahead too.  WK waves share out the blocks of a row
+// of b, and their sums are added in order at the end: more waves where rows of b are few.
+struct GroupTilesArgs {
+    GroupProductArgs p;
+    const v4u32* operands;
+    const v4u32* sums;
+    int32_t blocks, filled;          // filled: a multiple of 2 WK
+};
+
+template <bool kHalf, int P, int kGroupLog2, int MT, int NT, int WK>
+__global__ __launch_bounds__(256, 2) void group_product_kernel(GroupTilesArgs a)
+{
+    constexpr int kPer = 128 >> kGroupLog2, kSteps = 4 / kPer, kAll = 32 / kPer;       // groups of a block, instructions per group, blocks of a set
+    constexpr int WN = 4 / WK, kFetch = MT * P * WK;                                   // operands that a wave fetches for a trip
     __shared__ union {
-        struct {
-            v4u32 x[2][WK][MT][4][P][64];                                             // as the lanes of the matrix instruction take them
-            float sum[2][WK][kPer][16 * MT];
-        } in;
+        v4u32 x[2][WK][MT][4][P][64];
         float out[WK > 1 ? WK - 1 : 1][WK > 1 ? MT * NT * 4 : 1][WK > 1 ? 64 * WN : 1];
     } lds;
+    const GroupProductArgs& p = a.p;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
     const int wn = wv % WN, wk = wv / WN;
     // the tiles of the same rows of b on one of the eight dies, one after the other: they find the codes in its cache
     const int64_t tiles_a = (p.rows_a + 16 * MT - 1) / (16 * MT), turn = blockIdx.x / 8, tile_b = turn / tiles_a * 8 + blockIdx.x % 8;
     const int64_t i0 = (turn % tiles_a) * (16 * MT), j0 = tile_b * (16 * NT * WN) + wn * (16 * NT);
-    if (tile_b * (16 * NT * WN) >= p.rows_b) return;                                  // the whole workgroup
-    const int blocks = (p.width + 127) / 128, trips = (blocks + WK - 1) / WK;
+    if (tile_b * (16 * NT * WN) >= p.rows_b) return;                                   // the whole workgroup
+    const int trips = a.filled / WK;
 
     const uint8_t* codes[NT];
     const uint8_t* scales[NT];
@@ -216,68 +276,70 @@ __global__ __launch_bounds__(256, 2) void group_product_kernel(GroupProductArgs 
         v4u32 w[NT];
         uint32_t sb[NT][kPer];
     };
-    const auto load_codes = [&](Codes& c, int trip) {                                 // blocks behind the row's end: those of its last, times zeros
-        const int k = trip * WK + wk < blocks ? trip * WK + wk : blocks - 1;
+    const auto load_codes = [&](Codes& c, int trip) {                                  // blocks behind the row's end: those of its last, times zeros
+        const int k = trip * WK + wk < a.blocks ? trip * WK + wk : a.blocks - 1;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            c.w[n] = *reinterpret_cast<const v4u32*>(codes[n] + (int64_t)k * 64);
+            c.w[n] = *reinterpret_cast<const v4u32*>(codes[n] + k * 64);
             struct alignas(4) Words { uint32_t v[kPer]; };
-            const Words s = *reinterpret_cast<const Words*>(scales[n] + (int64_t)k * (4 * kPer));
+            const Words s = *reinterpret_cast<const Words*>(scales[n] + k * (4 * kPer));
 #pragma unroll
             for (int g = 0; g < kPer; ++g) c.sb[n][g] = s.v[g];
         }
     };
-    Eight<TI> raw[kOwn][4];
-    const TI* rows[kOwn];
+    // a trip's operands, 4 MT P WK of them, shared out between the waves
+    const uint8_t* const from = reinterpret_cast<const uint8_t*>(a.operands + i0 / 16 * a.filled * (4 * P) * 64);
+    const auto fetch = [&](int trip) {
+        if (trip >= trips) return;
+        v4u32* const to = &lds.x[trip & 1][0][0][0][0][0];
 #pragma unroll
-    for (int o = 0; o < kOwn; ++o) {
-        const int64_t i = i0 + 16 * ((wv + 4 * o) % MT) + r;
-        rows[o] = static_cast<const TI*>(p.a) + (i < p.rows_a ? i : p.rows_a - 1) * p.stride_a;
-    }
-    const auto load_rows = [&](int trip) {
-#pragma unroll
-        for (int o = 0; o < kOwn; ++o)
-            if (wv + 4 * o < kUnits)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) raw[o][t] = eight_at(rows[o], (trip * WK + (wv + 4 * o) / MT) * 128 + 32 * t + 8 * h, p.width);
-    };
-    const auto put_rows = [&](int trip) {
-#pragma unroll
-        for (int o = 0; o < kOwn; ++o) {
-            const int u = wv + 4 * o;
-            if (u >= kUnits) continue;
-            v4f32 total[kPer] = {};
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                cut_eight(raw[o][t], (trip * WK + u / MT) * 128 + 32 * t + 8 * h, p.width);
-                v4u32 c[P];
-                pieces_of<TI, P>(c, raw[o][t]);
-#pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    lds.in.x[trip & 1][u / MT][u % MT][t][q][lane] = c[q];
-                    total[t / kSteps] = mfma_16<kHalf>(all_ones<kHalf>(), c[q], total[t / kSteps]);
-                }
-            }
-            if (h == 0)
-#pragma unroll
-                for (int g = 0; g < kPer; ++g) lds.in.sum[trip & 1][u / MT][g][16 * (u % MT) + r] = total[g][0];
+        for (int f = 0; f < kFetch; ++f) {
+            const int e = f * 4 + wv, w = e / (MT * 4 * P), m = e / (4 * P) % MT, at = e % (4 * P);
+            to_lds_16(from + ((int64_t)m * a.filled + trip * WK + w) * (4 * P * 1024) + at * 1024, lane * 16, to + e * 64);
         }
     };
+    fetch(0);
+    Codes even, odd;
+    load_codes(even, 0);
+
+    // sum_g b_g S_g to begin with, by the first of the waves that share a row
     v4f32 acc[MT][NT] = {};
+    if (wk == 0) {
+        const int sets = (a.blocks + kAll - 1) / kAll, groups = a.blocks * kPer;
+        for (int e = 0; e < sets; ++e) {
+            v4u32 b[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                uint32_t sb[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const int g = e * 32 + 8 * h + q;
+                    sb[q] = reinterpret_cast<const uint32_t*>(scales[n])[g < groups ? g : groups - 1];      // groups behind the last: it, times zero
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) b[n][q] = __builtin_amdgcn_perm(sb[2 * q + 1], sb[2 * q], 0x07060302u);
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    const v4u32 s = a.sums[(((i0 / 16 + m) * sets + e) * 3 + q) * 64 + lane];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[m][n] = mfma_16<false>(s, b[n], acc[m][n]);
+                }
+        }
+    }
     const auto multiply = [&](const Codes& c, int trip) {
-        const auto& x = lds.in.x[trip & 1][wk];
+        const auto& x = lds.x[trip & 1][wk];
 #pragma unroll
         for (int g = 0; g < kPer; ++g) {
             v4u32 part[kSteps][MT][P];
-            v4f32 s[MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                s[m] = *reinterpret_cast<const v4f32*>(&lds.in.sum[trip & 1][wk][g][16 * m + 4 * h]);
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int t = 0; t < kSteps; ++t)
 #pragma unroll
                     for (int q = 0; q < P; ++q) part[t][m][q] = x[m][g * kSteps + t][q][lane];
-            }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 v4f32 d[MT] = {};
@@ -289,35 +351,27 @@ __global__ __launch_bounds__(256, 2) void group_product_kernel(GroupProductArgs 
 #pragma unroll
                         for (int m = 0; m < MT; ++m) d[m] = mfma_16<kHalf>(part[t][m][q], b, d[m]);
                 }
-                const float step = from_bfloat_bits(c.sb[n][g] & 0xFFFFu), base = __uint_as_float(c.sb[n][g] & 0xFFFF0000u);
+                const float step = from_bfloat_bits(c.sb[n][g] & 0xFFFFu);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[m][n][q] = __builtin_fmaf(step, d[m][q], __builtin_fmaf(base, s[m][q], acc[m][n][q]));
+                    for (int q = 0; q < 4; ++q) acc[m][n][q] = __builtin_fmaf(step, d[m][q], acc[m][n][q]);
+                if constexpr (kPer == 4 && MT == 4) __builtin_amdgcn_sched_barrier(0);    // else more is begun than there are registers for
             }
         }
     };
-    Codes even, odd;
-    load_rows(0);
-    load_codes(even, 0);
-    put_rows(0);
-    __syncthreads();
-    for (int trip = 0;;) {
-        if (trip + 1 < trips) load_rows(trip + 1);
+    arrived<0>();
+    for (int trip = 0; trip < trips; trip += 2) {
+        fetch(trip + 1);                                                               // where the trip before this one read, which a barrier ended
         load_codes(odd, trip + 1);
         multiply(even, trip);
-        if (++trip >= trips) break;
-        put_rows(trip);                                                               // where the trip before last read, which a barrier ended
-        __syncthreads();
-        if (trip + 1 < trips) load_rows(trip + 1);
-        load_codes(even, trip + 1);
-        multiply(odd, trip);
-        if (++trip >= trips) break;
-        put_rows(trip);
-        __syncthreads();
+        arrived<0>();
+        fetch(trip + 2);
+        load_codes(even, trip + 2);
+        multiply(odd, trip + 1);
+        arrived<0>();
     }
-    if constexpr (WK > 1) {
-        __syncthreads();
+    if constexpr (WK > 1) {                                                            // (no one reads the rows of a any more)
         if (wk > 0)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -336,15 +390,22 @@ __global__ __launch_bounds__(256, 2) void group_product_kernel(GroupProductArgs 
 #pragma unroll
                     for (int q = 0; q < 4; ++q) acc[m][n][q] += lds.out[w][(m * NT + n) * 4 + q][wn * 64 + lane];
     }
+    const auto store = [&](auto* out) {
+        using TO = std::remove_pointer_t<decltype(out)>;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int64_t i = i0 + 16 * m + 4 * h + q;
+            for (int q = 0; q < 4; ++q) {
+                const int64_t i = i0 + 16 * m + 4 * h + q;
+                TO* const row = out + i * p.out_stride + j0 + r;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-                if (i < p.rows_a && j0 + 16 * n + r < p.rows_b) store_number(p, i, j0 + 16 * n + r, p.scale * acc[m][n][q]);
-        }
+                for (int n = 0; n < NT; ++n)
+                    if (i < p.rows_a && j0 + 16 * n + r < p.rows_b) row[16 * n] = (TO)(p.scale * acc[m][n][q]);
+            }
+    };
+    if (p.type_out == 0)      store(static_cast<float*>(p.out));
+    else if (p.type_out == 1) store(static_cast<__bf16*>(p.out));
+    else                      store(static_cast<_Float16*>(p.out));
 }
 
 // Few rows of a, up to 16.  A wave keeps its part of them, KB blocks of 128 elements, in registers and goes through the rows of b, 16 at

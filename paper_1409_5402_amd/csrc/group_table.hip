@@ -12,7 +12,29 @@ using same::fail_without_handle;
 
 namespace {
 
-constexpr int64_t kRowsOfA = (int64_t)1 << 24, kRowsOfB = (int64_t)1 << 28;
+// Rows of either operand in a launch: grids stay below 2^32 threads (the output's size bounds the tiles), and what rows of a are laid down in
+// below 256 MB or 4096 rows.
+constexpr int64_t kRowsOfB = (int64_t)1 << 28;
+int64_t rows_of_a(const same_lda_rows* a)
+{
+    const int64_t most = ((int64_t)1 << 28) / (same::micro_groups(a->width) * 128 * (a->type == SAME_LDA_FLOAT ? 6 : 2)) / 64 * 64;
+    return most < 4096 ? 4096 : most > ((int64_t)1 << 24) ? (int64_t)1 << 24 : most;
+}
+
+bool few_rows(const same_lda_rows* a) { return a->rows <= 16 && same::micro_groups(a->width) <= 32; }
+
+// Workspace of the rows of a, laid down for tiles of up to 64 rows and trips of up to 8 blocks, and of their sums.
+struct RowsSpace {
+    size_t operands, bytes;
+};
+
+RowsSpace rows_space(const same_lda_rows* a)
+{
+    if (few_rows(a)) return {0, 0};
+    const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 63) / 64 * 4), filled = (size_t)((same::micro_groups(a->width) + 7) / 8 * 8);
+    const size_t operands = tiles * filled * 4 * (a->type == SAME_LDA_FLOAT ? 3 : 1) * 1024;
+    return {operands, operands + tiles * ((filled * 4 + 31) / 32) * 3 * 1024};
+}
 
 template <class TI, int P, bool kStack, int kGroupLog2, int KB>
 void product_few(same::GroupProductArgs& p, int blocks, hipStream_t st)
@@ -34,34 +56,48 @@ void product_few_by_width(same::GroupProductArgs& p, int blocks, hipStream_t st)
 }
 
 template <class TI, int kGroupLog2, int MT, int NT, int WK>
-void product_tiles(const same::GroupProductArgs& p, hipStream_t st)
+void product_tiles(const same::GroupProductArgs& p, void* operands, void* sums, hipStream_t st)
 {
-    const int64_t across = 16 * NT * (4 / WK), tiles_a = (p.rows_a + 16 * MT - 1) / (16 * MT), tiles_b = ((p.rows_b + across - 1) / across + 7) / 8 * 8;
-    hipLaunchKernelGGL((same::group_product_kernel<TI, kGroupLog2, MT, NT, WK>), dim3((unsigned)(tiles_a * tiles_b)), dim3(256), 0, st, p);
+    constexpr int P = sizeof(TI) == 4 ? 3 : 1;
+    const int blocks = (p.width + 127) / 128, filled = (blocks + 2 * WK - 1) / (2 * WK) * (2 * WK);
+    const int64_t tiles_a = (p.rows_a + 16 * MT - 1) / (16 * MT);
+    const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, static_cast<same::v4u32*>(operands), static_cast<uint16_t*>(sums)};
+    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT), (unsigned)at_most((filled + 3) / 4, 65535)), dim3(256), 0, st, rows);
+    const int64_t across = 16 * NT * (4 / WK), tiles_b = ((p.rows_b + across - 1) / across + 7) / 8 * 8;
+    const same::GroupTilesArgs tiles = {p, static_cast<const same::v4u32*>(operands), static_cast<const same::v4u32*>(sums), blocks, filled};
+    hipLaunchKernelGGL((same::group_product_kernel<same::kHalfMatrix<TI>, P, kGroupLog2, MT, NT, WK>), dim3((unsigned)(tiles_a * tiles_b)), dim3(256), 0, st, tiles);
 }
 
 template <class TI, int kGroupLog2>
-void product_launch(same::GroupProductArgs& p, hipStream_t st)
+void product_launch(same::GroupProductArgs& p, bool few, void* operands, void* sums, hipStream_t st)
 {
     const int blocks = (p.width + 127) / 128;
-    if (p.rows_a <= 16 && blocks <= 32) {
+    if (few) {
         if constexpr (sizeof(TI) == 4) return p.rows_a <= 4 ? product_few_by_width<TI, 1, true, kGroupLog2>(p, blocks, st) : product_few_by_width<TI, 3, false, kGroupLog2>(p, blocks, st);
         else return product_few_by_width<TI, 1, false, kGroupLog2>(p, blocks, st);
     }
     constexpr int kTall = sizeof(TI) == 4 ? 2 : 4;                       // of 16 rows of a
-    if (p.rows_a <= 16)      product_tiles<TI, kGroupLog2, 1, 2, 4>(p, st);
-    else if (p.rows_a <= 32) product_tiles<TI, kGroupLog2, 2, 2, sizeof(TI) == 4 ? 2 : 4>(p, st);
-    else                     product_tiles<TI, kGroupLog2, kTall, 4, 1>(p, st);
+    if (p.rows_a <= 16)      product_tiles<TI, kGroupLog2, 1, 2, 4>(p, operands, sums, st);
+    else if (p.rows_a <= 32) product_tiles<TI, kGroupLog2, 2, 2, sizeof(TI) == 4 ? 2 : 4>(p, operands, sums, st);
+    else                     product_tiles<TI, kGroupLog2, kTall, 4, 1>(p, operands, sums, st);
 }
 
 template <class TI>
-void product_to(same::GroupProductArgs& p, int group_log2, hipStream_t st)
+void product_to(same::GroupProductArgs& p, int group_log2, bool few, void* operands, void* sums, hipStream_t st)
 {
     switch (group_log2) {
-        case 5:  return product_launch<TI, 5>(p, st);
-        case 6:  return product_launch<TI, 6>(p, st);
-        default: return product_launch<TI, 7>(p, st);
+        case 5:  return product_launch<TI, 5>(p, few, operands, sums, st);
+        case 6:  return product_launch<TI, 6>(p, few, operands, sums, st);
+        default: return product_launch<TI, 7>(p, few, operands, sums, st);
     }
+}
+
+int check_product(const same_lda_rows* a, const same_lda_rows* b)
+{
+    int rc = check_rows("group_product", "a", a, kNumbers);
+    if (!rc) rc = check_rows("group_product", "b", b, kGrouped);
+    if (!rc && a->width != b->width) rc = fail_without_handle(SAME_LDA_EINVAL, "group_product: rows of %d and of %d elements", a->width, b->width);
+    return rc;
 }
 
 }  // namespace
@@ -99,12 +135,20 @@ int same_lda_group_quantize(const same_lda_rows* x, const same_lda_rows* group_o
     return launched("group_quantize");
 }
 
-int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* hip_stream)
+int same_lda_group_product_workspace(const same_lda_rows* a, const same_lda_rows* b, size_t* bytes)
 {
-    int rc = check_rows("group_product", "a", a, kNumbers);
-    if (!rc) rc = check_rows("group_product", "b", b, kGrouped);
+    if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "group_product: bytes is null");
+    const int rc = check_product(a, b);
     if (rc) return rc;
-    if (a->width != b->width) return fail_without_handle(SAME_LDA_EINVAL, "group_product: rows of %d and of %d elements", a->width, b->width);
+    *bytes = a->rows > 0 && b->rows > 0 ? rows_space(a).bytes : 0;
+    return SAME_LDA_OK;
+}
+
+int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* workspace, size_t workspace_bytes,
+                           void* hip_stream)
+{
+    int rc = check_product(a, b);
+    if (rc) return rc;
     if (b->rows == 0) return SAME_LDA_OK;                                                  // no columns: out is not looked at
     if ((rc = check_rows("group_product", "out", out, kNumbers, INT32_MAX))) return rc;
     if (out->rows != a->rows || out->width != b->rows)
@@ -112,13 +156,19 @@ int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float
                                    (long long)out->rows, out->width);
     if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "group_product: the scale must be finite");
     if (a->rows == 0) return SAME_LDA_OK;
+    const RowsSpace space = rows_space(a);
+    if (space.bytes > 0 && (!workspace || workspace_bytes < space.bytes || (uintptr_t)workspace % 16))
+        return fail_without_handle(SAME_LDA_EINVAL, "group_product: needs %zu bytes of workspace aligned to 16 (got %zu)", space.bytes, workspace ? workspace_bytes : (size_t)0);
+    void* const sums = static_cast<char*>(workspace) + space.operands;
+    const bool few = few_rows(a);
+    const int64_t rows_each = rows_of_a(a);
     const int group_log2 = __builtin_ctz((unsigned)b->type);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     // slices of either operand: grids stay below 2^32 threads (the output's size bounds the tiles)
-    for (int64_t i = 0; i < a->rows; i += kRowsOfA)
+    for (int64_t i = 0; i < a->rows; i += rows_each)
         for (int64_t j = 0; j < b->rows; j += kRowsOfB) {
             same::GroupProductArgs p = {};
-            p.rows_a = at_most(a->rows - i, kRowsOfA);
+            p.rows_a = at_most(a->rows - i, rows_each);
             p.rows_b = at_most(b->rows - j, kRowsOfB);
             p.a = static_cast<const char*>(a->data) + i * a->stride * element_bytes(a->type);
             p.stride_a = a->stride;
@@ -132,9 +182,9 @@ int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float
             p.out = static_cast<char*>(out->data) + (i * out->stride + j) * element_bytes(out->type);
             p.out_stride = out->stride;
             switch (a->type) {
-                case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, st); break;
-                case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, st); break;
-                default:              product_to<_Float16>(p, group_log2, st); break;
+                case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, few, workspace, sums, st); break;
+                case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, few, workspace, sums, st); break;
+                default:              product_to<_Float16>(p, group_log2, few, workspace, sums, st); break;
             }
         }
     return launched("group_product");

@@ -8,6 +8,7 @@
 
 #include "element.h"
 #include "micro_format.h"
+#include "to_lds.h"
 
 namespace same {
 
@@ -236,35 +237,11 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_a, uint32_t t
     ta = first + at - tb * in;
 }
 
-// 16 or 4 bytes per lane from base + offset straight to consecutive places of LDS from `to` on.  Written as assembly because the
-// compiler takes the builtin for a store that any later read from LDS may depend on, and waits for it there: here the only
-// readers are behind arrived().  No vector register is written.  The copy of the base is for two waits that the compiler does not
-// look for inside: a base that the vector unit has just written, and the state between writing m0 and using it.
-__device__ __forceinline__ void to_lds_16(const uint8_t* base, uint32_t offset, const void* to)
-{
-    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to;
-    uint64_t copy;
-    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(copy) : "s"(at), "v"(offset), "s"(base) : "m0");
-}
-__device__ __forceinline__ void to_lds_4(const uint8_t* base, uint32_t offset, const void* to)
-{
-    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to;
-    uint64_t copy;
-    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0" : "=&s"(copy) : "s"(at), "v"(offset), "s"(base) : "m0");
-}
 // f(0), f(1), ... f(N - 1), the argument a constant
 template <class F, int... I>
 __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f)
 {
     (f(std::integral_constant<int, I>()), ...);
-}
-
-// All of this wave's loads but the last N have come (they end in their order), then all waves'.
-template <int N>
-__device__ __forceinline__ void arrived()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-    __syncthreads();
 }
 
 // A wave's sums go out by way of LDS, 32 rows of its part of the tile at a time, so that a lane stores 16 bytes of one row.

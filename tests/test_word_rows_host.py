@@ -48,7 +48,7 @@ def test_bad_matrices_are_refused(bad, word):
     refused(L.same_lda_embed_dropout_grad(ref(m), P, 4, 1.0, ref(d), 0, ref(ok), P, 1 << 30, None), word)
     refused(L.same_lda_embed_dropout_grad(ref(ok), P, 4, 1.0, ref(d), 0, ref(m), P, 1 << 30, None), word)
     refused(L.same_lda_group_quantize(ref(m), ref(g), None), word)
-    refused(L.same_lda_group_product(ref(m), ref(g), 1.0, ref(ok), None), word)
+    refused(L.same_lda_group_product(ref(m), ref(g), 1.0, ref(ok), P, 1 << 40, None), word)
 
 
 @pytest.mark.parametrize("group", GROUPS)
@@ -59,7 +59,7 @@ def test_bad_grouped_matrices_are_refused(group):
         refused(L.same_lda_embed(ref(m), P, 4, 1.0, ref(ok), None), word)
         refused(L.same_lda_embed_dropout(ref(m), P, 4, 1.0, ref(d), ref(ok), None), word)
         refused(L.same_lda_group_quantize(ref(ok), ref(m), None), word)
-        refused(L.same_lda_group_product(ref(ok), ref(m), 1.0, ref(ok), None), word)
+        refused(L.same_lda_group_product(ref(ok), ref(m), 1.0, ref(ok), P, 1 << 40, None), word)
 
 
 @pytest.mark.parametrize("p, word", [(-0.1, "[0, 1]"), (1.1, "[0, 1]"), (float("nan"), "[0, 1]"), (float("inf"), "[0, 1]")])
@@ -104,15 +104,15 @@ def test_shapes_types_tokens_and_scales_are_refused():
     refused(L.same_lda_group_quantize(ref(a), ref(m), None), "must be grouped")
     refused(L.same_lda_group_quantize(ref(a), ref(rows(type=64, rows=5)), None), "into")
     refused(L.same_lda_group_quantize(ref(a), ref(rows(type=64, width=9)), None), "into")
-    refused(L.same_lda_group_product(ref(g), ref(g), 1.0, ref(rows(width=4)), None), "must not be grouped")
-    refused(L.same_lda_group_product(ref(m), ref(g), 1.0, ref(rows(width=4)), None), "must not be microscaled")
-    refused(L.same_lda_group_product(ref(a), ref(m), 1.0, ref(rows(width=4)), None), "must be grouped")
-    refused(L.same_lda_group_product(ref(a), ref(a), 1.0, ref(rows(width=4)), None), "must be grouped")
-    refused(L.same_lda_group_product(ref(a), ref(rows(type=32, width=9)), 1.0, ref(rows(width=4)), None), "elements")
-    refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(rows(width=5)), None), "do not give")
-    refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(rows(rows=5, width=4)), None), "do not give")
-    refused(L.same_lda_group_product(ref(a), ref(g), float("nan"), ref(rows(width=4)), None), "finite")
-    refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(g), None), "must not be grouped")
+    refused(L.same_lda_group_product(ref(g), ref(g), 1.0, ref(rows(width=4)), P, 1 << 40, None), "must not be grouped")
+    refused(L.same_lda_group_product(ref(m), ref(g), 1.0, ref(rows(width=4)), P, 1 << 40, None), "must not be microscaled")
+    refused(L.same_lda_group_product(ref(a), ref(m), 1.0, ref(rows(width=4)), P, 1 << 40, None), "must be grouped")
+    refused(L.same_lda_group_product(ref(a), ref(a), 1.0, ref(rows(width=4)), P, 1 << 40, None), "must be grouped")
+    refused(L.same_lda_group_product(ref(a), ref(rows(type=32, width=9)), 1.0, ref(rows(width=4)), P, 1 << 40, None), "elements")
+    refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(rows(width=5)), P, 1 << 40, None), "do not give")
+    refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(rows(rows=5, width=4)), P, 1 << 40, None), "do not give")
+    refused(L.same_lda_group_product(ref(a), ref(g), float("nan"), ref(rows(width=4)), P, 1 << 40, None), "finite")
+    refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(g), P, 1 << 40, None), "must not be grouped")
     for bad in [(-1, 8, 32), (1 << 31, 8, 32), (1, 0, 32), (1, (1 << 20) + 1, 32), (1, 8, 16), (1, 8, 0), (1, 8, 256), (1, 8, 3)]:
         refused(L.same_lda_group_size(*bad, ref(n), ref(n)), "shape")
     refused(L.same_lda_group_size(1, 8, 32, None, ref(n)), "null")
@@ -128,8 +128,8 @@ def test_empty_calls_do_nothing():
     assert L.same_lda_embed_dropout_grad(ref(a), P, 4, 1.0, ref(d), 0, ref(e), None, 0, None) == 0
     assert L.same_lda_embed(ref(g), P, 8, 1.0, ref(e), None) == 0
     assert L.same_lda_group_quantize(ref(e), ref(eg), None) == 0
-    assert L.same_lda_group_product(ref(e), ref(g), 1.0, ref(rows(rows=0, width=4, data=None)), None) == 0
-    assert L.same_lda_group_product(ref(a), ref(eg), 1.0, None, None) == 0
+    assert L.same_lda_group_product(ref(e), ref(g), 1.0, ref(rows(rows=0, width=4, data=None)), P, 1 << 40, None) == 0
+    assert L.same_lda_group_product(ref(a), ref(eg), 1.0, None, P, 1 << 40, None) == 0
 
 
 def test_sizes_of_grouped_matrices():
