@@ -236,71 +236,85 @@ __global__ __launch_bounds__(256) void group_rows_kernel(GroupRowsArgs a)
     }
 }
 
-// The second one: a workgroup of four waves takes 16 MT rows of a by 16 NT (4 / WK) of b.  The operands of a come to LDS a block ahead; the
-// codes come straight into the registers of the one wave that has these rows of b, a block ahead too.  WK waves share out the blocks of a row
-// of b, and their sums are added in order at the end: more waves where rows of b are few.
+// The second one: WM WN WK waves take 16 MT WM rows of a by 16 NT WN of b.  All operands come straight to LDS, kStages - 1 trips ahead, in
+// pieces of 1 KB as the lanes take them: what a trip waits for was asked for some two thousand cycles a stage before.  WK waves share out the
+// blocks of a row of b, and their sums are added in order at the end: more waves where rows of b are few.
 struct GroupTilesArgs {
     GroupProductArgs p;
     const v4u32* operands;
     const v4u32* sums;
-    int32_t blocks, filled;          // filled: a multiple of 2 WK
+    int32_t blocks, filled;          // filled: a multiple of WK
 };
 
-template <bool kHalf, int P, int kGroupLog2, int MT, int NT, int WK>
-__global__ __launch_bounds__(256, 2) void group_product_kernel(GroupTilesArgs a)
+template <int P, int kGroupLog2, int MT, int NT, int WM, int WN, int WK>
+struct GroupStage {
+    v4u32 rows[WK][WM][MT][4][P][64];
+    v4u32 codes[WK][WN][NT][64];
+    uint32_t scales[WK][WN][NT][16][128 >> kGroupLog2];
+};
+
+template <bool kHalf, int P, int kGroupLog2, int MT, int NT, int WM, int WN, int WK, int kStages>
+__global__ __launch_bounds__(64 * WM * WN * WK, 2) void group_product_kernel(GroupTilesArgs a)
 {
     constexpr int kPer = 128 >> kGroupLog2, kSteps = 4 / kPer, kAll = 32 / kPer;       // groups of a block, instructions per group, blocks of a set
-    constexpr int WN = 4 / WK, kFetch = MT * P * WK;                                   // operands that a wave fetches for a trip
+    constexpr int kWaves = WM * WN * WK;
+    using Stage = GroupStage<P, kGroupLog2, MT, NT, WM, WN, WK>;
     __shared__ union {
-        v4u32 x[2][WK][MT][4][P][64];
-        float out[WK > 1 ? WK - 1 : 1][WK > 1 ? MT * NT * 4 : 1][WK > 1 ? 64 * WN : 1];
+        Stage in[kStages];
+        float out[WK > 1 ? WK - 1 : 1][WK > 1 ? MT * NT * 4 : 1][WK > 1 ? 64 * WM * WN : 1];
     } lds;
     const GroupProductArgs& p = a.p;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
-    const int wn = wv % WN, wk = wv / WN;
+    const int wk = wv / (WM * WN), wm = wv / WN % WM, wn = wv % WN;
     // the tiles of the same rows of b on one of the eight dies, one after the other: they find the codes in its cache
-    const int64_t tiles_a = (p.rows_a + 16 * MT - 1) / (16 * MT), turn = blockIdx.x / 8, tile_b = turn / tiles_a * 8 + blockIdx.x % 8;
-    const int64_t i0 = (turn % tiles_a) * (16 * MT), j0 = tile_b * (16 * NT * WN) + wn * (16 * NT);
-    if (tile_b * (16 * NT * WN) >= p.rows_b) return;                                   // the whole workgroup
+    constexpr int kTall = 16 * MT * WM, kWide = 16 * NT * WN;
+    const int64_t tiles_a = (p.rows_a + kTall - 1) / kTall, turn = blockIdx.x / 8, tile_b = turn / tiles_a * 8 + blockIdx.x % 8;
+    const int64_t first_i = turn % tiles_a * kTall, first_j = tile_b * kWide;
+    if (first_j >= p.rows_b) return;                                                   // the whole workgroup
+    const int64_t i0 = first_i + wm * (16 * MT), j0 = first_j + wn * (16 * NT);
     const int trips = a.filled / WK;
+    const int last = (int)(p.rows_b - first_j < kWide ? p.rows_b - first_j : kWide) - 1;     // rows behind the last are computed from it and not written
 
-    const uint8_t* codes[NT];
-    const uint8_t* scales[NT];
+    // what a trip needs, in equal numbers for every wave (the last pieces are fetched twice where they do not go round)
+    constexpr int kRows = WK * WM * MT * 4 * P, kCodes = WK * WN * NT, kWords = WK * WN * NT * 16 * kPer;
+    constexpr int kRowsEach = (kRows + kWaves - 1) / kWaves, kCodesEach = (kCodes + kWaves - 1) / kWaves, kWordsEach = (kWords + 64 * kWaves - 1) / (64 * kWaves);
+    constexpr int kEach = kRowsEach + kCodesEach + kWordsEach;
+    const uint8_t* const rows = reinterpret_cast<const uint8_t*>(a.operands + first_i / 16 * a.filled * (4 * P) * 64);
+    const uint8_t* const codes = p.codes + first_j * p.pitch;
+    const uint8_t* const scales = p.scales + first_j * p.scale_pitch;
+    uint32_t code_at[kCodesEach], word_at[kWordsEach];                                 // of this lane, in the tile's rows of b
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int64_t j = j0 + 16 * n + r < p.rows_b ? j0 + 16 * n + r : p.rows_b - 1;   // rows behind the last are computed from it and not written
-        codes[n] = p.codes + j * p.pitch + 16 * h;
-        scales[n] = p.scales + j * p.scale_pitch;
+    for (int f = 0; f < kCodesEach; ++f) {
+        const int e = min(f * kWaves + wv, kCodes - 1);
+        code_at[f] = (uint32_t)min(e % (WN * NT) * 16 + r, last) * (uint32_t)p.pitch + 16 * h;
     }
-    struct Codes {
-        v4u32 w[NT];
-        uint32_t sb[NT][kPer];
-    };
-    const auto load_codes = [&](Codes& c, int trip) {                                  // blocks behind the row's end: those of its last, times zeros
-        const int k = trip * WK + wk < a.blocks ? trip * WK + wk : a.blocks - 1;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            c.w[n] = *reinterpret_cast<const v4u32*>(codes[n] + k * 64);
-            struct alignas(4) Words { uint32_t v[kPer]; };
-            const Words s = *reinterpret_cast<const Words*>(scales[n] + k * (4 * kPer));
-#pragma unroll
-            for (int g = 0; g < kPer; ++g) c.sb[n][g] = s.v[g];
-        }
-    };
-    // a trip's operands, 4 MT P WK of them, shared out between the waves
-    const uint8_t* const from = reinterpret_cast<const uint8_t*>(a.operands + i0 / 16 * a.filled * (4 * P) * 64);
+    for (int f = 0; f < kWordsEach; ++f) {
+        const int e = min((f * kWaves + wv) * 64, kWords - 64) + lane;
+        word_at[f] = (uint32_t)min(e / kPer % kWide, last) * (uint32_t)p.scale_pitch + 4 * (e % kPer);
+    }
     const auto fetch = [&](int trip) {
-        if (trip >= trips) return;
-        v4u32* const to = &lds.x[trip & 1][0][0][0][0][0];
+        Stage& to = lds.in[trip % kStages];
+        const int t = trip < trips ? trip : trips - 1;                                 // behind the last one: it again, not used
 #pragma unroll
-        for (int f = 0; f < kFetch; ++f) {
-            const int e = f * 4 + wv, w = e / (MT * 4 * P), m = e / (4 * P) % MT, at = e % (4 * P);
-            to_lds_16(from + ((int64_t)m * a.filled + trip * WK + w) * (4 * P * 1024) + at * 1024, lane * 16, to + e * 64);
+        for (int f = 0; f < kRowsEach; ++f) {
+            const int e = min(f * kWaves + wv, kRows - 1), k = e / (WM * MT * 4 * P), m = e / (4 * P) % (WM * MT), at = e % (4 * P);
+            to_lds_16(uniform(rows + (int64_t)(m * a.filled + t * WK + k) * (4 * P * 1024) + at * 1024), lane * 16, &to.rows[0][0][0][0][0][0] + e * 64);
+        }
+#pragma unroll
+        for (int f = 0; f < kCodesEach; ++f) {
+            const int e = min(f * kWaves + wv, kCodes - 1), k = min(t * WK + e / (WN * NT), a.blocks - 1);      // blocks behind the row's end: its last, times zeros
+            to_lds_16(uniform(codes + (int64_t)k * 64), code_at[f], &to.codes[0][0][0][0] + e * 64);
+        }
+#pragma unroll
+        for (int f = 0; f < kWordsEach; ++f) {
+            const int e = min((f * kWaves + wv) * 64, kWords - 64), k = min(t * WK + e / (kWide * kPer), a.blocks - 1);
+            to_lds_4(uniform(scales + (int64_t)k * (4 * kPer)), word_at[f], &to.scales[0][0][0][0][0] + e);
         }
     };
-    fetch(0);
-    Codes even, odd;
-    load_codes(even, 0);
+    static_assert(kWide * kPer % 64 == 0, "a piece of scales is of one block");
+#pragma unroll
+    for (int s = 0; s + 1 < kStages; ++s) fetch(s);
 
     // sum_g b_g S_g to begin with, by the first of the waves that share a row
     v4f32 acc[MT][NT] = {};
@@ -310,12 +324,11 @@ __global__ __launch_bounds__(256, 2) void group_product_kernel(GroupTilesArgs a)
             v4u32 b[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
+                const int64_t j = j0 + 16 * n + r < p.rows_b ? j0 + 16 * n + r : p.rows_b - 1;
+                const uint32_t* const of = reinterpret_cast<const uint32_t*>(p.scales + j * p.scale_pitch);
                 uint32_t sb[8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int g = e * 32 + 8 * h + q;
-                    sb[q] = reinterpret_cast<const uint32_t*>(scales[n])[g < groups ? g : groups - 1];      // groups behind the last: it, times zero
-                }
+                for (int q = 0; q < 8; ++q) sb[q] = of[min(e * 32 + 8 * h + q, groups - 1)];      // groups behind the last: it, times zero
 #pragma unroll
                 for (int q = 0; q < 4; ++q) b[n][q] = __builtin_amdgcn_perm(sb[2 * q + 1], sb[2 * q], 0x07060302u);
             }
@@ -329,8 +342,18 @@ __global__ __launch_bounds__(256, 2) void group_product_kernel(GroupTilesArgs a)
                 }
         }
     }
-    const auto multiply = [&](const Codes& c, int trip) {
-        const auto& x = lds.x[trip & 1][wk];
+    for (int trip = 0; trip < trips; ++trip) {
+        arrived<(kStages - 2) * kEach>();
+        fetch(trip + kStages - 1);                                                     // where the trip before this one read, which this barrier ended
+        const Stage& in = lds.in[trip % kStages];
+        v4u32 w[NT];
+        uint32_t sb[NT][kPer];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            w[n] = in.codes[wk][wn][n][lane];
+#pragma unroll
+            for (int g = 0; g < kPer; ++g) sb[n][g] = in.scales[wk][wn][n][r][g];
+        }
 #pragma unroll
         for (int g = 0; g < kPer; ++g) {
             v4u32 part[kSteps][MT][P];
@@ -339,46 +362,36 @@ __global__ __launch_bounds__(256, 2) void group_product_kernel(GroupTilesArgs a)
 #pragma unroll
                 for (int t = 0; t < kSteps; ++t)
 #pragma unroll
-                    for (int q = 0; q < P; ++q) part[t][m][q] = x[m][g * kSteps + t][q][lane];
+                    for (int q = 0; q < P; ++q) part[t][m][q] = in.rows[wk][wm][m][g * kSteps + t][q][lane];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 v4f32 d[MT] = {};
 #pragma unroll
                 for (int t = 0; t < kSteps; ++t) {
-                    const v4u32 b = codes_up<kHalf>(c.w[n][g * kSteps + t]);
+                    const v4u32 b = codes_up<kHalf>(w[n][g * kSteps + t]);
 #pragma unroll
                     for (int q = P - 1; q >= 0; --q)
 #pragma unroll
                         for (int m = 0; m < MT; ++m) d[m] = mfma_16<kHalf>(part[t][m][q], b, d[m]);
                 }
-                const float step = from_bfloat_bits(c.sb[n][g] & 0xFFFFu);
+                const float step = from_bfloat_bits(sb[n][g] & 0xFFFFu);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) acc[m][n][q] = __builtin_fmaf(step, d[m][q], acc[m][n][q]);
-                if constexpr (kPer == 4 && MT == 4) __builtin_amdgcn_sched_barrier(0);    // else more is begun than there are registers for
             }
         }
-    };
-    arrived<0>();
-    for (int trip = 0; trip < trips; trip += 2) {
-        fetch(trip + 1);                                                               // where the trip before this one read, which a barrier ended
-        load_codes(odd, trip + 1);
-        multiply(even, trip);
-        arrived<0>();
-        fetch(trip + 2);
-        load_codes(even, trip + 2);
-        multiply(odd, trip + 1);
-        arrived<0>();
     }
-    if constexpr (WK > 1) {                                                            // (no one reads the rows of a any more)
+    arrived<0>();                                                                      // nothing is on its way to LDS any more
+    if constexpr (WK > 1) {
+        const int at = (wm * WN + wn) * 64 + lane;
         if (wk > 0)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) lds.out[wk - 1][(m * NT + n) * 4 + q][wn * 64 + lane] = acc[m][n][q];
+                    for (int q = 0; q < 4; ++q) lds.out[wk - 1][(m * NT + n) * 4 + q][at] = acc[m][n][q];
         __syncthreads();
         if (wk > 0) return;
 #pragma unroll
@@ -388,7 +401,7 @@ __global__ __launch_bounds__(256, 2) void group_product_kernel(GroupTilesArgs a)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[m][n][q] += lds.out[w][(m * NT + n) * 4 + q][wn * 64 + lane];
+                    for (int q = 0; q < 4; ++q) acc[m][n][q] += lds.out[w][(m * NT + n) * 4 + q][at];
     }
     const auto store = [&](auto* out) {
         using TO = std::remove_pointer_t<decltype(out)>;

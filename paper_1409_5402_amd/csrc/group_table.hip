@@ -17,13 +17,13 @@ namespace {
 constexpr int64_t kRowsOfB = (int64_t)1 << 28;
 int64_t rows_of_a(const same_lda_rows* a)
 {
-    const int64_t most = ((int64_t)1 << 28) / (same::micro_groups(a->width) * 128 * (a->type == SAME_LDA_FLOAT ? 6 : 2)) / 64 * 64;
+    const int64_t most = ((int64_t)1 << 28) / (same::micro_groups(a->width) * 128 * (a->type == SAME_LDA_FLOAT ? 6 : 2)) / 128 * 128;
     return most < 4096 ? 4096 : most > ((int64_t)1 << 24) ? (int64_t)1 << 24 : most;
 }
 
 bool few_rows(const same_lda_rows* a) { return a->rows <= 16 && same::micro_groups(a->width) <= 32; }
 
-// Workspace of the rows of a, laid down for tiles of up to 64 rows and trips of up to 8 blocks, and of their sums.
+// Workspace of the rows of a, laid down for tiles of up to 128 rows and trips of up to 8 blocks, and of their sums.
 struct RowsSpace {
     size_t operands, bytes;
 };
@@ -31,7 +31,7 @@ struct RowsSpace {
 RowsSpace rows_space(const same_lda_rows* a)
 {
     if (few_rows(a)) return {0, 0};
-    const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 63) / 64 * 4), filled = (size_t)((same::micro_groups(a->width) + 7) / 8 * 8);
+    const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 127) / 128 * 8), filled = (size_t)((same::micro_groups(a->width) + 7) / 8 * 8);
     const size_t operands = tiles * filled * 4 * (a->type == SAME_LDA_FLOAT ? 3 : 1) * 1024;
     return {operands, operands + tiles * ((filled * 4 + 31) / 32) * 3 * 1024};
 }
@@ -55,17 +55,17 @@ void product_few_by_width(same::GroupProductArgs& p, int blocks, hipStream_t st)
     else product_few<TI, P, kStack, kGroupLog2, 4>(p, blocks, st);
 }
 
-template <class TI, int kGroupLog2, int MT, int NT, int WK>
+template <class TI, int kGroupLog2, int MT, int NT, int WM, int WN, int WK, int kStages>
 void product_tiles(const same::GroupProductArgs& p, void* operands, void* sums, hipStream_t st)
 {
-    constexpr int P = sizeof(TI) == 4 ? 3 : 1;
-    const int blocks = (p.width + 127) / 128, filled = (blocks + 2 * WK - 1) / (2 * WK) * (2 * WK);
-    const int64_t tiles_a = (p.rows_a + 16 * MT - 1) / (16 * MT);
+    constexpr int P = sizeof(TI) == 4 ? 3 : 1, kTall = 16 * MT * WM, kWide = 16 * NT * WN;
+    const int blocks = (p.width + 127) / 128, filled = (blocks + WK - 1) / WK * WK;
+    const int64_t tiles_a = (p.rows_a + kTall - 1) / kTall, tiles_b = ((p.rows_b + kWide - 1) / kWide + 7) / 8 * 8;
     const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, static_cast<same::v4u32*>(operands), static_cast<uint16_t*>(sums)};
-    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT), (unsigned)at_most((filled + 3) / 4, 65535)), dim3(256), 0, st, rows);
-    const int64_t across = 16 * NT * (4 / WK), tiles_b = ((p.rows_b + across - 1) / across + 7) / 8 * 8;
+    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT * WM), (unsigned)at_most((filled + 3) / 4, 65535)), dim3(256), 0, st, rows);
     const same::GroupTilesArgs tiles = {p, static_cast<const same::v4u32*>(operands), static_cast<const same::v4u32*>(sums), blocks, filled};
-    hipLaunchKernelGGL((same::group_product_kernel<same::kHalfMatrix<TI>, P, kGroupLog2, MT, NT, WK>), dim3((unsigned)(tiles_a * tiles_b)), dim3(256), 0, st, tiles);
+    hipLaunchKernelGGL((same::group_product_kernel<same::kHalfMatrix<TI>, P, kGroupLog2, MT, NT, WM, WN, WK, kStages>), dim3((unsigned)(tiles_a * tiles_b)), dim3(64 * WM * WN * WK), 0, st,
+                       tiles);
 }
 
 template <class TI, int kGroupLog2>
@@ -76,10 +76,11 @@ void product_launch(same::GroupProductArgs& p, bool few, void* operands, void* s
         if constexpr (sizeof(TI) == 4) return p.rows_a <= 4 ? product_few_by_width<TI, 1, true, kGroupLog2>(p, blocks, st) : product_few_by_width<TI, 3, false, kGroupLog2>(p, blocks, st);
         else return product_few_by_width<TI, 1, false, kGroupLog2>(p, blocks, st);
     }
-    constexpr int kTall = sizeof(TI) == 4 ? 2 : 4;                       // of 16 rows of a
-    if (p.rows_a <= 16)      product_tiles<TI, kGroupLog2, 1, 2, 4>(p, operands, sums, st);
-    else if (p.rows_a <= 32) product_tiles<TI, kGroupLog2, 2, 2, sizeof(TI) == 4 ? 2 : 4>(p, operands, sums, st);
-    else                     product_tiles<TI, kGroupLog2, kTall, 4, 1>(p, operands, sums, st);
+    constexpr bool kThree = sizeof(TI) == 4;
+    if (p.rows_a <= 16)      product_tiles<TI, kGroupLog2, 1, 2, 1, 4, 2, 3>(p, operands, sums, st);
+    else if (p.rows_a <= 32) product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 2, kThree ? 2 : 3>(p, operands, sums, st);
+    else if (p.rows_a <= 64) product_tiles<TI, kGroupLog2, kThree ? 2 : 4, 2, kThree ? 2 : 1, kThree ? 4 : 8, 1, kThree ? 2 : 4>(p, operands, sums, st);
+    else                     product_tiles<TI, kGroupLog2, kThree ? 2 : 4, 4, 2, 4, 1, kThree ? 2 : 3>(p, operands, sums, st);
 }
 
 template <class TI>

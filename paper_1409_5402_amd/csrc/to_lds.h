@@ -22,6 +22,13 @@ __device__ __forceinline__ void to_lds_4(const uint8_t* base, uint32_t offset, c
     asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0" : "=&s"(copy) : "s"(at), "v"(offset), "s"(base) : "m0");
 }
 
+// An address that is the same for the whole wave, in scalar registers wherever it was computed.
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p)
+{
+    const uint64_t at = (uint64_t)(uintptr_t)p;
+    return (const uint8_t*)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at));
+}
+
 // All of this wave's loads but the last N have come (they end in their order), then all waves'.
 template <int N>
 __device__ __forceinline__ void arrived()
