@@ -118,6 +118,29 @@ __device__ __forceinline__ void store_number(const GroupProductArgs& p, int64_t 
     else                      static_cast<_Float16*>(p.out)[at] = (_Float16)x;
 }
 
+struct Numbers {
+    v4f32 lo, hi;
+};
+
+// Up to eight numbers of row i from column j on (none where count is not positive).
+__device__ __forceinline__ void store_numbers(const GroupProductArgs& p, int64_t i, int64_t j, Numbers x, int count)
+{
+    const int64_t at = i * p.out_stride + j;
+    if (count >= 8) {
+        const float y[8] = {x.lo[0], x.lo[1], x.lo[2], x.lo[3], x.hi[0], x.hi[1], x.hi[2], x.hi[3]};
+        if (p.type_out == 0)      store_eight(static_cast<float*>(p.out) + at, y, 8);
+        else if (p.type_out == 1) store_eight(static_cast<__bf16*>(p.out) + at, y, 8);
+        else                      store_eight(static_cast<_Float16*>(p.out) + at, y, 8);
+    } else {
+#pragma unroll 1
+        for (int e = 0; e < count; ++e) {
+            store_number(p, i, j + e, x.lo[0]);
+            x.lo = {x.lo[1], x.lo[2], x.lo[3], x.hi[0]};
+            x.hi = {x.hi[1], x.hi[2], x.hi[3], 0.0f};
+        }
+    }
+}
+
 // What the matrix instruction takes: bfloat16 for rows in bfloat16 and binary32, binary16 for rows in that.
 template <class TI>
 constexpr bool kHalfMatrix = __is_same(TI, _Float16);
@@ -205,9 +228,10 @@ __global__ __launch_bounds__(256) void group_rows_kernel(GroupRowsArgs a)
     const TI* const row = static_cast<const TI*>(a.a) + i * a.stride_a;
     const int sets = (a.blocks + kAll - 1) / kAll, most = a.filled > sets * kAll ? a.filled : sets * kAll;
     for (int k = blockIdx.y * 4 + (threadIdx.x >> 6); k < most; k += gridDim.y * 4) {
-        Eight<TI> raw[4];
+        Eight<TI> raw[4] = {};
+        if (k < a.blocks)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) raw[t] = eight_at(row, k * 128 + 32 * t + 8 * h, a.width);
+            for (int t = 0; t < 4; ++t) raw[t] = eight_at(row, k * 128 + 32 * t + 8 * h, a.width);
         v4f32 total[kPer] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -254,7 +278,7 @@ struct GroupStage {
 };
 
 template <bool kHalf, int P, int kGroupLog2, int MT, int NT, int WM, int WN, int WK, int kStages>
-__global__ __launch_bounds__(64 * WM * WN * WK, 2) void group_product_kernel(GroupTilesArgs a)
+__global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, kGroupLog2, MT, NT, WM, WN, WK>) * 3 <= 163840 && WM * WN * WK == 4 ? 3 : 2) void group_product_kernel(GroupTilesArgs a)
 {
     constexpr int kPer = 128 >> kGroupLog2, kSteps = 4 / kPer, kAll = 32 / kPer;       // groups of a block, instructions per group, blocks of a set
     constexpr int kWaves = WM * WN * WK;
@@ -262,6 +286,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void group_product_kernel(Gro
     __shared__ union {
         Stage in[kStages];
         float out[WK > 1 ? WK - 1 : 1][WK > 1 ? MT * NT * 4 : 1][WK > 1 ? 64 * WM * WN : 1];
+        float strip[WM * WN][16 * MT][16 * NT + 4];
     } lds;
     const GroupProductArgs& p = a.p;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
@@ -281,7 +306,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void group_product_kernel(Gro
     constexpr int kEach = kRowsEach + kCodesEach + kWordsEach;
     const uint8_t* const rows = reinterpret_cast<const uint8_t*>(a.operands + first_i / 16 * a.filled * (4 * P) * 64);
     const uint8_t* const codes = p.codes + first_j * p.pitch;
-    const uint8_t* const scales = p.scales + first_j * p.scale_pitch;
+    const uint8_t* const words = p.scales + first_j * p.scale_pitch;
     uint32_t code_at[kCodesEach], word_at[kWordsEach];                                 // of this lane, in the tile's rows of b
 #pragma unroll
     for (int f = 0; f < kCodesEach; ++f) {
@@ -309,23 +334,23 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void group_product_kernel(Gro
 #pragma unroll
         for (int f = 0; f < kWordsEach; ++f) {
             const int e = min((f * kWaves + wv) * 64, kWords - 64), k = min(t * WK + e / (kWide * kPer), a.blocks - 1);
-            to_lds_4(uniform(scales + (int64_t)k * (4 * kPer)), word_at[f], &to.scales[0][0][0][0][0] + e);
+            to_lds_4(uniform(words + (int64_t)k * (4 * kPer)), word_at[f], &to.scales[0][0][0][0][0] + e);
         }
     };
     static_assert(kWide * kPer % 64 == 0, "a piece of scales is of one block");
 #pragma unroll
-    for (int s = 0; s + 1 < kStages; ++s) fetch(s);
+    for (int f = 0; f + 1 < kStages; ++f) fetch(f);
 
-    // sum_g b_g S_g to begin with, by the first of the waves that share a row
+    // sum_g b_g S_g to begin with, by the first of the waves that share a row: 32 groups at a time
     v4f32 acc[MT][NT] = {};
-    if (wk == 0) {
-        const int sets = (a.blocks + kAll - 1) / kAll, groups = a.blocks * kPer;
+    const int sets = (a.blocks + kAll - 1) / kAll, groups = a.blocks * kPer;
+    if (wk == 0)
+#pragma unroll 1
         for (int e = 0; e < sets; ++e) {
             v4u32 b[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const int64_t j = j0 + 16 * n + r < p.rows_b ? j0 + 16 * n + r : p.rows_b - 1;
-                const uint32_t* const of = reinterpret_cast<const uint32_t*>(p.scales + j * p.scale_pitch);
+                const uint32_t* const of = reinterpret_cast<const uint32_t*>(words + (int64_t)min(wn * (16 * NT) + 16 * n + r, last) * p.scale_pitch);
                 uint32_t sb[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) sb[q] = of[min(e * 32 + 8 * h + q, groups - 1)];      // groups behind the last: it, times zero
@@ -341,7 +366,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void group_product_kernel(Gro
                     for (int n = 0; n < NT; ++n) acc[m][n] = mfma_16<false>(s, b[n], acc[m][n]);
                 }
         }
-    }
+#pragma unroll 1
     for (int trip = 0; trip < trips; ++trip) {
         arrived<(kStages - 2) * kEach>();
         fetch(trip + kStages - 1);                                                     // where the trip before this one read, which this barrier ended
@@ -393,32 +418,34 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void group_product_kernel(Gro
 #pragma unroll
                     for (int q = 0; q < 4; ++q) lds.out[wk - 1][(m * NT + n) * 4 + q][at] = acc[m][n][q];
         __syncthreads();
+        if (wk == 0)
+#pragma unroll
+            for (int w = 0; w + 1 < WK; ++w)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[m][n][q] += lds.out[w][(m * NT + n) * 4 + q][at];
+        __syncthreads();
         if (wk > 0) return;
-#pragma unroll
-        for (int w = 0; w + 1 < WK; ++w)
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[m][n][q] += lds.out[w][(m * NT + n) * 4 + q][at];
     }
-    const auto store = [&](auto* out) {
-        using TO = std::remove_pointer_t<decltype(out)>;
+    // by way of LDS, so that a lane stores eight numbers of one row
+    auto& strip = lds.strip[wm * WN + wn];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t i = i0 + 16 * m + 4 * h + q;
-                TO* const row = out + i * p.out_stride + j0 + r;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    if (i < p.rows_a && j0 + 16 * n + r < p.rows_b) row[16 * n] = (TO)(p.scale * acc[m][n][q]);
-            }
-    };
-    if (p.type_out == 0)      store(static_cast<float*>(p.out));
-    else if (p.type_out == 1) store(static_cast<__bf16*>(p.out));
-    else                      store(static_cast<_Float16*>(p.out));
+            for (int q = 0; q < 4; ++q) strip[16 * m + 4 * h + q][16 * n + r] = p.scale * acc[m][n][q];
+    asm volatile("" ::: "memory");                                                     // a wave's accesses to LDS are done in their order
+    const int col = lane % (2 * NT) * 8, count = p.rows_b - (j0 + col) < 8 ? (int)(p.rows_b - (j0 + col)) : 8;
+    const int rows_here = p.rows_a - i0 < 16 * MT ? (int)(p.rows_a - i0) : 16 * MT;
+#pragma unroll 1
+    for (int row = lane / (2 * NT); row < rows_here; row += 32 / NT) {
+        const v4f32 lo = *reinterpret_cast<const v4f32*>(&strip[row][col]), hi = *reinterpret_cast<const v4f32*>(&strip[row][col + 4]);
+        store_numbers(p, i0 + row, j0 + col, {lo, hi}, count);
+    }
 }
 
 // Few rows of a, up to 16.  A wave keeps its part of them, KB blocks of 128 elements, in registers and goes through the rows of b, 16 at

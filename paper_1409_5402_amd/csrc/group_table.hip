@@ -62,7 +62,7 @@ void product_tiles(const same::GroupProductArgs& p, void* operands, void* sums, 
     const int blocks = (p.width + 127) / 128, filled = (blocks + WK - 1) / WK * WK;
     const int64_t tiles_a = (p.rows_a + kTall - 1) / kTall, tiles_b = ((p.rows_b + kWide - 1) / kWide + 7) / 8 * 8;
     const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, static_cast<same::v4u32*>(operands), static_cast<uint16_t*>(sums)};
-    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT * WM), (unsigned)at_most((filled + 3) / 4, 65535)), dim3(256), 0, st, rows);
+    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT * WM), (unsigned)at_most(((filled > blocks + 31 ? filled : blocks + 31) + 3) / 4, 65535)), dim3(256), 0, st, rows);
     const same::GroupTilesArgs tiles = {p, static_cast<const same::v4u32*>(operands), static_cast<const same::v4u32*>(sums), blocks, filled};
     hipLaunchKernelGGL((same::group_product_kernel<same::kHalfMatrix<TI>, P, kGroupLog2, MT, NT, WM, WN, WK, kStages>), dim3((unsigned)(tiles_a * tiles_b)), dim3(64 * WM * WN * WK), 0, st,
                        tiles);
@@ -76,11 +76,20 @@ void product_launch(same::GroupProductArgs& p, bool few, void* operands, void* s
         if constexpr (sizeof(TI) == 4) return p.rows_a <= 4 ? product_few_by_width<TI, 1, true, kGroupLog2>(p, blocks, st) : product_few_by_width<TI, 3, false, kGroupLog2>(p, blocks, st);
         else return product_few_by_width<TI, 1, false, kGroupLog2>(p, blocks, st);
     }
-    constexpr bool kThree = sizeof(TI) == 4;
-    if (p.rows_a <= 16)      product_tiles<TI, kGroupLog2, 1, 2, 1, 4, 2, 3>(p, operands, sums, st);
-    else if (p.rows_a <= 32) product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 2, kThree ? 2 : 3>(p, operands, sums, st);
-    else if (p.rows_a <= 64) product_tiles<TI, kGroupLog2, kThree ? 2 : 4, 2, kThree ? 2 : 1, kThree ? 4 : 8, 1, kThree ? 2 : 4>(p, operands, sums, st);
-    else                     product_tiles<TI, kGroupLog2, kThree ? 2 : 4, 4, 2, 4, 1, kThree ? 2 : 3>(p, operands, sums, st);
+    // us of the two launches, in the order of the forms below (rows of a x rows of b x width; G128, 16-bit)
+    const auto tiles = [&](int64_t tall, int64_t wide) { return ((p.rows_a + tall - 1) / tall) * ((p.rows_b + wide - 1) / wide); };
+    if constexpr (sizeof(TI) == 4) {
+        if (p.rows_a > 32 && tiles(64, 256) >= 512)      product_tiles<TI, kGroupLog2, 2, 4, 2, 4, 1, 2>(p, operands, sums, st);
+        else if (p.rows_a > 16 && tiles(32, 128) >= 384) product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 2>(p, operands, sums, st);
+        else                                             product_tiles<TI, kGroupLog2, 1, 2, 1, 2, 4, 2>(p, operands, sums, st);
+    } else {
+        if (p.rows_a > 32 && tiles(64, 256) >= 1536)     product_tiles<TI, kGroupLog2, 4, 4, 1, 4, 1, 2>(p, operands, sums, st);
+        else if (p.rows_a > 32 && tiles(64, 128) >= 384) product_tiles<TI, kGroupLog2, 4, 2, 1, 4, 1, 2>(p, operands, sums, st);
+        else if (p.rows_a > 32 && tiles(64, 64) >= 192)  product_tiles<TI, kGroupLog2, 4, 2, 1, 2, 2, 3>(p, operands, sums, st);
+        else if (p.rows_a > 16 && tiles(32, 128) >= 256) product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 4>(p, operands, sums, st);
+        else if (p.rows_a > 16)                          product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 4, 3>(p, operands, sums, st);
+        else                                             product_tiles<TI, kGroupLog2, 1, 2, 1, 4, 1, 4>(p, operands, sums, st);
+    }
 }
 
 template <class TI>

@@ -227,6 +227,24 @@ def test_product_of_few_rows_of_every_length(K, M, dtype):
         product_case(np.random.default_rng(K + M), M, N, K, dtype, group, "f32")
 
 
+@pytest.mark.parametrize("dtype, group", [("f32", 64), ("bf16", 32), ("f16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("M, N, K", [(520, 49_200, 130), (65, 25_000, 200), (40, 6400, 300), (33, 700, 1100), (20, 33_000, 260), (20, 600, 520), (7, 300, 4300), (130, 99_000, 70)])
+def test_product_in_every_form(M, N, K, dtype, group):
+    """Tiles of every size, which the numbers of rows choose: against the product in double on the device, at its bound."""
+    rng = np.random.default_rng(M)
+    x = numbers_of(rng, M, K, TYPES[dtype]).to(DEV)
+    q = binding.group_quantize(torch.randn(N, K, device=DEV, generator=torch.Generator(device=DEV).manual_seed(K)), group)
+    want = x.double() @ binding.group_dequantize(q).double().t().contiguous()
+    A = torch.nn.functional.pad(x.abs().double(), (0, q.scales.shape[1] * group - K)).view(M, -1, group).sum(2)
+    size = A @ (15.0 * q.scales[:, :, 0].abs().double() + q.scales[:, :, 1].abs().double()).t().contiguous()
+    n = group * (3 if dtype == "f32" else 1)
+    bound = 1.01 * (2 * n + 3 + 2 * q.scales.shape[1]) * U * size + 2.01 * U * want.abs()
+    got, check = guarded(M, N, torch.float32, N + 1, 1)
+    binding.group_product(x, q, out=got)
+    assert ((got.double() - want).abs() <= bound).all()
+    check()
+
+
 @pytest.mark.parametrize("M, N, K", [(1, 100, 700), (4, 90, 384), (7, 130, 1100), (16, 257, 4224), (33, 200, 900), (200, 300, 640)])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("group", GROUPS)
