@@ -324,8 +324,11 @@ int same_lda_dropout(const same_lda_rows* x, const same_lda_drop* drop, const sa
 int same_lda_embed_dropout(const same_lda_rows* table, const void* tokens, int32_t token_bytes, float scale, const same_lda_drop* drop,
                            const same_lda_rows* out, void* hip_stream);
 
-/* The gradient of same_lda_embed_dropout with respect to the table: same_lda_embed_grad (its workspace, its order of
- * additions) of the elements of grad that the lookup kept, with scale / (1 - p).  What dropped elements hold does not count. */
+/* The gradient of same_lda_embed_dropout with respect to the table: same_lda_embed_grad of the elements of grad that the lookup
+ * kept, with scale / (1 - p).  What dropped elements hold does not count.  Equal numbers give equal bits as there, but the number of tokens
+ * from which on they are sorted, and with it the order of additions, may be another.
+ *   workspace    as many bytes as same_lda_embed_dropout_grad_workspace says, otherwise as there                      */
+int same_lda_embed_dropout_grad_workspace(const same_lda_rows* grad, const same_lda_rows* table_grad, size_t* bytes);
 int same_lda_embed_dropout_grad(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale, const same_lda_drop* drop,
                                 int32_t accumulate, const same_lda_rows* table_grad, void* workspace, size_t workspace_bytes,
                                 void* hip_stream);

@@ -26,7 +26,7 @@ _DTYPES = {THETA: np.float32, PHI: np.float32, NDK: np.uint32, NWK: np.uint32, N
 EXPORTS = ["same_lda_init", "same_lda_sweep", "same_lda_sweep_poisson", "same_lda_sweep_sampled", "same_lda_loglik", "same_lda_free",
            "same_lda_set_batch", "same_lda_stage_batch", "same_lda_commit_batch", "same_lda_debug_draw_poisson", "same_lda_sddmm",
            "same_lda_vb_exp_elog_beta", "same_lda_vb_estep",
-           "same_lda_embed", "same_lda_embed_grad_workspace", "same_lda_embed_grad", "same_lda_dropout", "same_lda_embed_dropout", "same_lda_embed_dropout_grad",
+           "same_lda_embed", "same_lda_embed_grad_workspace", "same_lda_embed_grad", "same_lda_dropout", "same_lda_embed_dropout", "same_lda_embed_dropout_grad_workspace", "same_lda_embed_dropout_grad",
            "same_lda_group_size", "same_lda_group_quantize", "same_lda_group_product_workspace", "same_lda_group_product", "same_lda_micro_size", "same_lda_micro_quantize", "same_lda_micro_product",
            "same_lda_get", "same_lda_set", "same_lda_get_pass", "same_lda_set_pass", "same_lda_task_count",
            "same_lda_debug_draw", "same_lda_debug_draw_noalloc", "same_lda_debug_chunk_limit", "same_lda_set_timing", "same_lda_get_timing", "same_lda_selftest",
@@ -90,6 +90,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
         L.same_lda_embed_grad.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
         L.same_lda_dropout.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
         L.same_lda_embed_dropout.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_void_p, c_void_p, c_void_p]
+        L.same_lda_embed_dropout_grad_workspace.argtypes = [c_void_p, c_void_p, POINTER(c_size_t)]
         L.same_lda_embed_dropout_grad.argtypes = [c_void_p, c_void_p, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
         L.same_lda_group_size.argtypes = [c_int64, c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
         L.same_lda_group_quantize.argtypes = [c_void_p, c_void_p, c_void_p]
@@ -621,7 +622,7 @@ def embed_grad(grad, tokens, rows=None, scale=1.0, dtype=None, out=None, accumul
     flat, g = _flat_rows(grad, ids.numel(), width)
     out, o = _output(out, (rows, width), rows, width, dtype, grad.dtype, ids.device)
     n = c_size_t()
-    if _library.same_lda_embed_grad_workspace(g, o, byref(n)):
+    if (_library.same_lda_embed_grad_workspace if drop is None else _library.same_lda_embed_dropout_grad_workspace)(g, o, byref(n)):
         raise SameLdaError(-1, _library.same_lda_last_error(None).decode())
     space = _torch.empty(n.value, dtype=_torch.uint8, device=ids.device) if n.value else None
     t, at = ids.data_ptr() if ids.numel() else _EMPTY, space.data_ptr() if n.value else None

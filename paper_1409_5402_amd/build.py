@@ -6,7 +6,9 @@ import subprocess
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = [os.path.join(HERE, "csrc", name) for name in ("same_lda.hip", "word_table.hip", "embed_grad.hip", "embed_grad_dropout.hip", "word_rows.hip", "group_table.hip")]
+SRC = [os.path.join(HERE, "csrc", name) for name in ("same_lda.hip", "word_table.hip", "embed_grad.hip", "embed_grad_dropout_float.hip",
+                                                     "embed_grad_dropout_bfloat.hip", "embed_grad_dropout_half.hip", "word_rows.hip",
+                                                     "group_table.hip")]
 LIB = os.path.join(HERE, "libsame_lda.so")
 
 # -ffp-contract=off: every binary32 step of the draw is rounded once (no fused multiply-add);

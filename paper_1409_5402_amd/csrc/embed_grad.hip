@@ -34,18 +34,23 @@ constexpr int64_t kSmallTiles = 1 << 22;                             // up to th
 //                         128 89, 80; 400,000 x 192 116, 129; a million x 16 143, 61)
 // and a grid below 2^32 threads: 1024 for every 256 words begun, and every 64 chunks of a row.
 constexpr int64_t kScannedWords = 1 << 18;
-bool few_tokens(int64_t n, int64_t rows, const same_lda_rows* grad)
+// With dropout the workgroup of a frequent word has the choice for all its rows to make as well, so only up to 4096 tokens go in one launch, and
+// up to 8192 where rows are short or words are many (us, sorted after it: 4096 into 30,000 x 1024 bf16 56, 64, 8192 88, 71; 4000 into 2000 x 128
+// f32 45, 49, 8000 75, 51; 8000 into 2000 x 50 f32 35, 42, 16,000 48, 44; 8000 into 100,000 x 256 f16 54, 76, 16,000 86, 77).
+constexpr int64_t kDroppedTokens = 4096, kDroppedShort = 64;
+bool few_tokens(int64_t n, int64_t rows, const same_lda_rows* grad, bool drop)
 {
+    if (drop && n > kDroppedTokens && (n > kFewerTokens || (grad->width > kDroppedShort && rows <= 4 * n))) return false;
     const int64_t row_bytes = (int64_t)grad->width * element_bytes(grad->type);
     const bool more = row_bytes <= 2048 && (rows <= kScannedWords || row_bytes > 512);
     return n <= (more ? same::kFewTokens : kFewerTokens) && (rows + 256) * ((grad->width + 63) / 64) < (int64_t)1 << 30;
 }
 
-GradSpace grad_space(const same_lda_rows* grad, int64_t rows)
+GradSpace grad_space(const same_lda_rows* grad, int64_t rows, bool drop)
 {
     const int64_t n = grad->rows, width = grad->width;
     GradSpace s = {};
-    if (n == 0 || few_tokens(n, rows, grad)) return s;
+    if (n == 0 || few_tokens(n, rows, grad, drop)) return s;
     size_t at = 0;
     const auto part = [&at](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     int bits = 1;
@@ -87,6 +92,15 @@ int check_grad(const same_lda_rows* grad, const same_lda_rows* table_grad)
     return rc;
 }
 
+int workspace_of(const same_lda_rows* grad, const same_lda_rows* table_grad, bool drop, size_t* bytes)
+{
+    if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: bytes is null");
+    const int rc = check_grad(grad, table_grad);
+    if (rc) return rc;
+    *bytes = grad_space(grad, table_grad->rows, drop).bytes;
+    return SAME_LDA_OK;
+}
+
 // `drop`: that of the lookup, or null
 int grad_call(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale, const same::Drop* drop, int32_t accumulate,
               const same_lda_rows* table_grad, void* workspace, size_t workspace_bytes, void* hip_stream)
@@ -97,7 +111,7 @@ int grad_call(const same_lda_rows* grad, const void* tokens, int32_t token_bytes
     if (!tokens && grad->rows > 0) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: tokens is null");
     if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: the scale must be finite");
     const int64_t n = grad->rows, rows = table_grad->rows;
-    const GradSpace s = grad_space(grad, rows);
+    const GradSpace s = grad_space(grad, rows, drop);
     if (rows == 0 || (n == 0 && accumulate)) return SAME_LDA_OK;
     if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes || (uintptr_t)workspace % 16))
         return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: needs %zu bytes of workspace aligned to 16 (got %zu)", s.bytes, workspace ? workspace_bytes : (size_t)0);
@@ -106,7 +120,7 @@ int grad_call(const same_lda_rows* grad, const void* tokens, int32_t token_bytes
     char* const w = static_cast<char*>(workspace);
     same::GradArgs a = {grad->data, grad->stride, nullptr, nullptr, rows, scale, accumulate, table_grad->data, table_grad->stride,
                         nullptr, s.ranges, grad->width, 0, 0, {tokens, token_bytes == 8}, (int32_t)n, 0, 0, drop ? *drop : same::Drop{}};
-    if (!few_tokens(n, rows, grad)) {
+    if (!few_tokens(n, rows, grad, drop)) {
         uint32_t* const hist = reinterpret_cast<uint32_t*>(w + s.hist);
         uint32_t* const total = reinterpret_cast<uint32_t*>(w + s.total);
         int32_t* const start = reinterpret_cast<int32_t*>(w + s.start);
@@ -122,20 +136,22 @@ int grad_call(const same_lda_rows* grad, const void* tokens, int32_t token_bytes
         a.start = start;
         a.partial = reinterpret_cast<float*>(w + s.partial);
     }
-    return drop ? grad_sums_dropout(a, grad, table_grad, st) : grad_sums<false>(a, grad, table_grad, st);
+    switch (grad->type) {
+        case SAME_LDA_FLOAT:  return drop ? grad_sums_dropout_float(a, grad, table_grad, st) : grad_to<float, false>(a, grad, table_grad, st);
+        case SAME_LDA_BFLOAT: return drop ? grad_sums_dropout_bfloat(a, grad, table_grad, st) : grad_to<__bf16, false>(a, grad, table_grad, st);
+        default:              return drop ? grad_sums_dropout_half(a, grad, table_grad, st) : grad_to<_Float16, false>(a, grad, table_grad, st);
+    }
 }
 
 }  // namespace
 
 extern "C" {
 
-int same_lda_embed_grad_workspace(const same_lda_rows* grad, const same_lda_rows* table_grad, size_t* bytes)
+int same_lda_embed_grad_workspace(const same_lda_rows* grad, const same_lda_rows* table_grad, size_t* bytes) { return workspace_of(grad, table_grad, false, bytes); }
+
+int same_lda_embed_dropout_grad_workspace(const same_lda_rows* grad, const same_lda_rows* table_grad, size_t* bytes)
 {
-    if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: bytes is null");
-    const int rc = check_grad(grad, table_grad);
-    if (rc) return rc;
-    *bytes = grad_space(grad, table_grad->rows).bytes;
-    return SAME_LDA_OK;
+    return workspace_of(grad, table_grad, true, bytes);
 }
 
 int same_lda_embed_grad(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale, int32_t accumulate,

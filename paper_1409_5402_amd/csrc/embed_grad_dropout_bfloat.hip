@@ -1,0 +1,6 @@
+#include "embed_grad_launch.h"
+
+int same::host::grad_sums_dropout_bfloat(GradArgs& a, const same_lda_rows* grad, const same_lda_rows* table_grad, hipStream_t st)
+{
+    return grad_to<__bf16, true>(a, grad, table_grad, st);
+}

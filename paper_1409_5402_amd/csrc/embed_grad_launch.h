@@ -62,18 +62,10 @@ int grad_to(GradArgs& a, const same_lda_rows* grad, const same_lda_rows* out, hi
     }
 }
 
-// The sums of a lookup with dropout.
-__attribute__((visibility("hidden"))) int grad_sums_dropout(GradArgs& a, const same_lda_rows* grad, const same_lda_rows* table_grad, hipStream_t st);
-
-template <bool kDrop>
-int grad_sums(GradArgs& a, const same_lda_rows* grad, const same_lda_rows* table_grad, hipStream_t st)
-{
-    switch (grad->type) {
-        case SAME_LDA_FLOAT:  return grad_to<float, kDrop>(a, grad, table_grad, st);
-        case SAME_LDA_BFLOAT: return grad_to<__bf16, kDrop>(a, grad, table_grad, st);
-        default:              return grad_to<_Float16, kDrop>(a, grad, table_grad, st);
-    }
-}
+// The sums for gradients of one type after a lookup with dropout: a source each, they take longest to compile.
+__attribute__((visibility("hidden"))) int grad_sums_dropout_float(GradArgs& a, const same_lda_rows* grad, const same_lda_rows* table_grad, hipStream_t st);
+__attribute__((visibility("hidden"))) int grad_sums_dropout_bfloat(GradArgs& a, const same_lda_rows* grad, const same_lda_rows* table_grad, hipStream_t st);
+__attribute__((visibility("hidden"))) int grad_sums_dropout_half(GradArgs& a, const same_lda_rows* grad, const same_lda_rows* table_grad, hipStream_t st);
 
 }  // namespace host
 }  // namespace same

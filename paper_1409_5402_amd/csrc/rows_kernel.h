@@ -25,6 +25,7 @@ struct RowsArgs {
     int64_t out_stride;
     int32_t width, chunks;   // chunks of 8 elements of a row, the last one may be cut
     float inverse;           // of chunks
+    int32_t step_rows, step_chunks;   // what all workgroups take at once, kChunksAtOnce each, in rows and chunks
     Drop drop;
 };
 
@@ -35,7 +36,7 @@ struct GroupCode {};         // in grouped four-bit integers
 template <class TI>
 struct Piece {
     Eight<TI> c;
-    __device__ __forceinline__ void load(const RowsArgs& a, int64_t t, int chunk) { c = eight_at(static_cast<const TI*>(a.table) + t * a.stride, chunk * 8, a.width); }
+    __device__ __forceinline__ void load(const RowsArgs& a, int32_t t, int chunk) { c = eight_at(static_cast<const TI*>(a.table) + (int64_t)t * a.stride, chunk * 8, a.width); }
     __device__ __forceinline__ void numbers(float (&x)[8], const RowsArgs& a, int chunk)
     {
         cut_eight(c, chunk * 8, a.width);
@@ -47,9 +48,9 @@ struct Piece {
 template <>
 struct Piece<MicroCode> {
     float x[8];
-    __device__ __forceinline__ void load(const RowsArgs& a, int64_t t, int chunk)
+    __device__ __forceinline__ void load(const RowsArgs& a, int32_t t, int chunk)
     {
-        load_micro<8>(x, static_cast<const uint8_t*>(a.table) + t * a.stride, a.scales + t * (a.stride / 16), chunk * 8);
+        load_micro<8>(x, static_cast<const uint8_t*>(a.table) + (int64_t)t * a.stride, a.scales + (int64_t)t * (a.stride / 16), chunk * 8);
     }
     __device__ __forceinline__ void numbers(float (&y)[8], const RowsArgs&, int)
     {
@@ -61,51 +62,94 @@ struct Piece<MicroCode> {
 template <>
 struct Piece<GroupCode> {
     uint32_t word, sb;
-    __device__ __forceinline__ void load(const RowsArgs& a, int64_t t, int chunk)
+    __device__ __forceinline__ void load(const RowsArgs& a, int32_t t, int chunk)
     {
-        word = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.table) + t * a.stride)[group_word(chunk)];
-        sb = reinterpret_cast<const uint32_t*>(a.scales + t * a.scale_pitch)[chunk >> (a.group_log2 - 3)];
+        word = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.table) + (int64_t)t * a.stride)[group_word(chunk)];
+        sb = reinterpret_cast<const uint32_t*>(a.scales + (int64_t)t * a.scale_pitch)[chunk >> (a.group_log2 - 3)];
     }
     __device__ __forceinline__ void numbers(float (&x)[8], const RowsArgs&, int) { grouped_numbers(x, word, sb); }
 };
 
-// Memory bound.  A thread takes kMany chunks: their tokens, their rows and, while these are on their way, what is kept of them.
+// A thread takes kMany chunks at a time: their tokens, their rows and, while these are on their way, what is kept of them.  Bound by memory
+// without dropout, with it by the generator as well (some 70 instructions for eight elements).
+constexpr int kMany = 2, kChunksAtOnce = 256 * kMany;
+
 template <class TI, class TO, bool kDrop>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a)
 {
-    constexpr int kMany = 2;
     DropKey key = {};
     if constexpr (kDrop) key = drop_key(a.drop);
-    const int64_t all = a.n * a.chunks;
-    for (int64_t base = (int64_t)blockIdx.x * (256 * kMany); base < all; base += (int64_t)gridDim.x * (256 * kMany)) {
-        const int64_t row0 = base / a.chunks;                    // of the workgroup; a lane's own by a short division
-        const int c0 = (int)(base - row0 * a.chunks);
+    const int64_t begin = (int64_t)blockIdx.x * kChunksAtOnce;
+    uint32_t row0 = (uint32_t)(begin / a.chunks);                // of the workgroup; a lane's own by a short division
+    int c0 = (int)(begin - (int64_t)row0 * a.chunks);
+    const uint32_t n = (uint32_t)a.n, rows = (uint32_t)a.rows;   // below 2^31
+    while (row0 < n) {
         Piece<TI> piece[kMany] = {};
-        int64_t row[kMany], t[kMany];
+        uint32_t row[kMany], kept[kMany][4];
+        int32_t t[kMany];
         int chunk[kMany];
-        uint32_t kept[kMany];
 #pragma unroll
         for (int q = 0; q < kMany; ++q) {
             const int off = c0 + q * 256 + (int)threadIdx.x;     // below 2^17 + 512: the quotient is exact
             const int down = (int)(((float)off + 0.5f) * a.inverse);
-            row[q] = row0 + down;
+            row[q] = row0 + (uint32_t)down;
             chunk[q] = off - down * a.chunks;
-            t[q] = a.tokens.at(row[q] < a.n ? row[q] : a.n - 1);
+            t[q] = (int32_t)min(row[q], n - 1u);
         }
-        if (a.rows > 0)
+        if (a.tokens.ids) {                                      // all of them on their way at once
+            if (a.tokens.wide) {
+                int64_t id[kMany];
 #pragma unroll
-            for (int q = 0; q < kMany; ++q) piece[q].load(a, t[q] >= 0 && t[q] < a.rows ? t[q] : 0, chunk[q]);     // padding: the first row, not used
+                for (int q = 0; q < kMany; ++q) id[q] = static_cast<const int64_t*>(a.tokens.ids)[t[q]];
 #pragma unroll
-        for (int q = 0; q < kMany; ++q) kept[q] = kDrop ? kept_eight(key, (uint32_t)chunk[q], (uint32_t)row[q]) : 0xFFu;
+                for (int q = 0; q < kMany; ++q) t[q] = id[q] >= 0 && id[q] < a.rows ? (int32_t)id[q] : -1;
+            } else {
+                int32_t id[kMany];
+#pragma unroll
+                for (int q = 0; q < kMany; ++q) id[q] = static_cast<const int32_t*>(a.tokens.ids)[t[q]];
+#pragma unroll
+                for (int q = 0; q < kMany; ++q) t[q] = (uint32_t)id[q] < rows ? id[q] : -1;
+            }
+        }
+        if (rows > 0)
+#pragma unroll
+            for (int q = 0; q < kMany; ++q) piece[q].load(a, max(t[q], 0), chunk[q]);          // padding: the first row, not used
+#pragma unroll
+        for (int q = 0; q < kMany; ++q)
+            if constexpr (kDrop) kept_halves(kept[q], key, (uint32_t)chunk[q], row[q]);
 #pragma unroll
         for (int q = 0; q < kMany; ++q) {
-            if (row[q] >= a.n) continue;
+            if (row[q] >= n) continue;
             float x[8];
             piece[q].numbers(x, a, chunk[q]);
-            const uint32_t used = t[q] >= 0 && t[q] < a.rows ? kept[q] : 0u;
+            const uint32_t known = t[q] >= 0 ? ~0u : 0u;
+            Eight<TO> out;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = used >> j & 1u ? x[j] * a.factor : 0.0f;
-            store_eight<TO>(static_cast<TO*>(a.out) + row[q] * a.out_stride + (int64_t)chunk[q] * 8, x, a.width - chunk[q] * 8);
+            for (int j = 0; j < 8; ++j) out.v[j] = (TO)(x[j] * a.factor);
+            uint32_t w[sizeof(TO) * 2];
+            __builtin_memcpy(w, out.v, sizeof w);
+#pragma unroll
+            for (int j = 0; j < (int)(sizeof(TO) * 2); ++j) {                  // two elements a word, or one
+                uint32_t mask = known;
+                if constexpr (kDrop) mask &= sizeof(TO) == 2 ? kept[q][j & 3] : (uint32_t)((int32_t)(j & 1 ? kept[q][j / 2] : kept[q][j / 2] << 16) >> 16);
+                w[j] &= mask;
+            }
+            __builtin_memcpy(out.v, w, sizeof w);
+            TO* const to = static_cast<TO*>(a.out) + (int64_t)row[q] * a.out_stride + chunk[q] * 8;
+            const int count = a.width - chunk[q] * 8;
+            if (count >= 8) {
+                out.store(to);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < count) to[j] = out.v[j];
+            }
+        }
+        row0 += (uint32_t)a.step_rows;
+        c0 += a.step_chunks;
+        if (c0 >= a.chunks) {
+            c0 -= a.chunks;
+            ++row0;
         }
     }
 }

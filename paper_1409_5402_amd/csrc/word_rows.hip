@@ -21,24 +21,30 @@ int check_drop(const char* call, const same_lda_drop* drop, float* scale, Drop* 
     if (!std::isfinite((float)factor)) return fail_without_handle(SAME_LDA_EINVAL, "%s: the scale %g / (1 - %g) is beyond binary32", call, (double)*scale, drop->p);
     const uint64_t border = (uint64_t)keep;
     *scale = (float)factor;
-    *d = {(uint32_t)drop->seed, (uint32_t)(drop->seed >> 32), drop->step, drop->step_at, (uint32_t)(border >> 16), (uint32_t)(border & 0xFFFFu)};
+    const uint32_t keep_hi = border >> 32 ? 0xFFFFu : (uint32_t)(border >> 16);              // all of them: every half up to 65,535, and there every other
+    *d = {(uint32_t)drop->seed, (uint32_t)(drop->seed >> 32), drop->step, drop->step_at, keep_hi, (uint32_t)(border - ((uint64_t)keep_hi << 16))};
     return SAME_LDA_OK;
 }
 
 namespace {
 
+constexpr int64_t kRounds = 8;                                           // workgroups of a launch for each that a compute unit holds
+
 template <class TI, class TO>
-int rows_launch(const char* call, const RowsArgs& a, bool drop, hipStream_t st)
+int rows_launch(const char* call, RowsArgs& a, bool drop, hipStream_t st)
 {
-    const int64_t all = a.n * a.chunks;
-    const dim3 grid((unsigned)at_most((all + 511) / 512, kMaxGroups));
+    const int64_t groups = at_most((a.n * a.chunks + kChunksAtOnce - 1) / kChunksAtOnce, kComputeUnits * 8 * kRounds);
+    const int64_t step = groups * kChunksAtOnce;
+    a.step_rows = (int32_t)(step / a.chunks);
+    a.step_chunks = (int32_t)(step % a.chunks);
+    const dim3 grid((unsigned)groups);
     if (drop) hipLaunchKernelGGL((rows_kernel<TI, TO, true>), grid, dim3(256), 0, st, a);
     else if constexpr (__is_same(TI, GroupCode)) hipLaunchKernelGGL((rows_kernel<TI, TO, false>), grid, dim3(256), 0, st, a);
     return launched(call);
 }
 
 template <class TI>
-int rows_to(const char* call, const RowsArgs& a, bool drop, int32_t type, hipStream_t st)
+int rows_to(const char* call, RowsArgs& a, bool drop, int32_t type, hipStream_t st)
 {
     switch (type) {
         case SAME_LDA_FLOAT:  return rows_launch<TI, float>(call, a, drop, st);

@@ -92,7 +92,9 @@ def test_shapes_types_tokens_and_scales_are_refused():
     refused(L.same_lda_embed_dropout_grad(ref(a), None, 4, 1.0, ref(d), 0, ref(a), P, 1 << 30, None), "null")
     refused(L.same_lda_embed_dropout_grad(ref(a), P, 4, 1.0, ref(d), 0, ref(g), P, 1 << 30, None), "must not be grouped")
     many = rows(rows=50_000)
-    assert L.same_lda_embed_grad_workspace(ref(many), ref(a), ref(n)) == 0 and n.value > 0
+    assert L.same_lda_embed_dropout_grad_workspace(ref(many), ref(a), ref(n)) == 0 and n.value > 0
+    refused(L.same_lda_embed_dropout_grad_workspace(ref(many), ref(a), None), "null")
+    refused(L.same_lda_embed_dropout_grad_workspace(ref(many), ref(rows(width=7)), ref(n)), "elements")
     refused(L.same_lda_embed_dropout_grad(ref(many), P, 4, 1.0, ref(d), 0, ref(a), P, n.value - 1, None), "workspace")
     refused(L.same_lda_micro_quantize(ref(g), ref(m), None), "must not be grouped")
     refused(L.same_lda_micro_quantize(ref(a), ref(g), None), "must be microscaled")
@@ -136,6 +138,23 @@ def test_sizes_of_grouped_matrices():
     L, c, s = binding.load(), ctypes.c_size_t(), ctypes.c_size_t()
     for r, w, group, code, scale in [(0, 1, 32, 0, 0), (3, 1, 32, 192, 48), (3, 128, 64, 192, 24), (3, 129, 128, 384, 24), ((1 << 31) - 1, 1 << 20, 32, ((1 << 31) - 1) << 19, ((1 << 31) - 1) << 17)]:
         assert L.same_lda_group_size(r, w, group, ref(c), ref(s)) == 0 and (c.value, s.value) == (code, scale)
+
+
+def test_workspaces_of_products_and_of_gradients():
+    L, n, m = binding.load(), ctypes.c_size_t(), ctypes.c_size_t()
+    for r, w, t, some in [(1, 4096, F, False), (16, 4096, B, False), (16, 4097, B, True), (17, 8, H, True), (0, 8, F, False), (5000, 1 << 20, F, True), ((1 << 31) - 1, 128, B, True)]:
+        assert L.same_lda_group_product_workspace(ref(rows(rows=r, width=w, type=t)), ref(rows(type=64, width=w)), ref(n)) == 0 and (n.value > 0) == some
+        # rows laid down are 256 MB or 4096 rows, in three pieces of two bytes; their sums are less than a tenth of that
+        assert n.value <= 1.1 * max((1 << 28) + (1 << 20), 4096 * (w + 1024) * 6)
+    refused(L.same_lda_group_product_workspace(ref(rows()), ref(rows(type=64)), None), "null")
+    refused(L.same_lda_group_product_workspace(ref(rows()), ref(rows(type=64, width=9)), ref(n)), "elements")
+    a, g, out = rows(rows=20), rows(type=64), rows(rows=20, width=4)
+    assert L.same_lda_group_product_workspace(ref(a), ref(g), ref(n)) == 0
+    for space, size in [(P, n.value - 1), (None, n.value), (P + 8, n.value)]:
+        refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(out), space, size, None), "workspace")
+    # wide rows of a few thousand tokens are sorted where the lookup had dropout
+    assert L.same_lda_embed_grad_workspace(ref(rows(rows=8000, width=1024)), ref(rows(width=1024)), ref(n)) == 0 and n.value == 0
+    assert L.same_lda_embed_dropout_grad_workspace(ref(rows(rows=8000, width=1024)), ref(rows(width=1024)), ref(m)) == 0 and m.value > 0
 
 
 def test_binding_refuses_what_it_cannot_pass_on():
