@@ -15,15 +15,16 @@ namespace {
 // Rows of either operand in a launch: grids stay below 2^32 threads (the output's size bounds the tiles), and what rows of a are laid down in
 // below 256 MB or 4096 rows.
 constexpr int64_t kRowsOfB = (int64_t)1 << 28;
+int64_t filled_blocks(int64_t width) { return (same::micro_groups(width) + 3) / 4 * 4; }     // for up to four waves that share a row
 int64_t rows_of_a(const same_lda_rows* a)
 {
-    const int64_t most = ((int64_t)1 << 28) / (same::micro_groups(a->width) * 128 * (a->type == SAME_LDA_FLOAT ? 6 : 2)) / 128 * 128;
+    const int64_t most = ((int64_t)1 << 28) / (filled_blocks(a->width) * 128 * (a->type == SAME_LDA_FLOAT ? 6 : 2)) / 128 * 128;
     return most < 4096 ? 4096 : most > ((int64_t)1 << 24) ? (int64_t)1 << 24 : most;
 }
 
 bool few_rows(const same_lda_rows* a) { return a->rows <= 16 && same::micro_groups(a->width) <= 32; }
 
-// Workspace of the rows of a, laid down for tiles of up to 128 rows and trips of up to 8 blocks, and of their sums.
+// Workspace of the rows of a, laid down for tiles of up to 128 rows, and of their sums.
 struct RowsSpace {
     size_t operands, bytes;
 };
@@ -31,7 +32,7 @@ struct RowsSpace {
 RowsSpace rows_space(const same_lda_rows* a)
 {
     if (few_rows(a)) return {0, 0};
-    const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 127) / 128 * 8), filled = (size_t)((same::micro_groups(a->width) + 7) / 8 * 8);
+    const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 127) / 128 * 8), filled = (size_t)filled_blocks(a->width);
     const size_t operands = tiles * filled * 4 * (a->type == SAME_LDA_FLOAT ? 3 : 1) * 1024;
     return {operands, operands + tiles * ((filled * 4 + 31) / 32) * 3 * 1024};
 }
@@ -59,6 +60,7 @@ template <class TI, int kGroupLog2, int MT, int NT, int WM, int WN, int WK, int 
 void product_tiles(const same::GroupProductArgs& p, void* operands, void* sums, hipStream_t st)
 {
     constexpr int P = sizeof(TI) == 4 ? 3 : 1, kTall = 16 * MT * WM, kWide = 16 * NT * WN;
+    static_assert(WK <= 4 && kTall <= 128, "the workspace is for these");
     const int blocks = (p.width + 127) / 128, filled = (blocks + WK - 1) / WK * WK;
     const int64_t tiles_a = (p.rows_a + kTall - 1) / kTall, tiles_b = ((p.rows_b + kWide - 1) / kWide + 7) / 8 * 8;
     const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, static_cast<same::v4u32*>(operands), static_cast<uint16_t*>(sums)};
