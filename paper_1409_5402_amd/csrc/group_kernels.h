@@ -11,15 +11,48 @@
 
 namespace same {
 
-// ---- Rounding.  A lane takes 8 elements, 2^(group_log2 - 3) consecutive lanes a group.  The quotient (x - b) / s is taken in
-// binary32; where that leaves open on which side of a border between two codes it lies (or leaves its range) it is taken in binary64.
+// ---- Rounding.  A lane takes 8 elements, 2^(group_log2 - 3) consecutive lanes a group.  The quotient (x - b) / s is taken as a product
+// in binary32; where that leaves open on which side of a border between two codes it lies, x - b is compared with the border, exactly, and at
+// the ends of the range the quotient is taken in binary64.  Bound by memory in binary32 (100,000 x 256: 22.3 us, 5.2 TB/s read and written),
+// by its instructions on 16-bit rows, half as long (8192 x 8192 bf16: 67 us, 2.5 TB/s).
 struct GroupQuantizeArgs {
     const void* x;
     int64_t rows, stride;
     int32_t width, group_log2;
     uint32_t* codes;
     uint32_t* scales;
+    int32_t chunks;                  // of 8 elements of a filled row
+    float inverse;                   // of chunks
+    int32_t step_rows, step_chunks;  // what all workgroups take at once, kRoundedAtOnce each, in rows and chunks
 };
+
+constexpr int kRoundedAtOnce = 256;
+
+// Without the quieting of signalling NaNs that the functions of the language ask for.
+__device__ __forceinline__ float least3(float x, float y, float z)
+{
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+__device__ __forceinline__ float most3(float x, float y, float z)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+
+// The least (or largest) of 4, 8 or 16 consecutive lanes, in all of them.
+template <class F>
+__device__ __forceinline__ float of_lanes(float x, int group_log2, F&& f)
+{
+    const auto with = [&](auto control) { x = f(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), decltype(control)::value, 0xF, 0xF, true))); };
+    with(std::integral_constant<int, 0xB1>());                                 // lane ^ 1
+    with(std::integral_constant<int, 0x4E>());                                 // lane ^ 2
+    if (group_log2 > 5) with(std::integral_constant<int, 0x141>());            // 7 - lane of eight
+    if (group_log2 > 6) with(std::integral_constant<int, 0x140>());            // 15 - lane of sixteen
+    return x;
+}
 
 // the largest bfloat16 number that is not above x, which is finite; -0 becomes 0
 __device__ __forceinline__ float bfloat_below(float x)
@@ -31,56 +64,126 @@ __device__ __forceinline__ float bfloat_below(float x)
 }
 
 template <class TI>
-__global__ __launch_bounds__(256) void group_quantize_kernel(GroupQuantizeArgs a)
+__device__ __forceinline__ void group_round(const GroupQuantizeArgs& a, Eight<TI>& raw, uint32_t row, int c, int lanes)
 {
-    const int64_t pieces = micro_groups(a.width) * (kMicroGroup / 8);          // of 8 elements, per row
-    const int64_t all = a.rows * pieces;
-    const int lanes = 1 << (a.group_log2 - 3);
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {   // whole blocks of 16 lanes
-        const int64_t row = all >> 32 ? at / pieces : (int64_t)((uint32_t)at / (uint32_t)pieces);             // a division of 64 bits takes as long as the rest
-        const int c = (int)(at - row * pieces), count = a.width - 8 * c;
-        float x[8];
-        load_eight<TI>(x, static_cast<const TI*>(a.x) + row * a.stride, 8 * c, a.width);
-        float least = __builtin_inff(), most = -__builtin_inff();
-        int bad = 0;
+    const int count = a.width - 8 * c;
+    float x[8], sum = 0.0f;
+    if (count < 8) cut_eight(raw, 8 * c, a.width);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < count) {
-                bad |= (__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u;
-                least = fminf(least, x[j]);
-                most = fmaxf(most, x[j]);
-            }
-        for (int o = 1; o < lanes; o <<= 1) {
-            least = fminf(least, __shfl_xor(least, o));
-            most = fmaxf(most, __shfl_xor(most, o));
-            bad |= __shfl_xor(bad, o);
-        }
-        uint32_t word = 0u, sb = 0u;
-        if (bad) {
-            sb = 0x7FC07FC0u;
-        } else if (least <= most) {                                            // else a group behind the row's end
-            const float base = bfloat_below(least);
-            uint32_t step_bits = __float_as_uint((float)(__bf16)(float)(((double)most - (double)base) / 15.0)) >> 16;
+    for (int j = 0; j < 8; ++j) x[j] = to_float(raw.v[j]);
+    if (count < 8)                                                             // behind the row's end: its elements' first, which changes nothing
+#pragma unroll
+        for (int j = 1; j < 8; ++j) x[j] = j < count ? x[j] : x[0];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += x[j];
+    float least = least3(least3(x[0], x[1], x[2]), least3(x[3], x[4], x[5]), least3(x[6], x[7], x[7]));
+    float most = most3(most3(x[0], x[1], x[2]), most3(x[3], x[4], x[5]), most3(x[6], x[7], x[7]));
+    bool bad = !(fabsf(sum) < __builtin_inff());                               // an infinity, a NaN or a sum beyond binary32
+    if (bad) {
+        bad = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bad |= (__float_as_uint(x[j]) & 0x7FFFFFFFu) >= 0x7F800000u;
+    }
+    most = count <= 0 ? -__builtin_inff() : bad ? __builtin_inff() : most;
+    least = count <= 0 ? __builtin_inff() : bad ? -__builtin_inff() : least;
+    most = of_lanes(most, a.group_log2, [](float p, float q) { return most3(p, q, q); });
+    least = of_lanes(least, a.group_log2, [](float p, float q) { return least3(p, q, q); });
+    bad = most == __builtin_inff();
+    uint32_t word = 0u, sb = 0u;
+    if (bad) {
+        sb = 0x7FC07FC0u;
+    } else if (least <= most) {                                            // else a group behind the row's end
+        const float base = bfloat_below(least);
+        // (most - base) / 15 by a product that is off by less than four units of its last place: enough unless it is as near to a
+        // border between two bfloat16 numbers, or near the ends of the range
+        const float range = most - base, near_step = range * 0.06666667f;
+        uint32_t step_bits = (__float_as_uint(near_step) + 0x8000u) >> 16;
+        const int border = (int)(__float_as_uint(near_step) & 0xFFFFu) - 0x8000;
+        const bool ordinary = range >= 1e-30f && range <= 1e30f;
+        if (!(ordinary && abs(border) > 4)) {
+            step_bits = __float_as_uint((float)(__bf16)(float)(((double)most - (double)base) / 15.0)) >> 16;
             if ((double)base + 15.0 * (double)from_bfloat_bits(step_bits) > 3.4028234663852886e38) --step_bits;
-            const float step = from_bfloat_bits(step_bits);
-            sb = __float_as_uint(base) | step_bits;
-            const float inverse = 1.0f / step;
-            if (step_bits) {
+        }
+        const float step = from_bfloat_bits(step_bits);
+        sb = __float_as_uint(base) | step_bits;
+        if (step_bits) {
+            const float inverse = __builtin_amdgcn_rcpf(step);                // to a unit of the last place
+            float off = 1.0f;                                              // least distance to a border
+            float near[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float t = (x[e] - base) * inverse;
+                near[e] = rintf(t);
+                off = fminf(off, 0.5f - fabsf(t - near[e]));
+                near[e] = __builtin_amdgcn_fmed3f(near[e], 0.0f, 15.0f);
+                // (elements behind the row's end are zeros, whose code is cut off below)
+            }
+            if (!ordinary) {
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) {                              // eight turns of the registers
+                    const double exact = rint(((double)x[0] - (double)base) / (double)step);
+                    const float first = (float)fmin(fmax(exact, 0.0), 15.0), x0 = x[0];
+#pragma unroll
+                    for (int j = 0; j < 7; ++j) { near[j] = near[j + 1]; x[j] = x[j + 1]; }
+                    near[7] = first;
+                    x[7] = x0;
+                }
+            } else if (!(off > 1.52587890625e-5f)) {                       // t is off by less than 2^-18: within 2^-16 of a border
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float t = (x[e] - base) * inverse, near = rintf(t);
-                    float q = fminf(fmaxf(near, 0.0f), 15.0f);
-                    // t is off by less than 2^-18; at a border or out of range: in binary64
-                    if (!(fabsf(fabsf(t - near) - 0.5f) > 1.52587890625e-5f)) {
-                        const double exact = rint(((double)x[e] - (double)base) / (double)step);
-                        q = (float)fmin(fmax(exact, 0.0), 15.0);
-                    }
-                    if (e < count) word |= (uint32_t)q << (4 * (e >> 1) + 16 * (e & 1));
+                    // x - base is d and a rest exactly; the borders next to near are numbers of binary32, which d keeps its side of or is
+                    const float d = x[e] - base, back = d - x[e], rest = (x[e] - (d - back)) - (base + back);
+                    const float up = (near[e] + 0.5f) * step, down = (near[e] - 0.5f) * step;
+                    const int odd = (int)near[e] & 1;                          // no branches: bits
+                    const int above = (d > up) | ((d == up) & ((rest > 0.0f) | ((rest == 0.0f) & odd)));
+                    const int below = (d < down) | ((d == down) & ((rest < 0.0f) | ((rest == 0.0f) & odd)));
+                    near[e] = __builtin_amdgcn_fmed3f(near[e] + (float)(above - below), 0.0f, 15.0f);
                 }
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) word |= (uint32_t)near[e] << (4 * (e >> 1) + 16 * (e & 1));
+            if (count < 8)
+                for (int e = 0; e < 8; ++e)
+                    if (e >= count) word &= ~(15u << (4 * (e >> 1) + 16 * (e & 1)));
         }
-        a.codes[(at - c) + group_word(c)] = word;                              // rows of codes follow each other without a gap
-        if ((c & (lanes - 1)) == 0) a.scales[at >> (a.group_log2 - 3)] = sb;
+    }
+    const int64_t first = (int64_t)row * a.chunks;                             // rows of codes follow each other without a gap
+    a.codes[first + group_word(c)] = word;
+    if ((c & (lanes - 1)) == 0) a.scales[(first + c) >> (a.group_log2 - 3)] = sb;
+}
+
+template <class TI>
+__global__ __launch_bounds__(256) void group_quantize_kernel(GroupQuantizeArgs a)
+{
+    constexpr int kMany = kRoundedAtOnce / 256;
+    const int lanes = 1 << (a.group_log2 - 3);
+    const int64_t begin = (int64_t)blockIdx.x * kRoundedAtOnce;
+    uint32_t row0 = (uint32_t)(begin / a.chunks);                              // of the workgroup; a lane's own by a short division
+    int c0 = (int)(begin - (int64_t)row0 * a.chunks);
+    const uint32_t rows = (uint32_t)a.rows;
+    while (row0 < rows) {
+        Eight<TI> raw[kMany];
+        uint32_t row[kMany];
+        int chunk[kMany];
+#pragma unroll
+        for (int q = 0; q < kMany; ++q) {
+            const int at = c0 + q * 256 + (int)threadIdx.x;                    // below 2^17 + 512: the quotient is exact
+            const int down = (int)(((float)at + 0.5f) * a.inverse);
+            row[q] = row0 + (uint32_t)down;
+            chunk[q] = at - down * a.chunks;
+            raw[q] = eight_at(static_cast<const TI*>(a.x) + (int64_t)min(row[q], rows - 1u) * a.stride, 8 * chunk[q], a.width);
+        }
+#pragma unroll
+        for (int q = 0; q < kMany; ++q) {
+            if (row[q] >= rows) continue;                                      // whole blocks of 16 lanes
+            group_round(a, raw[q], row[q], chunk[q], lanes);
+        }
+        row0 += (uint32_t)a.step_rows;
+        c0 += a.step_chunks;
+        if (c0 >= a.chunks) {
+            c0 -= a.chunks;
+            ++row0;
+        }
     }
 }
 

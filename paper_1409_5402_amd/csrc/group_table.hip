@@ -135,10 +135,11 @@ int same_lda_group_quantize(const same_lda_rows* x, const same_lda_rows* group_o
         return fail_without_handle(SAME_LDA_EINVAL, "group_quantize: %lld x %d into %lld x %d", (long long)x->rows, x->width, (long long)group_out->rows, group_out->width);
     if (x->rows == 0) return SAME_LDA_OK;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const int32_t chunks = (int32_t)same::micro_groups(x->width) * 16;
+    const int64_t groups = at_most((x->rows * chunks + same::kRoundedAtOnce - 1) / same::kRoundedAtOnce, kComputeUnits * 64), step = groups * same::kRoundedAtOnce;
     const same::GroupQuantizeArgs a = {x->data, x->rows, x->stride, x->width, __builtin_ctz((unsigned)group_out->type), static_cast<uint32_t*>(group_out->data),
-                                       reinterpret_cast<uint32_t*>(group_out->scales)};
-    const int64_t pieces = x->rows * same::micro_groups(x->width) * 16;
-    const dim3 grid((unsigned)at_most((pieces + 255) / 256, kMaxGroups));
+                                       reinterpret_cast<uint32_t*>(group_out->scales), chunks, 1.0f / (float)chunks, (int32_t)(step / chunks), (int32_t)(step % chunks)};
+    const dim3 grid((unsigned)groups);
     switch (x->type) {
         case SAME_LDA_FLOAT:  hipLaunchKernelGGL(same::group_quantize_kernel<float>, grid, dim3(256), 0, st, a); break;
         case SAME_LDA_BFLOAT: hipLaunchKernelGGL(same::group_quantize_kernel<__bf16>, grid, dim3(256), 0, st, a); break;

@@ -109,7 +109,10 @@ def test_rounding_of_ties_borders_and_the_ends_of_the_range():
     ends[10, 1:] = 1e-38 * torch.arange(1, 128)
     ends[11] = -1e30 - 1e23 * torch.arange(128)
     offset = torch.from_numpy(1000 + rng.normal(size=(20, 128))).float()
-    for x in (ties, ends, offset):
+    small = torch.from_numpy(rng.normal(size=(40, 128)) * 2.0 ** np.arange(-148, -108)[:, None]).float()      # steps that are subnormal, or nearly
+    large = torch.from_numpy(rng.normal(size=(8, 128)) * 2.0 ** np.arange(118, 126)[:, None]).float()
+    coarse = torch.from_numpy(rng.integers(-60, 61, (200, 128)) / 4).bfloat16().float()                       # many numbers on a border
+    for x in (ties, ends, offset, small, large, coarse):
         for group in GROUPS:
             same(binding.group_quantize(x.to(DEV), group), x, group)
 
