@@ -78,19 +78,31 @@ void product_launch(same::GroupProductArgs& p, bool few, void* operands, void* s
         if constexpr (sizeof(TI) == 4) return p.rows_a <= 4 ? product_few_by_width<TI, 1, true, kGroupLog2>(p, blocks, st) : product_few_by_width<TI, 3, false, kGroupLog2>(p, blocks, st);
         else return product_few_by_width<TI, 1, false, kGroupLog2>(p, blocks, st);
     }
-    // us of the two launches, in the order of the forms below (rows of a x rows of b x width; G128, 16-bit)
+    // Tiles are as large as still gives every compute unit some, and where there are many those whose last round is the fuller one: by the
+    // workgroups that run at once (LDS bounds them), and what a round takes to that of the next form.  us of the two launches, G128, by form:
+    //   bf16                 64x256  64x128  64x64  32x128  32x64  16x128      binary32             64x256  32x128  32x64  16x64
+    //   512 x 50,021 x 1024     106     109    231     177    354     293      512 x 50,021 x 1024     236     251    446    641
+    //   2048 x 8192 x 4096      169     196    392     288    461     489      256 x 20,000 x 2000     101      94    142    193
+    //   64 x 50,021 x 1024       25      23     41      33     53      48      64 x 50,021 x 1024       38      42     67     88
+    //   256 x 8000 x 1000        22      16     23      19     32      29      128 x 8192 x 8192       162      76    100    126
+    //   128 x 8192 x 8192        93      68     44      49     58      73      512 x 1000 x 4000        87      42     34     45
+    //   32 x 50,021 x 4096       58      56     85      52     66      78      40 x 10,000 x 2000       49      23     31     23
+    //   32 x 4096 x 4096         45      32     24      23     17      21      32 x 4096 x 4096         82      36     27     20
+    //   1 x 20,000 x 8192        92      70     79      52     59      46
     const auto tiles = [&](int64_t tall, int64_t wide) { return ((p.rows_a + tall - 1) / tall) * ((p.rows_b + wide - 1) / wide); };
+    const auto rounds = [&](int64_t tall, int64_t wide, int64_t per_unit) { return (tiles(tall, wide) + per_unit * kComputeUnits - 1) / (per_unit * kComputeUnits); };
     if constexpr (sizeof(TI) == 4) {
-        if (p.rows_a > 32 && tiles(64, 256) >= 512)      product_tiles<TI, kGroupLog2, 2, 4, 2, 4, 1, 2>(p, operands, sums, st);
-        else if (p.rows_a > 16 && tiles(32, 128) >= 384) product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 2>(p, operands, sums, st);
-        else                                             product_tiles<TI, kGroupLog2, 1, 2, 1, 2, 4, 2>(p, operands, sums, st);
+        if (p.rows_a > 32 && 17 * rounds(64, 256, 1) <= 10 * rounds(32, 128, 2)) product_tiles<TI, kGroupLog2, 2, 4, 2, 4, 1, 2>(p, operands, sums, st);
+        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 2>(p, operands, sums, st);
+        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits / 2) product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 2, 2>(p, operands, sums, st);
+        else                                                         product_tiles<TI, kGroupLog2, 1, 2, 1, 2, 4, 2>(p, operands, sums, st);
     } else {
-        if (p.rows_a > 32 && tiles(64, 256) >= 1536)     product_tiles<TI, kGroupLog2, 4, 4, 1, 4, 1, 2>(p, operands, sums, st);
-        else if (p.rows_a > 32 && tiles(64, 128) >= 384) product_tiles<TI, kGroupLog2, 4, 2, 1, 4, 1, 2>(p, operands, sums, st);
-        else if (p.rows_a > 32 && tiles(64, 64) >= 192)  product_tiles<TI, kGroupLog2, 4, 2, 1, 2, 2, 3>(p, operands, sums, st);
-        else if (p.rows_a > 16 && tiles(32, 128) >= 256) product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 4>(p, operands, sums, st);
-        else if (p.rows_a > 16)                          product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 4, 3>(p, operands, sums, st);
-        else                                             product_tiles<TI, kGroupLog2, 1, 2, 1, 4, 1, 4>(p, operands, sums, st);
+        if (p.rows_a > 32 && 5 * rounds(64, 256, 2) <= 4 * rounds(64, 128, 3)) product_tiles<TI, kGroupLog2, 4, 4, 1, 4, 1, 2>(p, operands, sums, st);
+        else if (p.rows_a > 32 && tiles(64, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 4, 2, 1, 4, 1, 2>(p, operands, sums, st);
+        else if (p.rows_a > 32 && tiles(64, 64) > kComputeUnits / 2) product_tiles<TI, kGroupLog2, 4, 2, 1, 2, 2, 3>(p, operands, sums, st);
+        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 4>(p, operands, sums, st);
+        else if (p.rows_a > 16)                                      product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 4, 3>(p, operands, sums, st);
+        else                                                         product_tiles<TI, kGroupLog2, 1, 2, 1, 4, 1, 4>(p, operands, sums, st);
     }
 }
 
