@@ -309,28 +309,26 @@ __device__ __forceinline__ v4u32 all_ones()
 }
 
 // Any number of rows, in two launches.  The first one lays the rows of a down as the lanes of the matrix instruction take them, cut into pieces
-// and filled up with zeros: per 16 rows and block of 128 elements 4 P operands of 1 KB; and the sums S of their groups, 32 groups to the
-// three operands of a bfloat16 instruction.
+// and filled up with zeros: per 16 rows and block of 128 elements 4 P operands of 1 KB; and the sums S of their groups.
 struct GroupRowsArgs {
     const void* a;
     int64_t rows_a, stride_a;
     int32_t width;
     int32_t blocks, filled;          // of 128 elements in a row; with those that are zeros
     v4u32* operands;                 // [16 rows][filled][4][P][64]
-    uint16_t* sums;                  // [16 rows][sets of 32 groups][3][64][8]
+    float* sums;                     // [16 rows][filled][groups of a block][16]
 };
 
 template <class TI, int kGroupLog2>
 __global__ __launch_bounds__(256) void group_rows_kernel(GroupRowsArgs a)
 {
     constexpr bool kHalf = kHalfMatrix<TI>;
-    constexpr int P = sizeof(TI) == 4 ? 3 : 1, kPer = 128 >> kGroupLog2, kSteps = 4 / kPer, kAll = 32 / kPer;   // groups of a block, instructions per group, blocks of a set
+    constexpr int P = sizeof(TI) == 4 ? 3 : 1, kPer = 128 >> kGroupLog2, kSteps = 4 / kPer;             // groups of a block, instructions per group
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int64_t tile = blockIdx.x;
     const int64_t i = tile * 16 + r < a.rows_a ? tile * 16 + r : a.rows_a - 1;         // rows behind the last one: it again
     const TI* const row = static_cast<const TI*>(a.a) + i * a.stride_a;
-    const int sets = (a.blocks + kAll - 1) / kAll, most = a.filled > sets * kAll ? a.filled : sets * kAll;
-    for (int k = blockIdx.y * 4 + (threadIdx.x >> 6); k < most; k += gridDim.y * 4) {
+    for (int k = blockIdx.y * 4 + (threadIdx.x >> 6); k < a.filled; k += gridDim.y * 4) {
         Eight<TI> raw[4] = {};
         if (k < a.blocks)
 #pragma unroll
@@ -343,23 +341,13 @@ __global__ __launch_bounds__(256) void group_rows_kernel(GroupRowsArgs a)
             pieces_of<TI, P>(c, raw[t]);
 #pragma unroll
             for (int q = 0; q < P; ++q) {
-                if (k < a.filled) a.operands[((tile * a.filled + k) * (4 * P) + t * P + q) * 64 + lane] = c[q];
+                a.operands[((tile * a.filled + k) * (4 * P) + t * P + q) * 64 + lane] = c[q];
                 total[t / kSteps] = mfma_16<kHalf>(all_ones<kHalf>(), c[q], total[t / kSteps]);
             }
         }
-        if (h == 0 && k < sets * kAll)
+        if (h == 0)
 #pragma unroll
-            for (int g = 0; g < kPer; ++g) {
-                const int in = (k % kAll) * kPer + g;                                  // of the set: element in % 8 of lane (in / 8, r)
-                uint16_t* const to = a.sums + (((tile * sets + k / kAll) * 3 * 64 + (in / 8) * 16 + r) * 8 + in % 8);
-                float y = total[g][0];
-#pragma unroll
-                for (int q = 0; q < 3; ++q) {
-                    const uint32_t bits = __float_as_uint(y);
-                    to[q * 64 * 8] = (uint16_t)(bits >> 16);
-                    y -= __uint_as_float(bits & 0xFFFF0000u);
-                }
-            }
+            for (int g = 0; g < kPer; ++g) a.sums[((tile * a.filled + k) * kPer + g) * 16 + r] = total[g][0];
     }
 }
 
@@ -369,7 +357,7 @@ __global__ __launch_bounds__(256) void group_rows_kernel(GroupRowsArgs a)
 struct GroupTilesArgs {
     GroupProductArgs p;
     const v4u32* operands;
-    const v4u32* sums;
+    const float* sums;
     int32_t blocks, filled;          // filled: a multiple of WK
 };
 
@@ -378,12 +366,14 @@ struct GroupStage {
     v4u32 rows[WK][WM][MT][4][P][64];
     v4u32 codes[WK][WN][NT][64];
     uint32_t scales[WK][WN][NT][16][128 >> kGroupLog2];
+    static constexpr int kSums = WK * WM * MT * (128 >> kGroupLog2) * 16;
+    float sums[kSums < 64 ? 64 : kSums];                                       // [WK][WM][MT][groups][16]
 };
 
 template <bool kHalf, int P, int kGroupLog2, int MT, int NT, int WM, int WN, int WK, int kStages>
 __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, kGroupLog2, MT, NT, WM, WN, WK>) * 3 <= 163840 && WM * WN * WK == 4 ? 3 : 2) void group_product_kernel(GroupTilesArgs a)
 {
-    constexpr int kPer = 128 >> kGroupLog2, kSteps = 4 / kPer, kAll = 32 / kPer;       // groups of a block, instructions per group, blocks of a set
+    constexpr int kPer = 128 >> kGroupLog2, kSteps = 4 / kPer;                         // groups of a block, instructions per group
     constexpr int kWaves = WM * WN * WK;
     using Stage = GroupStage<P, kGroupLog2, MT, NT, WM, WN, WK>;
     __shared__ union {
@@ -404,13 +394,14 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
     const int last = (int)(p.rows_b - first_j < kWide ? p.rows_b - first_j : kWide) - 1;     // rows behind the last are computed from it and not written
 
     // what a trip needs, in equal numbers for every wave (the last pieces are fetched twice where they do not go round)
-    constexpr int kRows = WK * WM * MT * 4 * P, kCodes = WK * WN * NT, kWords = WK * WN * NT * 16 * kPer;
+    constexpr int kRows = WK * WM * MT * 4 * P, kCodes = WK * WN * NT, kWords = WK * WN * NT * 16 * kPer, kSums = Stage::kSums;
     constexpr int kRowsEach = (kRows + kWaves - 1) / kWaves, kCodesEach = (kCodes + kWaves - 1) / kWaves, kWordsEach = (kWords + 64 * kWaves - 1) / (64 * kWaves);
-    constexpr int kEach = kRowsEach + kCodesEach + kWordsEach;
+    constexpr int kSumsEach = (kSums + 64 * kWaves - 1) / (64 * kWaves), kEach = kRowsEach + kCodesEach + kWordsEach + kSumsEach;
     const uint8_t* const rows = reinterpret_cast<const uint8_t*>(a.operands + first_i / 16 * a.filled * (4 * P) * 64);
     const uint8_t* const codes = p.codes + first_j * p.pitch;
     const uint8_t* const words = p.scales + first_j * p.scale_pitch;
-    uint32_t code_at[kCodesEach], word_at[kWordsEach];                                 // of this lane, in the tile's rows of b
+    const uint8_t* const sums = reinterpret_cast<const uint8_t*>(a.sums + first_i / 16 * a.filled * (kPer * 16));
+    uint32_t code_at[kCodesEach], word_at[kWordsEach], sum_at[kSumsEach];              // of this lane, in the tile's rows
 #pragma unroll
     for (int f = 0; f < kCodesEach; ++f) {
         const int e = min(f * kWaves + wv, kCodes - 1);
@@ -420,6 +411,11 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
     for (int f = 0; f < kWordsEach; ++f) {
         const int e = min((f * kWaves + wv) * 64, kWords - 64) + lane;
         word_at[f] = (uint32_t)min(e / kPer % kWide, last) * (uint32_t)p.scale_pitch + 4 * (e % kPer);
+    }
+#pragma unroll
+    for (int f = 0; f < kSumsEach; ++f) {
+        const int e = min(min((f * kWaves + wv) * 64, kSums < 64 ? 0 : kSums - 64) + lane, kSums - 1);
+        sum_at[f] = (uint32_t)((e / (kPer * 16) % (WM * MT) * a.filled + e / (WM * MT * kPer * 16)) * (kPer * 16) + e % (kPer * 16)) * 4;
     }
     const auto fetch = [&](int trip) {
         Stage& to = lds.in[trip % kStages];
@@ -439,36 +435,15 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
             const int e = min((f * kWaves + wv) * 64, kWords - 64), k = min(t * WK + e / (kWide * kPer), a.blocks - 1);
             to_lds_4(uniform(words + (int64_t)k * (4 * kPer)), word_at[f], &to.scales[0][0][0][0][0] + e);
         }
+#pragma unroll
+        for (int f = 0; f < kSumsEach; ++f)
+            to_lds_4(uniform(sums + (int64_t)t * (WK * kPer * 64)), sum_at[f], &to.sums[min((f * kWaves + wv) * 64, kSums < 64 ? 0 : kSums - 64)]);
     };
-    static_assert(kWide * kPer % 64 == 0, "a piece of scales is of one block");
+    static_assert(kWide * kPer % 64 == 0 && (kSums < 64 || kSums % 64 == 0), "a piece of scales is of one block, of sums a whole one");
 #pragma unroll
     for (int f = 0; f + 1 < kStages; ++f) fetch(f);
 
-    // sum_g b_g S_g to begin with, by the first of the waves that share a row: 32 groups at a time
     v4f32 acc[MT][NT] = {};
-    const int sets = (a.blocks + kAll - 1) / kAll, groups = a.blocks * kPer;
-    if (wk == 0)
-#pragma unroll 1
-        for (int e = 0; e < sets; ++e) {
-            v4u32 b[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint32_t* const of = reinterpret_cast<const uint32_t*>(words + (int64_t)min(wn * (16 * NT) + 16 * n + r, last) * p.scale_pitch);
-                uint32_t sb[8];
-#pragma unroll
-                for (int q = 0; q < 8; ++q) sb[q] = of[min(e * 32 + 8 * h + q, groups - 1)];      // groups behind the last: it, times zero
-#pragma unroll
-                for (int q = 0; q < 4; ++q) b[n][q] = __builtin_amdgcn_perm(sb[2 * q + 1], sb[2 * q], 0x07060302u);
-            }
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int q = 0; q < 3; ++q) {
-                    const v4u32 s = a.sums[(((i0 / 16 + m) * sets + e) * 3 + q) * 64 + lane];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[m][n] = mfma_16<false>(s, b[n], acc[m][n]);
-                }
-        }
 #pragma unroll 1
     for (int trip = 0; trip < trips; ++trip) {
         arrived<(kStages - 2) * kEach>();
@@ -484,7 +459,11 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
         }
 #pragma unroll
         for (int g = 0; g < kPer; ++g) {
+            __builtin_amdgcn_sched_barrier(0);                                         // one group's operands in registers at a time: more of them spill
             v4u32 part[kSteps][MT][P];
+            v4f32 total[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) total[m] = *reinterpret_cast<const v4f32*>(&in.sums[(((wk * WM + wm) * MT + m) * kPer + g) * 16 + 4 * h]);
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -502,11 +481,11 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
 #pragma unroll
                         for (int m = 0; m < MT; ++m) d[m] = mfma_16<kHalf>(part[t][m][q], b, d[m]);
                 }
-                const float step = from_bfloat_bits(sb[n][g] & 0xFFFFu);
+                const float step = from_bfloat_bits(sb[n][g] & 0xFFFFu), base = __uint_as_float(sb[n][g] & 0xFFFF0000u);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[m][n][q] = __builtin_fmaf(step, d[m][q], acc[m][n][q]);
+                    for (int q = 0; q < 4; ++q) acc[m][n][q] = __builtin_fmaf(step, d[m][q], __builtin_fmaf(base, total[m][q], acc[m][n][q]));
             }
         }
     }

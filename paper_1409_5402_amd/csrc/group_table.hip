@@ -34,7 +34,7 @@ RowsSpace rows_space(const same_lda_rows* a)
     if (few_rows(a)) return {0, 0};
     const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 127) / 128 * 8), filled = (size_t)filled_blocks(a->width);
     const size_t operands = tiles * filled * 4 * (a->type == SAME_LDA_FLOAT ? 3 : 1) * 1024;
-    return {operands, operands + tiles * ((filled * 4 + 31) / 32) * 3 * 1024};
+    return {operands, operands + tiles * filled * 4 * 16 * sizeof(float)};
 }
 
 template <class TI, int P, bool kStack, int kGroupLog2, int KB>
@@ -61,12 +61,13 @@ void product_tiles(const same::GroupProductArgs& p, void* operands, void* sums, 
 {
     constexpr int P = sizeof(TI) == 4 ? 3 : 1, kTall = 16 * MT * WM, kWide = 16 * NT * WN;
     static_assert(WK <= 4 && kTall <= 128, "the workspace is for these");
+    constexpr int kFit = kStages * sizeof(same::GroupStage<P, kGroupLog2, MT, NT, WM, WN, WK>) <= 163840 ? kStages : kStages - 1;
     const int blocks = (p.width + 127) / 128, filled = (blocks + WK - 1) / WK * WK;
     const int64_t tiles_a = (p.rows_a + kTall - 1) / kTall, tiles_b = ((p.rows_b + kWide - 1) / kWide + 7) / 8 * 8;
-    const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, static_cast<same::v4u32*>(operands), static_cast<uint16_t*>(sums)};
-    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT * WM), (unsigned)at_most(((filled > blocks + 31 ? filled : blocks + 31) + 3) / 4, 65535)), dim3(256), 0, st, rows);
-    const same::GroupTilesArgs tiles = {p, static_cast<const same::v4u32*>(operands), static_cast<const same::v4u32*>(sums), blocks, filled};
-    hipLaunchKernelGGL((same::group_product_kernel<same::kHalfMatrix<TI>, P, kGroupLog2, MT, NT, WM, WN, WK, kStages>), dim3((unsigned)(tiles_a * tiles_b)), dim3(64 * WM * WN * WK), 0, st,
+    const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, static_cast<same::v4u32*>(operands), static_cast<float*>(sums)};
+    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT * WM), (unsigned)at_most((filled + 3) / 4, 65535)), dim3(256), 0, st, rows);
+    const same::GroupTilesArgs tiles = {p, static_cast<const same::v4u32*>(operands), static_cast<const float*>(sums), blocks, filled};
+    hipLaunchKernelGGL((same::group_product_kernel<same::kHalfMatrix<TI>, P, kGroupLog2, MT, NT, WM, WN, WK, kFit>), dim3((unsigned)(tiles_a * tiles_b)), dim3(64 * WM * WN * WK), 0, st,
                        tiles);
 }
 
