@@ -48,11 +48,14 @@ void product_few(same::GroupProductArgs& p, int blocks, hipStream_t st)
     hipLaunchKernelGGL((same::group_product_few_kernel<TI, P, kStack, kGroupLog2, KB>), dim3((unsigned)at_most(turns, kComputeUnits * 8 / waves)), dim3(64 * waves), 0, st, p);
 }
 
+// Up to two blocks of a row in a wave while eight waves hold the row (us with 1, 2 and 4 of them: 1 x 100,000 x 128 bf16 4.8, 6.5, 10.1;
+// x 256 7.7, 6.3, 9.6; x 1024 19.3, 16.5, 18.5; 16 x 50,021 x 2048 f32 22.7, 22.8, 35.5).  Two waves per SIMD: with three or four of these
+// 1 x 50,021 x 2048 bf16 takes 21 and 18 us for 16, its rows of a being fetched by more workgroups.
 template <class TI, int P, bool kStack, int kGroupLog2>
 void product_few_by_width(same::GroupProductArgs& p, int blocks, hipStream_t st)
 {
     if (blocks == 1) product_few<TI, P, kStack, kGroupLog2, 1>(p, blocks, st);
-    else if (blocks <= 2 || blocks == 16) product_few<TI, P, kStack, kGroupLog2, 2>(p, blocks, st);
+    else if (blocks <= 16) product_few<TI, P, kStack, kGroupLog2, 2>(p, blocks, st);
     else product_few<TI, P, kStack, kGroupLog2, 4>(p, blocks, st);
 }
 
@@ -82,14 +85,14 @@ void product_launch(same::GroupProductArgs& p, bool few, void* operands, void* s
     // Tiles are as large as still gives every compute unit some, and where there are many those whose last round is the fuller one: by the
     // workgroups that run at once (LDS bounds them), and what a round takes to that of the next form.  us of the two launches, G128, by form:
     //   bf16                 64x256  64x128  64x64  32x128  32x64  16x128      binary32             64x256  32x128  32x64  16x64
-    //   512 x 50,021 x 1024     106     109    231     177    354     293      512 x 50,021 x 1024     236     251    446    641
-    //   2048 x 8192 x 4096      169     196    392     288    461     489      256 x 20,000 x 2000     101      94    142    193
-    //   64 x 50,021 x 1024       25      23     41      33     53      48      64 x 50,021 x 1024       38      42     67     88
-    //   256 x 8000 x 1000        22      16     23      19     32      29      128 x 8192 x 8192       162      76    100    126
-    //   128 x 8192 x 8192        93      68     44      49     58      73      512 x 1000 x 4000        87      42     34     45
-    //   32 x 50,021 x 4096       58      56     85      52     66      78      40 x 10,000 x 2000       49      23     31     23
-    //   32 x 4096 x 4096         45      32     24      23     17      21      32 x 4096 x 4096         82      36     27     20
-    //   1 x 20,000 x 8192        92      70     79      52     59      46
+    //   512 x 50,021 x 4096     250     268    446     409    643     716      512 x 50,021 x 4096     615     648   1251   1739
+    //   2048 x 8192 x 4096      166     190    359     270    434     446      2048 x 8192 x 4096      389     467    959   1028
+    //   64 x 50,021 x 1024       22      19     33      26     45      36      64 x 50,021 x 1024       32      35     57     76
+    //   256 x 8000 x 1000        17      14     18      16     27      22      256 x 20,000 x 2000      93      80    128    176
+    //   128 x 8192 x 8192        91      63     40      45     52      68      128 x 8192 x 8192       162      72     94    118
+    //   32 x 50,021 x 4096       54      54     76      50     60      73      512 x 1000 x 4000        87      40     33     44
+    //   32 x 4096 x 4096         43      30     21      21     16      19      40 x 10,000 x 2000       45      21     27     21
+    //   1 x 20,000 x 8192        90      64     70      46     53      43      32 x 4096 x 4096         81      34     25     19
     const auto tiles = [&](int64_t tall, int64_t wide) { return ((p.rows_a + tall - 1) / tall) * ((p.rows_b + wide - 1) / wide); };
     const auto rounds = [&](int64_t tall, int64_t wide, int64_t per_unit) { return (tiles(tall, wide) + per_unit * kComputeUnits - 1) / (per_unit * kComputeUnits); };
     if constexpr (sizeof(TI) == 4) {
