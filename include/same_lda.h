@@ -265,8 +265,8 @@ int same_lda_synchronize(same_lda_t* h);
  * zero blocks to a multiple of 128 elements and follow each other without gaps: 64 bytes of codes (data, aligned to
  * 16) and 4 of scales (aligned to 4) per 128 elements; stride is not used.
  * SAME_LDA_GROUPS_OF_32, _64, _128: an element is q s + b, q in 0 .. 15, the step s and the base b of its group of 32, 64 or
- * 128 consecutive elements of a row in bfloat16.  Rows are filled up with codes 0 to a multiple of 128 elements and follow each
- * other without gaps: 64 bytes of codes (data, aligned to 16) per 128 elements, 4 bytes per group (scales, aligned to 4; s, then
+ * 128 consecutive elements of a row in bfloat16.  Rows are filled up to a multiple of 128 elements, with codes 0 and, in groups that hold
+ * no element, s and b 0 (codes there do not count, an s or b that is not finite would), and follow each other without gaps: 64 bytes of codes (data, aligned to 16) per 128 elements, 4 bytes per group (scales, aligned to 4; s, then
  * b); stride is not used.  Of 128 elements the 32-bit word 4 h + j (little endian) has the eight from 32 j + 8 h on: element 2 t of them is the
  * half byte t counted from the lowest, element 2 t + 1 the half byte 4 + t.                                       */
 typedef struct {

@@ -318,7 +318,7 @@ def test_a_rows_result_does_not_depend_on_other_rows_being_finite(dtype):
 
 
 def test_what_stands_behind_a_rows_end_does_not_count():
-    """Codes behind the last element are zeros by the form; a table made elsewhere may hold others, and rows of a go on in memory."""
+    """Codes behind the last element are zeros by the form, a table made elsewhere may hold others; and rows of a go on in memory."""
     rng = np.random.default_rng(9)
     for K in (1, 100, 130, 250):
         for M in (1, 6, 20, 70):
@@ -328,6 +328,13 @@ def test_what_stands_behind_a_rows_end_does_not_count():
             wide = torch.as_strided(x, (M, K + 130), (K + 140, 1), 1)
             want = binding.group_product(x, q, dtype=torch.float32)
             wide[:, K:] = float("nan")
+            assert torch.equal(binding.group_product(x, q, dtype=torch.float32), want)
+            behind = torch.arange(q.codes.shape[1] * 2) >= K                   # element e of a block: word 4 (e // 8 % 4) + e // 32, half byte 4 (e % 2) + e % 8 // 2
+            e = torch.arange(len(behind))[behind]
+            half = e // 128 * 128 + (4 * (e // 8 % 4) + e % 128 // 32) * 8 + 4 * (e % 2) + e % 8 // 2
+            mask = torch.zeros(len(behind), dtype=torch.uint8)
+            mask[half] = 15
+            q.codes |= (mask[::2] | mask[1::2] << 4).to(DEV)
             assert torch.equal(binding.group_product(x, q, dtype=torch.float32), want)
 
 
