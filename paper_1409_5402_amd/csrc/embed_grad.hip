@@ -34,13 +34,17 @@ constexpr int64_t kSmallTiles = 1 << 22;                             // up to th
 //                         128 89, 80; 400,000 x 192 116, 129; a million x 16 143, 61)
 // and a grid below 2^32 threads: 1024 for every 256 words begun, and every 64 chunks of a row.
 constexpr int64_t kScannedWords = 1 << 18;
-// With dropout the workgroup of a frequent word has the choice for all its rows to make as well, so only up to 4096 tokens go in one launch, and
-// up to 8192 where rows are short or words are many (us, sorted after it: 4096 into 30,000 x 1024 bf16 56, 64, 8192 88, 71; 4000 into 2000 x 128
-// f32 45, 49, 8000 75, 51; 8000 into 2000 x 50 f32 35, 42, 16,000 48, 44; 8000 into 100,000 x 256 f16 54, 76, 16,000 86, 77).
-constexpr int64_t kDroppedTokens = 4096, kDroppedShort = 64;
+// With dropout the workgroup of a frequent word has the choice for all its rows to make as well, so beyond 4096 tokens only short rows, or rows of
+// tables of many words, go in one launch, and beyond 8192 only both (us, sorted after it: 4096 into 30,000 x 1024 bf16 57, 64, 8192 91, 72; 8000
+// into 2000 x 128 f32 36, 53, x 256 54, 39; 8000 into 100,000 x 256 f16 52, 79, 16,000 88, 78; 16,000 into 2000 x 50 f32 48, 45, into 100,000 x
+// 64 39, 64).
+constexpr int64_t kDroppedTokens = 4096;
 bool few_tokens(int64_t n, int64_t rows, const same_lda_rows* grad, bool drop)
 {
-    if (drop && n > kDroppedTokens && (n > kFewerTokens || (grad->width > kDroppedShort && rows <= 4 * n))) return false;
+    if (drop && n > kDroppedTokens) {
+        const bool many = rows > 4 * n;
+        if (n > kFewerTokens ? !(many && grad->width <= 64) : !(many || grad->width <= 128)) return false;
+    }
     const int64_t row_bytes = (int64_t)grad->width * element_bytes(grad->type);
     const bool more = row_bytes <= 2048 && (rows <= kScannedWords || row_bytes > 512);
     return n <= (more ? same::kFewTokens : kFewerTokens) && (rows + 256) * ((grad->width + 63) / 64) < (int64_t)1 << 30;

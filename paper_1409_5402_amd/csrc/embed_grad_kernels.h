@@ -45,13 +45,16 @@ struct GradArgs {
 
 // Which elements of a row of grad count: all, or those that the lookup's dropout kept.  Chunks of V elements, 8 a multiple of V: the 8 / V
 // lanes that hold eight columns share out the rows of a trip, so that a generator's block is made once (131,072 x 333 bf16: each lane for
-// itself 193 us, now 139; without dropout 95).
+// itself 193 us, now 128; without dropout 95).
+// kApart: the blocks one after another and not side by side, for which registers are too few in some kernels (us apart and not: few tokens,
+// V = 8, 4096 x 1024 f32 into bf16 56, 88; V = 4, 8000 x 50 27.2, 26.4; sorted tokens, V = 8, 131,072 x 1024 bf16 145, 140; V = 1, 131,072 x 333
+// bf16 128, 137).
 struct KeepAll {
     static constexpr bool kDrop = false;
     __device__ __forceinline__ KeepAll(const GradArgs&, int) {}
 };
 
-template <int V>
+template <int V, bool kApart>
 struct KeepSome {
     static constexpr bool kDrop = true;
     static constexpr int kShare = 8 / V;
@@ -67,13 +70,21 @@ struct KeepSome {
     __device__ __forceinline__ void rows(uint32_t (&kept)[N], int count, At at, Place place) const
     {
         if (kShare == 1 || N == 1 || !shared) {
+            if constexpr (kApart) {
+                uint64_t all = 0u;                                     // a byte per row
+#pragma unroll 1
+                for (int q = 0; q < count; ++q) all |= (uint64_t)((kept_eight(key, eight, (uint32_t)place(q)) >> (sub * V)) & 255u) << (8 * q);
 #pragma unroll
-            for (int q = 0; q < N; ++q)
-                if (q < count) kept[q] = kept_eight(key, eight, (uint32_t)at(q)) >> (sub * V);
+                for (int q = 0; q < N; ++q) kept[q] = (uint32_t)(all >> (8 * q));
+            } else {
+#pragma unroll
+                for (int q = 0; q < N; ++q)
+                    if (q < count) kept[q] = kept_eight(key, eight, (uint32_t)at(q)) >> (sub * V);
+            }
             return;
         }
         uint32_t lo = 0u, hi = 0u;                                     // a byte per row
-#pragma unroll
+#pragma unroll(kApart ? 1 : 8)
         for (int i = 0; i < (N + kShare - 1) / kShare; ++i) {
             const int q = sub + kShare * i;
             const int32_t row = place(q < count ? q : count - 1);
@@ -97,8 +108,8 @@ struct KeepSome {
     }
 };
 
-template <int V, bool kDrop>
-using Keep = typename std::conditional<kDrop, KeepSome<V>, KeepAll>::type;
+template <int V, bool kDrop, bool kApart>
+using Keep = typename std::conditional<kDrop, KeepSome<V, kApart>, KeepAll>::type;
 
 // acc += the rows at places at(0) .. at(count - 1) of the list, count in [1, N]: all loads before the first addition (at(q) is a
 // place to read from for q >= count too)
@@ -191,7 +202,7 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(GradArgs a)
     const int column = blockIdx.y * lanes + lane;
     const bool mine = column < a.chunks;
     const int c = mine ? column : a.chunks - 1;                     // lanes behind the row's end follow its last chunk and write nothing
-    const Keep<V, kDrop> keep(a, column);
+    const Keep<V, kDrop, (V < 8)> keep(a, column);
     const int64_t item0 = ((int64_t)blockIdx.x << (8 - a.lanes_log2)) + (threadIdx.x >> a.lanes_log2);
     for (int64_t item = item0; item < a.ranges + a.rows; item += (int64_t)gridDim.x << (8 - a.lanes_log2)) {
         if (item < a.ranges) {
@@ -306,9 +317,10 @@ constexpr int kFewTokens = 16384;                                   // 1024 for 
 constexpr int kFewWords = 256;                                      // most words of a workgroup
 constexpr int kColumns = 16;
 
-// (two workgroups per compute unit where 64 registers are enough, which is where V < 8)
+// (two workgroups per compute unit where 64 registers are enough, which is where V < 8; with dropout they are not: 4000 x 128 f32 into 20,000
+// words 55 us, with one 22)
 template <class TI, class TO, int V, int kRows, bool kDrop>
-__global__ __launch_bounds__(1024, V < 8 && kRows == 8 ? 8 : 4) void embed_grad_few_kernel(GradArgs a)
+__global__ __launch_bounds__(1024, V < 8 && kRows == 8 && !kDrop ? 8 : 4) void embed_grad_few_kernel(GradArgs a)
 {
     constexpr int kTokens = 1024 * kRows;
     __shared__ union {
@@ -417,7 +429,7 @@ __global__ __launch_bounds__(1024, V < 8 && kRows == 8 ? 8 : 4) void embed_grad_
     const bool mine = column < a.chunks;
     const int c = mine ? column : a.chunks - 1;
     const TI* const from = static_cast<const TI*>(a.grad) + (int64_t)c * V;
-    const Keep<V, kDrop> keep(a, column);
+    const Keep<V, kDrop, V == 8> keep(a, column);
     // acc += the rows at the sorted positions p .. p_behind - 1
     const auto sum = [&](float (&acc)[V], uint32_t p, uint32_t p_behind) {
         for (; p < p_behind; p += 8) {

@@ -209,7 +209,8 @@ def test_gradient_matches_the_oracle(width, grad, out):
 
 
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
-@pytest.mark.parametrize("n, V, width", [(20_000, 40, 16), (20_000, 30_000, 10), (17_000, 300, 66), (20_001, 500, 9), (18_000, 100, 128), (9_000, 50, 600), (16_384, 3, 24)])
+@pytest.mark.parametrize("n, V, width", [(20_000, 40, 16), (20_000, 30_000, 10), (17_000, 300, 66), (20_001, 500, 9), (18_000, 100, 128), (9_000, 50, 600), (16_384, 3, 24),
+                                         (8_000, 60, 100), (8_192, 3, 128), (8_100, 40_000, 330), (16_000, 70_000, 50), (16_384, 66_000, 9), (16_383, 70_000, 64)])
 def test_gradient_of_sorted_tokens_and_long_runs(n, V, width, grad):
     rng = np.random.default_rng(n + width)
     D = numbers_of(rng, n, width, TYPES[grad]).to(DEV)
