@@ -365,11 +365,11 @@ int same_lda_group_quantize(const same_lda_rows* x, const same_lda_rows* group_o
 
 /* out[i][j] = scale * sum_k a[i][k] * (q_jk s_jk + b_jk): rows of numbers as they are, by a matrix in grouped integers of the same
  * width.  Sums are binary32; of binary32 rows all 24 bits count.  The result is rounded once to the output's type.  Groups
- * are summed as s sum a q + b sum a, so a row of a that is not finite, or one for which the sum of (15 |s| + |b|) |a| is beyond
- * binary32, gives numbers that may be infinite or NaN.
+ * are summed as s sum a q + b sum a, so a row of a that is not finite, or one for which a group's 15 sum |a| or the sum of (15 |s| + |b|) |a|
+ * is beyond binary32, gives numbers that may be infinite or NaN.
  *   a            any number of rows, SAME_LDA_FLOAT, _BFLOAT or _HALF
  *   out          [a->rows][b->rows]
- *   workspace    as many bytes as same_lda_group_product_workspace says for the same matrices (none for few rows), aligned to 16; its
+ *   workspace    as many bytes as same_lda_group_product_workspace says for the same matrices (none for few rows and small products), aligned to 16; its
  *                contents are scratch, in use until the call's kernels have ended                                  */
 int same_lda_group_product_workspace(const same_lda_rows* a, const same_lda_rows* b, size_t* bytes);
 int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float scale, const same_lda_rows* out, void* workspace,

@@ -535,9 +535,9 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
     }
 }
 
-// Few rows of a, up to 16.  A wave keeps its part of them, KB blocks of 128 elements, in registers and goes through the rows of b, 16 at
-// a time, whose codes come straight from memory, those of the next turns while these are multiplied: every byte of b is read once, a once per
-// workgroup.  Bound by memory where rows are long (1 x 50,021 x 4096 bf16: 30 us, 3.6 TB/s of codes and scales; 13 in binary32, G64: 40),
+// Few rows of a, up to 16 a workgroup.  A wave keeps its part of them, KB blocks of 128 elements, in registers and goes through the rows of b, 16 at
+// a time, whose codes come straight from memory, those of the next turns while these are multiplied: every byte of b is read once (for every 16 rows of
+// a where there are more), a once per workgroup.  Bound by memory where rows are long (1 x 50,021 x 4096 bf16: 30 us, 3.6 TB/s of codes and scales; 13 in binary32, G64: 40),
 // by the launch and the one wait for a where they are short (1 x 100,000 x 256 f32, G64: 8.2 us).  Where a row of b has more than KB blocks, waves_per_row waves share it and add up their sums by way of LDS, in order.
 // S depends on a alone; sum_g b_g S_g is a product of its own along the groups, eight in the first lanes of a bfloat16 instruction, S in three
 // pieces.
@@ -557,6 +557,8 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
     const int kw = p.waves_per_row, streams = (int)(blockDim.x >> 6) / kw, stream = wv / kw, mine = wv - stream * kw;
     const int blocks = (p.width + 127) / 128, first = mine * KB;
 
+    const int64_t first_i = (int64_t)blockIdx.y * 16;
+    const int rows_here = p.rows_a - first_i < 16 ? (int)(p.rows_a - first_i) : 16;
     const int64_t tiles = (p.rows_b + 15) / 16, turns = (tiles + streams - 1) / streams;
     struct Codes {
         v4u32 w[KB];
@@ -585,7 +587,7 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
     v4u32 x[KB][4][kKept], sums[kSets][3];
     {
         const int m = kStack ? r & 3 : r;
-        const TI* const row = static_cast<const TI*>(p.a) + (m < p.rows_a ? m : p.rows_a - 1) * p.stride_a;
+        const TI* const row = static_cast<const TI*>(p.a) + (first_i + (m < rows_here ? m : rows_here - 1)) * p.stride_a;
         Eight<TI> raw[KB][4];
 #pragma unroll
         for (int k = 0; k < KB; ++k)
@@ -669,7 +671,7 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int i = 4 * h + q;
-                if (i < p.rows_a && tile * 16 + r < p.rows_b) store_number(p, i, tile * 16 + r, p.scale * acc[q]);
+                if (i < rows_here && tile * 16 + r < p.rows_b) store_number(p, first_i + i, tile * 16 + r, p.scale * acc[q]);
             }
             return;
         }
@@ -678,7 +680,7 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
         __syncthreads();
         for (int e = (int)threadIdx.x - stream * kw * 64; e < 256; e += kw * 64) {
             const int i = e >> 4, j = e & 15;
-            if (i < p.rows_a && tile * 16 + j < p.rows_b) {
+            if (i < rows_here && tile * 16 + j < p.rows_b) {
                 float all = 0.0f;
 #pragma unroll
                 for (int w = 0; w < 8; ++w) {                                  // all on their way at once
@@ -687,7 +689,7 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
                     if constexpr (kStack) y += part[buffer][of][i + 4][j] + part[buffer][of][i + 8][j];
                     all += w < kw ? y : 0.0f;
                 }
-                store_number(p, i, tile * 16 + j, p.scale * all);
+                store_number(p, first_i + i, tile * 16 + j, p.scale * all);
             }
         }
         buffer ^= 1;                                                           // the next turn's sums go elsewhere; the one after it is behind a barrier

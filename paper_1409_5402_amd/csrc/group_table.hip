@@ -22,16 +22,26 @@ int64_t rows_of_a(const same_lda_rows* a)
     return most < 4096 ? 4096 : most > ((int64_t)1 << 24) ? (int64_t)1 << 24 : most;
 }
 
-bool few_rows(const same_lda_rows* a) { return a->rows <= 16 && same::micro_groups(a->width) <= 32; }
+
+// One launch of the kernel that keeps 16 rows of a in registers, or two in tiles: there up to 16 rows, and more while they and the rows of b make no
+// more than so many products of 16 x 16 x 128, for which the table is read again for every 16 (us in one and in two, bf16: 64 x 1000 x 1000 3.9,
+// 9.2; 32 x 4096 x 4096 11.5, 16.0; 512 x 2000 x 500 9.7, 10.0; 64 x 30,000 x 256 9.3, 8.5; 64 x 4096 x 4096 15.9, 16.5; 512 x 4000 x 300 14.5, 9.3;
+// 100 x 8000 x 2000 30, 17; and the second launch and its workspace cost the host 4 to 5).
+constexpr int64_t kFewProducts = 16384;
+bool few_rows(const same_lda_rows* a, const same_lda_rows* b)
+{
+    const int64_t blocks = same::micro_groups(a->width);
+    return blocks <= 32 && (a->rows <= 16 || (a->rows + 15) / 16 * ((b->rows + 15) / 16) * blocks <= kFewProducts);
+}
 
 // Workspace of the rows of a, laid down for tiles of up to 128 rows, and of their sums.
 struct RowsSpace {
     size_t operands, bytes;
 };
 
-RowsSpace rows_space(const same_lda_rows* a)
+RowsSpace rows_space(const same_lda_rows* a, const same_lda_rows* b)
 {
-    if (few_rows(a)) return {0, 0};
+    if (few_rows(a, b)) return {0, 0};
     const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 127) / 128 * 8), filled = (size_t)filled_blocks(a->width);
     const size_t operands = tiles * filled * 4 * (a->type == SAME_LDA_FLOAT ? 3 : 1) * 1024;
     return {operands, operands + tiles * filled * 4 * 16 * sizeof(float)};
@@ -45,7 +55,8 @@ void product_few(same::GroupProductArgs& p, int blocks, hipStream_t st)
     p.waves_per_row = kw;
     const int waves = kw < 4 ? 4 : kw, streams = waves / kw;
     const int64_t turns = ((p.rows_b + 15) / 16 + streams - 1) / streams;
-    hipLaunchKernelGGL((same::group_product_few_kernel<TI, P, kStack, kGroupLog2, KB>), dim3((unsigned)at_most(turns, kComputeUnits * 8 / waves)), dim3(64 * waves), 0, st, p);
+    const int64_t across = (p.rows_a + 15) / 16, most = (kComputeUnits * 8 / waves + across - 1) / across;
+    hipLaunchKernelGGL((same::group_product_few_kernel<TI, P, kStack, kGroupLog2, KB>), dim3((unsigned)at_most(turns, most), (unsigned)across), dim3(64 * waves), 0, st, p);
 }
 
 // Up to two blocks of a row in a wave while eight waves hold the row (us with 1, 2 and 4 of them: 1 x 100,000 x 128 bf16 4.8, 6.5, 10.1;
@@ -169,7 +180,7 @@ int same_lda_group_product_workspace(const same_lda_rows* a, const same_lda_rows
     if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "group_product: bytes is null");
     const int rc = check_product(a, b);
     if (rc) return rc;
-    *bytes = a->rows > 0 && b->rows > 0 ? rows_space(a).bytes : 0;
+    *bytes = a->rows > 0 && b->rows > 0 ? rows_space(a, b).bytes : 0;
     return SAME_LDA_OK;
 }
 
@@ -185,11 +196,11 @@ int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float
                                    (long long)out->rows, out->width);
     if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "group_product: the scale must be finite");
     if (a->rows == 0) return SAME_LDA_OK;
-    const RowsSpace space = rows_space(a);
+    const RowsSpace space = rows_space(a, b);
     if (space.bytes > 0 && (!workspace || workspace_bytes < space.bytes || (uintptr_t)workspace % 16))
         return fail_without_handle(SAME_LDA_EINVAL, "group_product: needs %zu bytes of workspace aligned to 16 (got %zu)", space.bytes, workspace ? workspace_bytes : (size_t)0);
     void* const sums = static_cast<char*>(workspace) + space.operands;
-    const bool few = few_rows(a);
+    const bool few = few_rows(a, b);
     const int64_t rows_each = rows_of_a(a);
     const int group_log2 = __builtin_ctz((unsigned)b->type);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);

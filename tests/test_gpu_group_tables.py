@@ -154,7 +154,11 @@ def test_lookup_of_grouped_rows(width, group, out):
 def tolerance(a, size, q):
     n = q.group * (3 if a.dtype == torch.float32 else 1)
     # s D and b S are at most M: where that is beyond binary32 they may be infinite, and nothing is said of the result
-    return np.where(size < float(torch.finfo(torch.float32).max), (2 * n + 2 * q.scales.shape[1]) * U * size, np.inf)
+    most = float(torch.finfo(torch.float32).max)
+    # a group's D = sum a q, q up to 15, is infinite where 15 sum |a| is beyond binary32, however small the step that it is multiplied with
+    A = np.abs(a.double().cpu().numpy())
+    D = 15.0 * np.pad(A, ((0, 0), (0, -A.shape[1] % q.group))).reshape(A.shape[0], -1, q.group).sum(2).max(axis=1)
+    return np.where((size < most) & (D < most)[:, None], (2 * n + 2 * q.scales.shape[1]) * U * size, np.inf)
 
 
 def product_case(rng, M, N, K, dtype, group, out, scale=1.0, positive=False, a=None):
@@ -178,7 +182,8 @@ def product_case(rng, M, N, K, dtype, group, out, scale=1.0, positive=False, a=N
     return x, q, got
 
 
-SHAPES = [(1, 1, 1), (1, 16, 128), (1, 17, 129), (3, 5, 31), (5, 33, 250), (6, 40, 96), (13, 100, 300), (16, 64, 256), (17, 31, 130), (31, 65, 512), (33, 20, 200), (64, 48, 384), (65, 130, 64), (130, 70, 160)]
+SHAPES = [(1, 1, 1), (1, 16, 128), (1, 17, 129), (3, 5, 31), (5, 33, 250), (6, 40, 96), (13, 100, 300), (16, 64, 256), (17, 31, 130), (31, 65, 512), (33, 20, 200), (64, 48, 384), (65, 130, 64), (130, 70, 160),
+          (1, 17, 4101), (17, 31, 4130), (33, 20, 4200), (65, 130, 4097), (130, 70, 4224)]
 
 
 @pytest.mark.parametrize("group", GROUPS)
@@ -195,6 +200,7 @@ def test_product_matches_the_oracle(M, N, K, dtype, group):
 def test_product_in_every_pair_of_types(dtype, out):
     product_case(np.random.default_rng(5), 9, 50, 190, dtype, 64, out, -1.5)
     product_case(np.random.default_rng(6), 40, 50, 190, dtype, 64, out, -1.5)
+    product_case(np.random.default_rng(7), 40, 50, 4190, dtype, 64, out, -1.5)
 
 
 @pytest.mark.parametrize("M, N, K", [(1, 500, 50), (1, 700, 256), (6, 300, 100), (30, 200, 512), (100, 90, 300)])
@@ -231,7 +237,7 @@ def test_product_of_few_rows_of_every_length(K, M, dtype):
 
 
 @pytest.mark.parametrize("dtype, group", [("f32", 64), ("bf16", 32), ("f16", 128), ("bf16", 64)])
-@pytest.mark.parametrize("M, N, K", [(520, 49_200, 130), (65, 25_000, 200), (50, 12_000, 300), (40, 6400, 300), (33, 700, 1100), (20, 33_000, 260), (20, 600, 520), (7, 300, 4300), (130, 99_000, 70)])
+@pytest.mark.parametrize("M, N, K", [(520, 49_200, 130), (65, 40_000, 200), (50, 12_000, 1100), (40, 6400, 2000), (33, 700, 4200), (20, 33_000, 700), (20, 600, 520), (7, 300, 4300), (130, 99_000, 70), (500, 600, 400)])
 def test_product_in_every_form(M, N, K, dtype, group):
     """Tiles of every size, which the numbers of rows choose: against the product in double on the device, at its bound."""
     rng = np.random.default_rng(M)
@@ -248,7 +254,7 @@ def test_product_in_every_form(M, N, K, dtype, group):
     check()
 
 
-@pytest.mark.parametrize("M, N, K", [(1, 100, 700), (4, 90, 384), (7, 130, 1100), (16, 257, 4224), (33, 200, 900), (200, 300, 640)])
+@pytest.mark.parametrize("M, N, K", [(1, 100, 700), (4, 90, 384), (7, 130, 1100), (16, 257, 4224), (33, 200, 900), (200, 300, 640), (33, 200, 4224), (200, 300, 4160)])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("group", GROUPS)
 def test_product_is_exact_where_binary32_is(group, dtype, M, N, K):
@@ -264,29 +270,31 @@ def test_product_is_exact_where_binary32_is(group, dtype, M, N, K):
     assert torch.equal(got.double().cpu(), a.double() @ w.t())
 
 
+@pytest.mark.parametrize("K", [700, 4300])
 @pytest.mark.parametrize("M", [1, 4, 5, 13, 40, 150])
-def test_rows_in_binary32_count_with_all_their_bits(M):
+def test_rows_in_binary32_count_with_all_their_bits(M, K):
     """One odd integer of 18 bits in each row, which no two 8-bit pieces hold: with codes as they are every sum fits binary32."""
-    K, N = 700, 40
+    N, blocks = 40, -(-K // 128)
     rng = np.random.default_rng(M)
     a = torch.zeros(M, K)
     a[torch.arange(M), torch.from_numpy(rng.integers(0, K, M))] = torch.from_numpy((2 * rng.integers(1 << 16, 1 << 17, M) + 1) * rng.choice([-1, 1], M)).float()
-    codes = torch.from_numpy(rng.integers(0, 256, (N, 384))).to(torch.uint8)
-    scales = torch.zeros(N, 12, 2, dtype=torch.bfloat16)
+    codes = torch.from_numpy(rng.integers(0, 256, (N, 64 * blocks))).to(torch.uint8)
+    scales = torch.zeros(N, 2 * blocks, 2, dtype=torch.bfloat16)
     scales[:, :, 0] = 0.25
     q = binding.GroupMatrix(codes.to(DEV), scales.to(DEV), K, 64)
     w = binding.group_dequantize(q).double().cpu()
     assert torch.equal(binding.group_product(a.to(DEV), q).double().cpu(), a.double() @ w.t())
 
 
-@pytest.mark.parametrize("stride, offset", [(200, 0), (201, 0), (200, 1), (203, 5), (208, 8)])
+@pytest.mark.parametrize("K", [200, 4200])
+@pytest.mark.parametrize("stride, offset", [(0, 0), (1, 0), (0, 1), (3, 5), (8, 8)])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_product_of_strided_rows(dtype, stride, offset):
-    rng = np.random.default_rng(stride)
-    q = binding.group_quantize(numbers_of(rng, 77, 200, torch.float32).to(DEV), 32)
+def test_product_of_strided_rows(dtype, stride, offset, K):
+    rng = np.random.default_rng(200 + stride)
+    q = binding.group_quantize(numbers_of(rng, 77, K, torch.float32).to(DEV), 32)
     for M in (1, 7, 30, 90):
-        X = numbers_of(rng, M, 200, TYPES[dtype])
-        x, _ = guarded(M, 200, TYPES[dtype], stride, offset)
+        X = numbers_of(rng, M, K, TYPES[dtype])
+        x, _ = guarded(M, K, TYPES[dtype], K + stride, offset)
         x.copy_(X)
         want = binding.group_product(X.to(DEV), q)
         assert torch.equal(binding.group_product(x, q), want)
@@ -296,17 +304,18 @@ def test_product_of_strided_rows(dtype, stride, offset):
             check()
 
 
+@pytest.mark.parametrize("K", [300, 4300])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_a_rows_result_does_not_depend_on_other_rows_being_finite(dtype):
+def test_a_rows_result_does_not_depend_on_other_rows_being_finite(dtype, K):
     rng = np.random.default_rng(8)
     for M in (3, 12, 40, 130):
-        x = numbers_of(rng, M, 300, TYPES[dtype])
-        w = numbers_of(rng, 50, 300, torch.float32)
+        x = numbers_of(rng, M, K, TYPES[dtype])
+        w = numbers_of(rng, 50, K, torch.float32)
         good = binding.group_product(x.to(DEV), binding.group_quantize(w.to(DEV), 64))
         w[20, 100] = float("nan")
         q = binding.group_quantize(w.to(DEV), 64)
         y = x.clone()
-        y[1, 299] = float("inf")
+        y[1, K - 1] = float("inf")
         y[2, 0] = float("nan")
         got = binding.group_product(y.to(DEV), q)
         rest = torch.ones(M, dtype=torch.bool)
@@ -320,7 +329,7 @@ def test_a_rows_result_does_not_depend_on_other_rows_being_finite(dtype):
 def test_what_stands_behind_a_rows_end_does_not_count():
     """Codes behind the last element are zeros by the form, a table made elsewhere may hold others; and rows of a go on in memory."""
     rng = np.random.default_rng(9)
-    for K in (1, 100, 130, 250):
+    for K in (1, 100, 130, 250, 4110):
         for M in (1, 6, 20, 70):
             q = binding.group_quantize(numbers_of(rng, 30, K, torch.float32).to(DEV), 32)
             x, _ = guarded(M, K, torch.bfloat16, K + 140, 1)
@@ -340,7 +349,7 @@ def test_what_stands_behind_a_rows_end_does_not_count():
 
 def test_streams_and_graphs_and_repeats():
     rng = np.random.default_rng(10)
-    for M, N, K in [(1, 3000, 1024), (13, 2000, 2048), (200, 700, 512)]:
+    for M, N, K in [(1, 3000, 1024), (13, 2000, 2048), (200, 700, 512), (200, 700, 4200)]:
         x = numbers_of(rng, M, K, torch.bfloat16).to(DEV)
         q = binding.group_quantize(numbers_of(rng, N, K, torch.float32).to(DEV), 64)
         want = binding.group_product(x, q)

@@ -142,13 +142,14 @@ def test_sizes_of_grouped_matrices():
 
 def test_workspaces_of_products_and_of_gradients():
     L, n, m = binding.load(), ctypes.c_size_t(), ctypes.c_size_t()
-    for r, w, t, some in [(1, 4096, F, False), (16, 4096, B, False), (16, 4097, B, True), (17, 8, H, True), (0, 8, F, False), (5000, 1 << 20, F, True), ((1 << 31) - 1, 128, B, True)]:
-        assert L.same_lda_group_product_workspace(ref(rows(rows=r, width=w, type=t)), ref(rows(type=64, width=w)), ref(n)) == 0 and (n.value > 0) == some
+    for r, w, t, words, some in [(1, 4096, F, 1 << 30, False), (16, 4096, B, 4, False), (16, 4097, B, 4, True), (17, 8, H, 131_072, False), (17, 8, H, 131_073, True), (0, 8, F, 4, False),
+                                 (512, 4096, B, 256, False), (512, 4096, B, 257, True), (5000, 1 << 20, F, 4, True), ((1 << 31) - 1, 128, B, (1 << 31) - 1, True)]:
+        assert L.same_lda_group_product_workspace(ref(rows(rows=r, width=w, type=t)), ref(rows(type=64, rows=words, width=w)), ref(n)) == 0 and (n.value > 0) == some
         # rows laid down are 256 MB or 4096 rows, in three pieces of two bytes, and 128 more; sums are 3 KB for 16 rows and 32 groups, whose operands are 16 KB or more
         assert n.value <= (1 + 3 / 16) * max((1 << 28) + (1 << 20), 4096 * (w + 1024) * 6)
     refused(L.same_lda_group_product_workspace(ref(rows()), ref(rows(type=64)), None), "null")
     refused(L.same_lda_group_product_workspace(ref(rows()), ref(rows(type=64, width=9)), ref(n)), "elements")
-    a, g, out = rows(rows=20), rows(type=64), rows(rows=20, width=4)
+    a, g, out = rows(rows=20, width=4200), rows(type=64, width=4200), rows(rows=20, width=4)
     assert L.same_lda_group_product_workspace(ref(a), ref(g), ref(n)) == 0
     for space, size in [(P, n.value - 1), (None, n.value), (P + 8, n.value)]:
         refused(L.same_lda_group_product(ref(a), ref(g), 1.0, ref(out), space, size, None), "workspace")
