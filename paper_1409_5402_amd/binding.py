@@ -439,39 +439,49 @@ class Dropout:
     """Which elements of a matrix are kept: each with probability 1 - p, by its place, the seed and the step alone, so a backward pass that is
     given the same Dropout repeats the forward pass's choice.  `step`: an integer in [0, 2^56), another one for every call whose
     choice is to be another; or a tensor of one int64 element on the GPU, read when the kernel runs (a captured graph that counts it up
-    draws anew in every replay)."""
+    draws anew in every replay).  p, seed and step stay what they are: another step in a number is another Dropout."""
 
-    __slots__ = ("p", "seed", "step", "_packed")
+    __slots__ = ("_p", "_seed", "_step", "_packed")
 
     def __init__(self, p, seed, step=0):
         p = float(p)
         if not 0.0 <= p <= 1.0:
             raise ValueError(f"the probability {p} is not in [0, 1]")
-        at = 0
+        seed = operator.index(seed)
+        if not 0 <= seed < 1 << 64:
+            raise ValueError(f"the seed {seed} is not in [0, 2^64)")
+        self._p, self._seed, self._step, self._packed = p, seed, step, None
         if _is_torch(step):
-            import torch
-            if step.dtype != torch.int64 or step.numel() != 1:
-                raise TypeError(f"a step in a tensor is one int64 element, not {step.numel()} of {step.dtype}")
-            at, count = step.data_ptr(), 0
+            self._pack()
         else:
             count = operator.index(step)
             if not 0 <= count < 1 << 56:
                 raise ValueError(f"the step {count} is not in [0, 2^56)")
-        seed = operator.index(seed)
-        if not 0 <= seed < 1 << 64:
-            raise ValueError(f"the seed {seed} is not in [0, 2^64)")
-        self.p, self.seed, self.step = p, seed, step
-        self._packed = _pack_drop(p, seed, count, at)
+            self._packed = _pack_drop(p, seed, count, 0)
+
+    p = property(lambda self: self._p)
+    seed = property(lambda self: self._seed)
+    step = property(lambda self: self._step)
+
+    def _pack(self) -> bytes:
+        """As a same_lda_drop.  A step in a tensor is looked at in every call: its memory may be another one than before."""
+        if self._packed is not None:
+            return self._packed
+        import torch
+        step = self._step
+        if step.numel() != 1 or step.dtype != torch.int64:
+            raise TypeError(f"a step in a tensor is one int64 element, not {step.numel()} of {step.dtype}")
+        return _pack_drop(self._p, self._seed, 0, step.data_ptr())
 
     def _on(self):
         """The operand among a call's that must be on its GPU: the step's tensor, if it is one."""
-        return None if type(self.step) is int or not _is_torch(self.step) else self.step
+        return None if self._packed is not None else self._step
 
 
 def _drop(drop) -> bytes:
     if type(drop) is not Dropout:
         raise TypeError(f"drop is a Dropout, not a {type(drop).__name__}")
-    return drop._packed
+    return drop._pack()
 
 
 def _type_of(dtype) -> int:

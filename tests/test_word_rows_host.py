@@ -1,5 +1,7 @@
 """Refusals of dropout and of the operators on grouped integers: everything here is found on the host, before any device call."""
+import copy
 import ctypes
+import pickle
 
 import pytest
 import torch
@@ -193,3 +195,37 @@ def test_binding_refuses_what_it_cannot_pass_on():
     assert (v.p, v.seed, v.step, v.step_at) == (0.25, (1 << 64) - 1, 0, s.data_ptr())
     v = Drop.from_buffer_copy(binding._drop(binding.Dropout(0.25, 7, (1 << 56) - 1)))
     assert (v.p, v.seed, v.step, v.step_at) == (0.25, 7, (1 << 56) - 1, None)
+
+
+def test_a_dropout_passes_on_what_it_holds_when_it_is_used():
+    """What is passed to the library is what the object says: its numbers cannot be changed under it, and the address of a step in
+    a tensor is that of the call, also after the tensor has other memory or the object was copied."""
+    d = binding.Dropout(0.5, 7, 2)
+    for name, value in (("p", 0.9), ("seed", 8), ("step", 3)):
+        with pytest.raises(AttributeError):
+            setattr(d, name, value)
+    with pytest.raises(AttributeError):
+        d.step += 1
+    assert (d.p, d.seed, d.step) == (0.5, 7, 2)
+
+    def at(d):
+        v = Drop.from_buffer_copy(binding._drop(d))
+        return v.p, v.seed, v.step, v.step_at
+
+    assert at(d) == (0.5, 7, 2, None) and at(copy.deepcopy(d)) == at(pickle.loads(pickle.dumps(d))) == at(d)
+    s = torch.tensor([5])
+    d = binding.Dropout(0.25, 9, s)
+    assert d.step is s and at(d) == (0.25, 9, 0, s.data_ptr())
+    first, other = s.data_ptr(), torch.tensor([6, 7])
+    s.set_(other.untyped_storage(), 1, (1,))
+    assert first != s.data_ptr() == other.data_ptr() + 8 and at(d) == (0.25, 9, 0, s.data_ptr())
+    s.data = torch.tensor([8])
+    assert at(d) == (0.25, 9, 0, s.data_ptr())
+    e = copy.deepcopy(d)
+    assert e.step is not s and at(e) == (0.25, 9, 0, e.step.data_ptr()) and at(d)[3] == s.data_ptr()
+    s.resize_(2)
+    with pytest.raises(TypeError):            # no step any more
+        binding._drop(d)
+    s.resize_(0)
+    with pytest.raises(TypeError):
+        binding._drop(d)
