@@ -87,19 +87,20 @@ void sort_pass(const same::GradArgs& a, const GradSpace& s, int64_t n, int pass,
     hipLaunchKernelGGL((same::token_place<R, false>), dim3(s.tiles), dim3(256), 0, st, a.tokens, a.rows, a.sorted, n, shift, s.bits, s.tiles, hist, total, to);
 }
 
-int check_grad(const same_lda_rows* grad, const same_lda_rows* table_grad)
+int check_grad(const char* call, const same_lda_rows* grad, const same_lda_rows* table_grad)
 {
-    int rc = check_rows("embed_grad", "grad", grad, kNumbers);
-    if (!rc) rc = check_rows("embed_grad", "table_grad", table_grad, kNumbers);
+    int rc = check_rows(call, "grad", grad, kNumbers);
+    if (!rc) rc = check_rows(call, "table_grad", table_grad, kNumbers);
     if (!rc && grad->width != table_grad->width)
-        rc = fail_without_handle(SAME_LDA_EINVAL, "embed_grad: rows of %d and of %d elements", grad->width, table_grad->width);
+        rc = fail_without_handle(SAME_LDA_EINVAL, "%s: rows of %d and of %d elements", call, grad->width, table_grad->width);
     return rc;
 }
 
 int workspace_of(const same_lda_rows* grad, const same_lda_rows* table_grad, bool drop, size_t* bytes)
 {
-    if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: bytes is null");
-    const int rc = check_grad(grad, table_grad);
+    const char* const call = grad_call_name(drop);
+    if (!bytes) return fail_without_handle(SAME_LDA_EINVAL, "%s: bytes is null", call);
+    const int rc = check_grad(call, grad, table_grad);
     if (rc) return rc;
     *bytes = grad_space(grad, table_grad->rows, drop).bytes;
     return SAME_LDA_OK;
@@ -109,18 +110,19 @@ int workspace_of(const same_lda_rows* grad, const same_lda_rows* table_grad, boo
 int grad_call(const same_lda_rows* grad, const void* tokens, int32_t token_bytes, float scale, const same::Drop* drop, int32_t accumulate,
               const same_lda_rows* table_grad, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
-    int rc = check_grad(grad, table_grad);
-    if (!rc) rc = check_tokens("embed_grad", tokens, token_bytes, grad->rows);
+    const char* const call = grad_call_name(drop);
+    int rc = check_grad(call, grad, table_grad);
+    if (!rc) rc = check_tokens(call, tokens, token_bytes, grad->rows);
     if (rc) return rc;
-    if (!tokens && grad->rows > 0) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: tokens is null");
-    if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: the scale must be finite");
+    if (!tokens && grad->rows > 0) return fail_without_handle(SAME_LDA_EINVAL, "%s: tokens is null", call);
+    if (!std::isfinite(scale)) return fail_without_handle(SAME_LDA_EINVAL, "%s: the scale must be finite", call);
     const int64_t n = grad->rows, rows = table_grad->rows;
     const GradSpace s = grad_space(grad, rows, drop);
     if (rows == 0 || (n == 0 && accumulate)) return SAME_LDA_OK;
     if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes || (uintptr_t)workspace % 16))
-        return fail_without_handle(SAME_LDA_EINVAL, "embed_grad: needs %zu bytes of workspace aligned to 16 (got %zu)", s.bytes, workspace ? workspace_bytes : (size_t)0);
+        return fail_without_handle(SAME_LDA_EINVAL, "%s: needs %zu bytes of workspace aligned to 16 (got %zu)", call, s.bytes, workspace ? workspace_bytes : (size_t)0);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (n == 0) return rows_of_zeros("embed_grad", table_grad, st);
+    if (n == 0) return rows_of_zeros(call, table_grad, st);
     char* const w = static_cast<char*>(workspace);
     same::GradArgs a = {grad->data, grad->stride, nullptr, nullptr, rows, scale, accumulate, table_grad->data, table_grad->stride,
                         nullptr, s.ranges, grad->width, 0, 0, {tokens, token_bytes == 8}, (int32_t)n, 0, 0, drop ? *drop : same::Drop{}};
@@ -136,7 +138,7 @@ int grad_call(const same_lda_rows* grad, const void* tokens, int32_t token_bytes
         }
         if (rows > 4 * n) hipLaunchKernelGGL(same::word_runs_sparse, dim3((unsigned)((rows + 256) / 256)), dim3(256), 0, st, a.sorted, n, rows, start);
         else              hipLaunchKernelGGL(same::word_runs, dim3((unsigned)((n + 256) / 256)), dim3(256), 0, st, a.sorted, n, rows, start);
-        if ((rc = launched("embed_grad"))) return rc;
+        if ((rc = launched(call))) return rc;
         a.start = start;
         a.partial = reinterpret_cast<float*>(w + s.partial);
     }

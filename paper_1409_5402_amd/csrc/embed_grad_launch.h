@@ -10,6 +10,8 @@ namespace host {
 
 constexpr int kFewerTokens = 8192;                                   // most tokens of the smaller of the kernels that take few
 
+inline const char* grad_call_name(bool drop) { return drop ? "embed_dropout_grad" : "embed_grad"; }     // in messages
+
 template <class TI, class TO, int V, bool kDrop>
 int grad_launch(GradArgs& a, hipStream_t st)
 {
@@ -31,7 +33,7 @@ int grad_launch(GradArgs& a, hipStream_t st)
         a.words = (int32_t)((units + workgroups - 1) / workgroups << a.unit_log2);
         if (a.n <= kFewerTokens) hipLaunchKernelGGL((embed_grad_few_kernel<TI, TO, V, kFewerTokens / 1024, kDrop>), dim3((unsigned)workgroups, across), dim3(1024), 0, st, a);
         else                     hipLaunchKernelGGL((embed_grad_few_kernel<TI, TO, V, kFewTokens / 1024, kDrop>), dim3((unsigned)workgroups, across), dim3(1024), 0, st, a);
-        return launched("embed_grad");
+        return launched(grad_call_name(kDrop));
     }
     const dim3 grid((unsigned)at_most((a.ranges + a.rows + per - 1) / per, most), across);
     if (a.lanes_log2 < 4) hipLaunchKernelGGL((embed_grad_kernel<TI, TO, V, true, kDrop>), grid, dim3(256), 0, st, a);
@@ -40,7 +42,7 @@ int grad_launch(GradArgs& a, hipStream_t st)
     const int64_t items = (int64_t)1024 >> a.lanes_log2;             // ranges of a workgroup
     const unsigned columns = (unsigned)((a.chunks + (1 << a.lanes_log2) - 1) >> a.lanes_log2), deep = (columns + 65534) / 65535;   // 65,535 of them side by side
     hipLaunchKernelGGL((embed_grad_join_kernel<TO, V>), dim3((unsigned)((a.ranges + items - 1) / items), (columns + deep - 1) / deep, deep), dim3(1024), 0, st, a);
-    return launched("embed_grad");
+    return launched(grad_call_name(kDrop));
 }
 
 template <class TI, class TO, bool kDrop>

@@ -229,3 +229,21 @@ def test_a_dropout_passes_on_what_it_holds_when_it_is_used():
     s.resize_(0)
     with pytest.raises(TypeError):
         binding._drop(d)
+
+
+def test_refusals_name_the_call_that_was_made():
+    L, a, n = binding.load(), rows(), ctypes.c_size_t()
+    many = rows(rows=50_000)
+    for drop, name in ((Drop(0.5, 1, 2, None), "embed_dropout_grad: "), (None, "embed_grad: ")):
+        def call(g, tokens, size, scale, t, space, bytes):
+            if drop is None:
+                return L.same_lda_embed_grad(g, tokens, size, scale, 0, t, space, bytes, None)
+            return L.same_lda_embed_dropout_grad(g, tokens, size, scale, ref(drop), 0, t, space, bytes, None)
+        space = L.same_lda_embed_grad_workspace if drop is None else L.same_lda_embed_dropout_grad_workspace
+        ok = (ref(a), P, 4, 1.0, ref(a), P, 1 << 30)
+        for at, value in [(0, None), (4, None), (0, ref(rows(type=5))), (4, ref(rows(type=64))), (4, ref(rows(width=7))), (2, 2), (1, P + 2), (1, None), (3, float("nan"))]:
+            refused(call(*ok[:at], value, *ok[at + 1:]), name)
+        for at, bytes in ((P, 0), (None, 1 << 30), (P + 8, 1 << 30)):
+            refused(call(ref(many), P, 4, 1.0, ref(a), at, bytes), name, "workspace")
+        for bad in [(None, ref(a), ref(n)), (ref(a), ref(rows(width=7)), ref(n)), (ref(a), ref(a), None)]:
+            refused(space(*bad), name)
