@@ -19,12 +19,12 @@ __device__ __forceinline__ float from_bfloat_bits(uint32_t b) { return __uint_as
 // Word of the chunk c of eight elements among the words of a row.
 __host__ __device__ constexpr int group_word(int c) { return (c & ~15) | ((c & 3) << 2) | ((c >> 2) & 3); }
 
-// The eight elements of a word: q s + b in binary32, rounded once (q s is exact).
+// The eight elements of a word: q s + b in binary32, rounded once (q s has at most twelve bits, but may be beyond binary32 where the sum is not).
 __device__ __forceinline__ void grouped_numbers(float (&x)[8], uint32_t word, uint32_t sb)
 {
     const float s = from_bfloat_bits(sb & 0xFFFFu), b = __uint_as_float(sb & 0xFFFF0000u);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)((word >> (4 * (e >> 1) + 16 * (e & 1))) & 15u) * s + b;
+    for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf((float)((word >> (4 * (e >> 1) + 16 * (e & 1))) & 15u), s, b);
 }
 
 }  // namespace same
