@@ -357,7 +357,7 @@ int same_lda_micro_product(const same_lda_rows* a, const same_lda_rows* b, float
 int same_lda_group_size(int64_t rows, int32_t width, int32_t group, size_t* code_bytes, size_t* scale_bytes);
 
 /* x in grouped integers.  Of a group's least and largest number b is the least rounded down to bfloat16 (not below its least finite
- * number, which leaves s below 0 where all are below that), s = (largest - b) / 15 rounded to binary32 and on to bfloat16 (the next lower one where b + 15 s would be beyond binary32), and
+ * number, which leaves s below 0 where all are below that), s = (largest - b) / 15 rounded to binary32 and on to bfloat16 (the next one towards zero where b + 15 s would be beyond binary32, so what is finite is read back as finite binary32 numbers), and
  * an element is the nearest of b, b + s, .. b + 15 s, ties to the even q (s = 0: q = 0).  A group that holds an infinity or a NaN
  * becomes NaN as a whole (s, b NaN, codes 0).  Where numbers are of one sign this form has 16 sizes, the microscaled one
  * eight.                                                                                                          */

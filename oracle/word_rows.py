@@ -4,7 +4,8 @@
     kept            element (i, j) is kept where 32 bits r_ij < round((1 - p) 2^32); r_ij from Philox4x32-10 at its place
     dropout         scale / (1 - p) * x where kept, else 0
     embed_dropout_grad   G_w = scale / (1 - p) * sum over t_i = w of grad_i where kept
-    group_quantize  per group of a row: b = the least number rounded down to bfloat16, s = bfloat16(binary32((largest - b) / 15)),
+    group_quantize  per group of a row: b = the least number rounded down to bfloat16, s = bfloat16(binary32((largest - b) / 15)), the next
+                    one towards zero where b + 15 s is beyond binary32,
                     q = nearest integer to (x - b) / s, ties to even, in 0 .. 15
     group_product   scale * sum_k a_ik (q_jk s + b)
 """
@@ -80,7 +81,7 @@ def _bf16_down(x):
 
 
 def _bf16_nearest(f):
-    """A positive binary32 number to the nearest bfloat16, ties to even."""
+    """A binary32 number to the nearest bfloat16, ties to even."""
     b = int(np.float32(f).view(np.uint32))
     b = (b + 0x7FFF + ((b >> 16) & 1)) & 0xFFFF0000
     return float(np.uint32(b).view(np.float32))
@@ -100,7 +101,7 @@ def group_quantize(x, group):
                 continue
             b = _bf16_down(v.min())
             s = _bf16_nearest(np.float32((v.max() - b) / 15.0))
-            if b + 15.0 * s > float(np.finfo(np.float32).max):
+            if abs(b + 15.0 * s) > float(np.finfo(np.float32).max):      # the next one towards zero
                 s = float((np.float32(s).view(np.uint32) - np.uint32(0x10000)).view(np.float32))
             step[i, g], base[i, g] = s, b
             if s != 0:                                # (below 0 where all numbers are below the least finite bfloat16)

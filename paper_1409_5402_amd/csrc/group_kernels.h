@@ -102,7 +102,7 @@ __device__ __forceinline__ void group_round(const GroupQuantizeArgs& a, Eight<TI
         const bool ordinary = range >= 1e-30f && range <= 1e30f;
         if (!(ordinary && abs(border) > 4)) {
             step_bits = __float_as_uint((float)(__bf16)(float)(((double)most - (double)base) / 15.0)) >> 16;
-            if ((double)base + 15.0 * (double)from_bfloat_bits(step_bits) > 3.4028234663852886e38) --step_bits;
+            if (fabs((double)base + 15.0 * (double)from_bfloat_bits(step_bits)) > 3.4028234663852886e38) --step_bits;      // towards zero
         }
         const float step = from_bfloat_bits(step_bits);
         sb = __float_as_uint(base) | step_bits;

@@ -44,3 +44,20 @@ def test_a_group_whose_span_is_beyond_binary32_is_read_back(group):
     x[3:6] *= 0.99
     x[6] = np.where(rng.uniform(size=300) < 0.1, 3.2e38, -3.2e38)
     read_back(torch.from_numpy(x).float(), group)
+
+
+@pytest.mark.parametrize("group", GROUPS)
+def test_groups_beyond_the_last_finite_bfloat16_numbers_are_read_back(group):
+    """Groups that lie wholly below the least one have a step below 0, and b + 15 s stays within binary32 there too."""
+    rng = np.random.default_rng(group)
+    low = -wr.BF16_MAX
+    x = np.zeros((10, 300))
+    x[0], x[1], x[2] = -TOP, TOP, (low - TOP) / 2
+    x[3] = np.linspace(-TOP, low, 300)
+    x[4] = np.linspace(-low, TOP, 300)
+    x[5, ::2] = -TOP
+    x[6, ::2] = TOP
+    x[7] = low
+    x[8] = -low
+    x[9] = rng.uniform(-TOP, low, 300)
+    read_back(torch.from_numpy(x).float(), group)

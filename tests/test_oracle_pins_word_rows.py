@@ -114,3 +114,24 @@ def test_predictive_weights_of_grouped_models(K, alpha, beta, group):
     far = np.abs(theta @ numbers.T - want)
     assert np.all(far <= 1.000001 * theta @ bound.T + 1e-40)
     assert 0.005 < far.sum() / want.sum() < 0.06
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_groups_at_either_end_of_binary32_stand_for_finite_numbers(group):
+    """b + 15 s is at most binary32's largest number in magnitude, also where a group lies below the least finite bfloat16 number and s
+    is below 0; the reading is within a step of the number, or, of numbers below the least finite bfloat16 number b, at b."""
+    top = float(np.finfo(np.float32).max)
+    low = -wr.BF16_MAX
+    x = np.zeros((6, 128))
+    x[0] = -top
+    x[1] = np.linspace(-top, low, 128)
+    x[2] = (low - top) / 2
+    x[3] = top
+    x[4] = np.linspace(-low, top, 128)
+    x[5, ::2], x[5, 1::2] = -top, top
+    x = x.astype(np.float32).astype(np.float64)
+    q, step, base = wr.group_quantize(x, group)
+    read = wr.group_numbers(q, step, base, 128)
+    assert np.all(np.abs(base + 15.0 * step) <= top) and np.all(np.abs(read) <= top)
+    assert np.all(step[0] < 0) and np.all(np.abs(read - x) <= np.maximum(np.repeat(np.abs(step), group, axis=1), top + low))
+    assert np.all(read[0] == base[0, 0] + 15.0 * step[0, 0])
