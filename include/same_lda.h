@@ -364,9 +364,9 @@ int same_lda_group_size(int64_t rows, int32_t width, int32_t group, size_t* code
 int same_lda_group_quantize(const same_lda_rows* x, const same_lda_rows* group_out, void* hip_stream);
 
 /* out[i][j] = scale * sum_k a[i][k] * (q_jk s_jk + b_jk): rows of numbers as they are, by a matrix in grouped integers of the same
- * width.  Sums are binary32; of binary32 rows all 24 bits count.  The result is rounded once to the output's type.  Groups
- * are summed as s sum a q + b sum a, so a row of a that is not finite, or one for which a group's 15 sum |a| or the sum of (15 |s| + |b|) |a|
- * is beyond binary32, gives numbers that may be infinite or NaN.
+ * width.  Sums are binary32; of binary32 rows all 24 bits count (of numbers below 2^-109 in a row whose largest is 2^-64 or more, those down to
+ * 2^-133).  The result is rounded once to the output's type.  Groups are summed as s sum a q + b sum a, so a row of a that is not finite, one for
+ * which the sum of (15 |s| + |b|) |a| is beyond binary32, or one in bfloat16 for which a group's 15 sum |a| is, gives numbers that may be infinite or NaN.
  *   a            any number of rows, SAME_LDA_FLOAT, _BFLOAT or _HALF
  *   out          [a->rows][b->rows]
  *   workspace    as many bytes as same_lda_group_product_workspace says for the same matrices (none for few rows and small products), aligned to 16; its

@@ -194,6 +194,11 @@ __global__ __launch_bounds__(256) void group_quantize_kernel(GroupQuantizeArgs a
 // with 16-bit numbers are exact.  With D = sum a q and S = sum a over a group, both summed by matrix instructions in binary32 (S
 // with a second operand of ones), the group adds s D + b S.  Rows in binary32 are cut into three bfloat16 numbers of eight bits
 // each, whose sum they are, and take three instructions.
+//
+// bfloat16 ends at 2^-133, so what a number has below that is not in its pieces, and 15 S is beyond binary32 where S is not far from its end.  Rows in
+// binary32 are therefore multiplied by a power of two before they are cut where their largest number is below 2^-64 (up to [2^-31, 2^-30): all bits are
+// above 2^-133 then, and no sum is beyond binary32, of 2^20 products with 2^132 either) or not below 2^112 (down to [2^111, 2^112)), and the result
+// by its inverse.  Other rows stay as they are: their sums would lose bits at one end for what they gain at the other.
 typedef float v4f32 __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
 typedef _Float16 v8f16 __attribute__((ext_vector_type(8)));
@@ -268,6 +273,31 @@ __device__ __forceinline__ v4f32 mfma_16(v4u32 a, v4u32 b, v4f32 c)
     else                 return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf16, a), __builtin_bit_cast(v8bf16, b), c, 0, 0, 0);
 }
 
+// The largest magnitude of x, y and z, of which NaN has none.
+__device__ __forceinline__ float largest3(float x, float y, float z)
+{
+    float r;
+    asm("v_max3_f32 %0, |%1|, |%2|, |%3|" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ float largest(float most, const float (&x)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 2) most = largest3(most, x[j], x[j + 1]);
+    return most;
+}
+
+// The power of two, as its exponent, for a row whose largest magnitude is `most`: in -16 .. 118, 0 for zero, an infinity and NaN.
+__device__ __forceinline__ int power_for(float most)
+{
+    const int e = __builtin_amdgcn_frexp_expf(most);                           // most is in [2^(e - 1), 2^e)
+    return e < -63 ? -30 - e : e > 112 ? 112 - e : 0;
+}
+
+__device__ __forceinline__ float two_to(int power) { return __uint_as_float((uint32_t)(127 + power) << 23); }
+
 // Eight numbers in binary32 as three operands of bfloat16 numbers that add up to them, element j and j + 4 in a register: the upper eight
 // bits of what is left, which leaves the rest exactly.
 __device__ __forceinline__ void three_pieces(v4u32 (&out)[3], const float (&from)[8])
@@ -309,7 +339,11 @@ __device__ __forceinline__ v4u32 all_ones()
 }
 
 // Any number of rows, in two launches.  The first one lays the rows of a down as the lanes of the matrix instruction take them, cut into pieces
-// and filled up with zeros: per 16 rows and block of 128 elements 4 P operands of 1 KB; and the sums S of their groups.
+// and filled up with zeros: per 16 rows and block of 128 elements 4 P operands of 1 KB; and the sums S of their groups.  Rows in binary32 need
+// their largest number first: those of up to kWholeBlocks blocks are taken whole by one workgroup, of longer ones another launch before it finds the
+// powers of two.
+constexpr int kWholeBlocks = 8;
+
 struct GroupRowsArgs {
     const void* a;
     int64_t rows_a, stride_a;
@@ -317,26 +351,73 @@ struct GroupRowsArgs {
     int32_t blocks, filled;          // of 128 elements in a row; with those that are zeros
     v4u32* operands;                 // [16 rows][filled][4][P][64]
     float* sums;                     // [16 rows][filled][groups of a block][16]
+    float* inverse;                  // [16 rows][16]: of rows in binary32, the inverse of their power of two
 };
 
-template <class TI, int kGroupLog2>
-__global__ __launch_bounds__(256) void group_rows_kernel(GroupRowsArgs a)
+// A workgroup per row, those that fill up the last 16 too.
+__global__ __launch_bounds__(256) void group_row_powers_kernel(GroupRowsArgs a)
+{
+    __shared__ float of_wave[4];
+    const int64_t i = (int64_t)blockIdx.x < a.rows_a ? blockIdx.x : a.rows_a - 1;
+    const float* const row = static_cast<const float*>(a.a) + i * a.stride_a;
+    float most = 0.0f;
+    for (int at = (int)threadIdx.x * 8; at < a.width; at += 4 * 2048) {
+        Eight<float> x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = eight_at(row, at + u * 2048, a.width);       // behind the row's end: its last eight again
+#pragma unroll
+        for (int u = 0; u < 4; ++u) most = largest(most, x[u].v);
+    }
+    for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) a.inverse[blockIdx.x] = two_to(-power_for(largest(0.0f, of_wave)));
+}
+
+// kWhole: the workgroup's waves have a block each of all that there are.
+template <class TI, int kGroupLog2, bool kWhole>
+__global__ __launch_bounds__(kWhole ? 64 * kWholeBlocks : 256) void group_rows_kernel(GroupRowsArgs a)
 {
     constexpr bool kHalf = kHalfMatrix<TI>;
     constexpr int P = sizeof(TI) == 4 ? 3 : 1, kPer = 128 >> kGroupLog2, kSteps = 4 / kPer;             // groups of a block, instructions per group
-    const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    static_assert(!kWhole || P == 3, "only rows in binary32 need a whole row");
+    __shared__ float of_wave[kWhole ? kWholeBlocks : 1][16];
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, waves = blockDim.x >> 6, r = lane & 15, h = lane >> 4;
     const int64_t tile = blockIdx.x;
     const int64_t i = tile * 16 + r < a.rows_a ? tile * 16 + r : a.rows_a - 1;         // rows behind the last one: it again
     const TI* const row = static_cast<const TI*>(a.a) + i * a.stride_a;
-    for (int k = blockIdx.y * 4 + (threadIdx.x >> 6); k < a.filled; k += gridDim.y * 4) {
+    for (int k = blockIdx.y * waves + wv; k < a.filled; k += gridDim.y * waves) {
         Eight<TI> raw[4] = {};
         if (k < a.blocks)
 #pragma unroll
             for (int t = 0; t < 4; ++t) raw[t] = eight_at(row, k * 128 + 32 * t + 8 * h, a.width);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) cut_eight(raw[t], k * 128 + 32 * t + 8 * h, a.width);
+        if constexpr (P == 3) {
+            float factor;
+            if constexpr (kWhole) {                                                    // as many waves as blocks: all of them get here, once
+                float most = 0.0f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) most = largest(most, raw[t].v);
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                if (h == 0) of_wave[wv][r] = most;
+                __syncthreads();
+                for (int w = 0; w < waves; ++w) most = fmaxf(most, of_wave[w][r]);
+                const int power = power_for(most);
+                factor = two_to(power);
+                if (threadIdx.x < 16) a.inverse[tile * 16 + r] = two_to(-power);
+            } else {
+                factor = __uint_as_float(0x7F000000u - __float_as_uint(a.inverse[tile * 16 + r]));       // 2^p from 2^-p: 254 less the exponent's bits
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) raw[t].v[j] *= factor;
+        }
         v4f32 total[kPer] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            cut_eight(raw[t], k * 128 + 32 * t + 8 * h, a.width);
             v4u32 c[P];
             pieces_of<TI, P>(c, raw[t]);
 #pragma unroll
@@ -363,6 +444,7 @@ struct GroupTilesArgs {
     GroupProductArgs p;
     const v4u32* operands;
     const float* sums;
+    const float* inverse;
     int32_t blocks, filled;          // filled: a multiple of WK
 };
 
@@ -386,6 +468,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
         float out[WK > 1 ? WK - 1 : 1][WK > 1 ? MT * NT * 4 : 1][WK > 1 ? 64 * WM * WN : 1];
         float strip[WM * WN][16 * MT][16 * NT + 4];
     } lds;
+    __shared__ v4f32 inverse[P == 3 ? 16 : 1];                                         // of up to 64 rows
+    static_assert(P != 3 || 16 * MT * WM <= 64, "a piece of 64 rows");
     const GroupProductArgs& p = a.p;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
     const int wk = wv / (WM * WN), wm = wv / WN % WM, wn = wv % WN;
@@ -445,6 +529,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
             to_lds_4(uniform(sums + (int64_t)t * (WK * kPer * 64)), sum_at[f], &to.sums[min((f * kWaves + wv) * 64, kSums < 64 ? 0 : kSums - 64)]);
     };
     static_assert(kWide * kPer % 64 == 0 && (kSums < 64 || kSums % 64 == 0), "a piece of scales is of one block, of sums a whole one");
+    if constexpr (P == 3)
+        if (wv == 0) to_lds_4(uniform(reinterpret_cast<const uint8_t*>(a.inverse + first_i)), 4 * min(lane, kTall - 1), inverse);
 #pragma unroll
     for (int f = 0; f + 1 < kStages; ++f) fetch(f);
 
@@ -520,11 +606,14 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
     // by way of LDS, so that a lane stores eight numbers of one row
     auto& strip = lds.strip[wm * WN + wn];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m) {
+        v4f32 back = {1.0f, 1.0f, 1.0f, 1.0f};
+        if constexpr (P == 3) back = inverse[(wm * MT + m) * 4 + h];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) strip[16 * m + 4 * h + q][16 * n + r] = p.scale * acc[m][n][q];
+            for (int q = 0; q < 4; ++q) strip[16 * m + 4 * h + q][16 * n + r] = p.scale * (P == 3 ? acc[m][n][q] * back[q] : acc[m][n][q]);
+    }
     asm volatile("" ::: "memory");                                                     // a wave's accesses to LDS are done in their order
     const int col = lane % (2 * NT) * 8, count = p.rows_b - (j0 + col) < 8 ? (int)(p.rows_b - (j0 + col)) : 8;
     const int rows_here = p.rows_a - i0 < 16 * MT ? (int)(p.rows_a - i0) : 16 * MT;
@@ -553,6 +642,8 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
     constexpr int kKept = kAside ? 2 : P;
     __shared__ float part[2][8][16][17];                                       // [turn][wave][row of a][row of b]
     __shared__ v4u32 aside[kAside ? 8 : 1][kAside ? KB * 4 : 1][64];
+    constexpr bool kPowers = sizeof(TI) == 4;                                  // each wave's part of a row by a power of two of its own
+    float back[kPowers ? 4 : 1];                                               // the inverses for its sums
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
     const int kw = p.waves_per_row, streams = (int)(blockDim.x >> 6) / kw, stream = wv / kw, mine = wv - stream * kw;
     const int blocks = (p.width + 127) / 128, first = mine * KB;
@@ -594,6 +685,31 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
 #pragma unroll
             for (int t = 0; t < 4; ++t) raw[k][t] = eight_at(row, (first + k) * 128 + 32 * t + 8 * h, p.width);
         load(ring[0], blockIdx.x);                                             // behind the rows of a, which are waited for first
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) cut_eight(raw[k][t], (first + k) * 128 + 32 * t + 8 * h, p.width);
+        if constexpr (kPowers) {
+            float most = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) most = largest(most, raw[k][t].v);
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const int power = power_for(most);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) back[q] = two_to(-__shfl(power, 4 * h + q));
+            if (__any(power != 0)) {
+                const float factor = two_to(power);
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) raw[k][t].v[j] *= factor;
+            }
+        }
         v4f32 total[kSets * 8];
 #pragma unroll
         for (int g = 0; g < kSets * 8; ++g) total[g] = v4f32{};
@@ -601,7 +717,6 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
         for (int k = 0; k < KB; ++k)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                cut_eight(raw[k][t], (first + k) * 128 + 32 * t + 8 * h, p.width);
                 v4u32 c[sizeof(TI) == 4 ? 3 : 1];
                 pieces_of(c, raw[k][t]);
                 if constexpr (kStack) {
@@ -660,6 +775,9 @@ __global__ __launch_bounds__(512, 2) void group_product_few_kernel(GroupProductA
 #pragma unroll
                 for (int q = 0; q < 4; ++q) acc[q] = __builtin_fmaf(step, d[q], acc[q]);
             }
+        if constexpr (kPowers)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[q] *= back[q];
         const int64_t tile = turn * streams + stream;
         if (kw == 1) {                                                         // the same for the whole launch
             if constexpr (kStack)

@@ -34,18 +34,25 @@ bool few_rows(const same_lda_rows* a, const same_lda_rows* b)
     return blocks <= 32 && (a->rows <= 16 || (a->rows + 15) / 16 * ((b->rows + 15) / 16) * blocks <= kFewProducts);
 }
 
-// Workspace of the rows of a, laid down for tiles of up to 128 rows, and of their sums.
+// Workspace of the rows of a, laid down for tiles of up to 128 rows, of their sums and, in binary32, of the inverses of their powers of two.
 struct RowsSpace {
-    size_t operands, bytes;
+    size_t operands, sums, bytes;
 };
 
 RowsSpace rows_space(const same_lda_rows* a, const same_lda_rows* b)
 {
-    if (few_rows(a, b)) return {0, 0};
+    if (few_rows(a, b)) return {0, 0, 0};
     const size_t tiles = (size_t)((at_most(a->rows, rows_of_a(a)) + 127) / 128 * 8), filled = (size_t)filled_blocks(a->width);
     const size_t operands = tiles * filled * 4 * (a->type == SAME_LDA_FLOAT ? 3 : 1) * 1024;
-    return {operands, operands + tiles * filled * 4 * 16 * sizeof(float)};
+    const size_t sums = tiles * filled * 4 * 16 * sizeof(float);
+    return {operands, sums, operands + sums + (a->type == SAME_LDA_FLOAT ? tiles * 16 * sizeof(float) : 0)};
 }
+
+// Where rows of a are laid down.
+struct Laid {
+    same::v4u32* operands;
+    float *sums, *inverse;
+};
 
 template <class TI, int P, bool kStack, int kGroupLog2, int KB>
 void product_few(same::GroupProductArgs& p, int blocks, hipStream_t st)
@@ -71,22 +78,30 @@ void product_few_by_width(same::GroupProductArgs& p, int blocks, hipStream_t st)
 }
 
 template <class TI, int kGroupLog2, int MT, int NT, int WM, int WN, int WK, int kStages>
-void product_tiles(const same::GroupProductArgs& p, void* operands, void* sums, hipStream_t st)
+void product_tiles(const same::GroupProductArgs& p, const Laid& to, hipStream_t st)
 {
     constexpr int P = sizeof(TI) == 4 ? 3 : 1, kTall = 16 * MT * WM, kWide = 16 * NT * WN;
     static_assert(WK <= 4 && kTall <= 128, "the workspace is for these");
     constexpr int kFit = kStages * sizeof(same::GroupStage<P, kGroupLog2, MT, NT, WM, WN, WK>) <= 163840 ? kStages : kStages - 1;
     const int blocks = (p.width + 127) / 128, filled = (blocks + WK - 1) / WK * WK;
     const int64_t tiles_a = (p.rows_a + kTall - 1) / kTall, tiles_b = ((p.rows_b + kWide - 1) / kWide + 7) / 8 * 8;
-    const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, static_cast<same::v4u32*>(operands), static_cast<float*>(sums)};
-    hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2>), dim3((unsigned)(tiles_a * MT * WM), (unsigned)at_most((filled + 3) / 4, 65535)), dim3(256), 0, st, rows);
-    const same::GroupTilesArgs tiles = {p, static_cast<const same::v4u32*>(operands), static_cast<const float*>(sums), blocks, filled};
+    const same::GroupRowsArgs rows = {p.a, p.rows_a, p.stride_a, p.width, blocks, filled, to.operands, to.sums, to.inverse};
+    const unsigned sixteens = (unsigned)(tiles_a * MT * WM);
+    bool whole = false;
+    if constexpr (P == 3) {
+        if ((whole = filled <= same::kWholeBlocks))
+            hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2, true>), dim3(sixteens), dim3((unsigned)(64 * filled)), 0, st, rows);
+        else
+            hipLaunchKernelGGL(same::group_row_powers_kernel, dim3(16 * sixteens), dim3(256), 0, st, rows);
+    }
+    if (!whole) hipLaunchKernelGGL((same::group_rows_kernel<TI, kGroupLog2, false>), dim3(sixteens, (unsigned)at_most((filled + 3) / 4, 65535)), dim3(256), 0, st, rows);
+    const same::GroupTilesArgs tiles = {p, to.operands, to.sums, to.inverse, blocks, filled};
     hipLaunchKernelGGL((same::group_product_kernel<same::kHalfMatrix<TI>, P, kGroupLog2, MT, NT, WM, WN, WK, kFit>), dim3((unsigned)(tiles_a * tiles_b)), dim3(64 * WM * WN * WK), 0, st,
                        tiles);
 }
 
 template <class TI, int kGroupLog2>
-void product_launch(same::GroupProductArgs& p, bool few, void* operands, void* sums, hipStream_t st)
+void product_launch(same::GroupProductArgs& p, bool few, const Laid& to, hipStream_t st)
 {
     const int blocks = (p.width + 127) / 128;
     if (few) {
@@ -107,27 +122,27 @@ void product_launch(same::GroupProductArgs& p, bool few, void* operands, void* s
     const auto tiles = [&](int64_t tall, int64_t wide) { return ((p.rows_a + tall - 1) / tall) * ((p.rows_b + wide - 1) / wide); };
     const auto rounds = [&](int64_t tall, int64_t wide, int64_t per_unit) { return (tiles(tall, wide) + per_unit * kComputeUnits - 1) / (per_unit * kComputeUnits); };
     if constexpr (sizeof(TI) == 4) {
-        if (p.rows_a > 32 && 17 * rounds(64, 256, 1) <= 10 * rounds(32, 128, 2)) product_tiles<TI, kGroupLog2, 2, 4, 2, 4, 1, 2>(p, operands, sums, st);
-        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 2>(p, operands, sums, st);
-        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits / 2) product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 2, 2>(p, operands, sums, st);
-        else                                                         product_tiles<TI, kGroupLog2, 1, 2, 1, 2, 4, 2>(p, operands, sums, st);
+        if (p.rows_a > 32 && 17 * rounds(64, 256, 1) <= 10 * rounds(32, 128, 2)) product_tiles<TI, kGroupLog2, 2, 4, 2, 4, 1, 2>(p, to, st);
+        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 2>(p, to, st);
+        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits / 2) product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 2, 2>(p, to, st);
+        else                                                         product_tiles<TI, kGroupLog2, 1, 2, 1, 2, 4, 2>(p, to, st);
     } else {
-        if (p.rows_a > 32 && 5 * rounds(64, 256, 2) <= 4 * rounds(64, 128, 3)) product_tiles<TI, kGroupLog2, 4, 4, 1, 4, 1, 2>(p, operands, sums, st);
-        else if (p.rows_a > 32 && tiles(64, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 4, 2, 1, 4, 1, 2>(p, operands, sums, st);
-        else if (p.rows_a > 32 && tiles(64, 64) > kComputeUnits / 2) product_tiles<TI, kGroupLog2, 4, 2, 1, 2, 2, 3>(p, operands, sums, st);
-        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 4>(p, operands, sums, st);
-        else if (p.rows_a > 16)                                      product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 4, 3>(p, operands, sums, st);
-        else                                                         product_tiles<TI, kGroupLog2, 1, 2, 1, 4, 1, 4>(p, operands, sums, st);
+        if (p.rows_a > 32 && 5 * rounds(64, 256, 2) <= 4 * rounds(64, 128, 3)) product_tiles<TI, kGroupLog2, 4, 4, 1, 4, 1, 2>(p, to, st);
+        else if (p.rows_a > 32 && tiles(64, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 4, 2, 1, 4, 1, 2>(p, to, st);
+        else if (p.rows_a > 32 && tiles(64, 64) > kComputeUnits / 2) product_tiles<TI, kGroupLog2, 4, 2, 1, 2, 2, 3>(p, to, st);
+        else if (p.rows_a > 16 && tiles(32, 64) > kComputeUnits)     product_tiles<TI, kGroupLog2, 2, 2, 1, 4, 1, 4>(p, to, st);
+        else if (p.rows_a > 16)                                      product_tiles<TI, kGroupLog2, 2, 2, 1, 2, 4, 3>(p, to, st);
+        else                                                         product_tiles<TI, kGroupLog2, 1, 2, 1, 4, 1, 4>(p, to, st);
     }
 }
 
 template <class TI>
-void product_to(same::GroupProductArgs& p, int group_log2, bool few, void* operands, void* sums, hipStream_t st)
+void product_to(same::GroupProductArgs& p, int group_log2, bool few, const Laid& to, hipStream_t st)
 {
     switch (group_log2) {
-        case 5:  return product_launch<TI, 5>(p, few, operands, sums, st);
-        case 6:  return product_launch<TI, 6>(p, few, operands, sums, st);
-        default: return product_launch<TI, 7>(p, few, operands, sums, st);
+        case 5:  return product_launch<TI, 5>(p, few, to, st);
+        case 6:  return product_launch<TI, 6>(p, few, to, st);
+        default: return product_launch<TI, 7>(p, few, to, st);
     }
 }
 
@@ -199,7 +214,8 @@ int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float
     const RowsSpace space = rows_space(a, b);
     if (space.bytes > 0 && (!workspace || workspace_bytes < space.bytes || (uintptr_t)workspace % 16))
         return fail_without_handle(SAME_LDA_EINVAL, "group_product: needs %zu bytes of workspace aligned to 16 (got %zu)", space.bytes, workspace ? workspace_bytes : (size_t)0);
-    void* const sums = static_cast<char*>(workspace) + space.operands;
+    char* const w = static_cast<char*>(workspace);
+    const Laid to = {reinterpret_cast<same::v4u32*>(w), reinterpret_cast<float*>(w + space.operands), reinterpret_cast<float*>(w + space.operands + space.sums)};
     const bool few = few_rows(a, b);
     const int64_t rows_each = rows_of_a(a);
     const int group_log2 = __builtin_ctz((unsigned)b->type);
@@ -222,9 +238,9 @@ int same_lda_group_product(const same_lda_rows* a, const same_lda_rows* b, float
             p.out = static_cast<char*>(out->data) + (i * out->stride + j) * element_bytes(out->type);
             p.out_stride = out->stride;
             switch (a->type) {
-                case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, few, workspace, sums, st); break;
-                case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, few, workspace, sums, st); break;
-                default:              product_to<_Float16>(p, group_log2, few, workspace, sums, st); break;
+                case SAME_LDA_FLOAT:  product_to<float>(p, group_log2, few, to, st); break;
+                case SAME_LDA_BFLOAT: product_to<__bf16>(p, group_log2, few, to, st); break;
+                default:              product_to<_Float16>(p, group_log2, few, to, st); break;
             }
         }
     return launched("group_product");

@@ -61,3 +61,118 @@ def test_groups_beyond_the_last_finite_bfloat16_numbers_are_read_back(group):
     x[8] = -low
     x[9] = rng.uniform(-TOP, low, 300)
     read_back(torch.from_numpy(x).float(), group)
+
+
+# ---- the product of rows of binary32 numbers of any size
+#
+# Tolerance: that of products of rows of usual numbers, (2 N + 2 groups) 2^-24 of the sum over groups of (15 |s| + |b|) sum |a| with N = 3 G terms of
+# a group's sum, and 2 u for the scale and a power of two.  Below 2^-126 an addition is off by up to 2^-150 instead: two for a group and three at the end.
+# In rows whose largest number is 2^-64 or more, numbers below 2^-109 lose what lies below 2^-133 of them.
+
+SHAPES = [(1, 40, 300), (4, 33, 1100), (3, 70, 4000), (5, 40, 130), (13, 50, 1000), (16, 40, 4000), (9, 300, 2048),        # few rows: stacked pieces, three instructions; 1, 2, 4 blocks a wave
+          (2, 50, 4130), (30, 300, 4200), (33, 9000, 4200), (40, 2000, 5000),                                              # tiles, long rows
+          (40, 20_000, 600), (130, 20_000, 300), (300, 8000, 1100), (520, 9000, 4096), (24, 6400, 2000), (18, 33_000, 700)]  # tiles, up to 32 blocks
+
+
+def table_of(g, N, K, group, size):
+    """Numbers around `size` in grouped integers, and the numbers, steps and bases that it holds, in double."""
+    q = binding.group_quantize(torch.randn(N, K, device=DEV, generator=g) * size, group)
+    s, b = q.scales[:, :, 0].double(), q.scales[:, :, 1].double()
+    e = torch.arange(K, device=DEV)
+    at = e % 128
+    half = at % 8 // 2 + 4 * (at % 2)
+    byte = e // 128 * 64 + 4 * (4 * (at % 32 // 8) + at // 32) + half // 2
+    w = (q.codes[:, byte].int() >> (4 * (half % 2)).int() & 15).double()
+    return q, w * s.repeat_interleave(group, 1)[:, :K] + b.repeat_interleave(group, 1)[:, :K], s, b
+
+
+def check(x, q, w, s, b, scale=1.0):
+    got = binding.group_product(x, q, scale, dtype=torch.float32)
+    X = x.double()
+    want = scale * (X @ w.t().contiguous())
+    groups = q.scales.shape[1]
+
+    def sums(y):
+        return torch.nn.functional.pad(y, (0, groups * q.group - y.shape[1])).view(len(y), groups, q.group).sum(2)
+
+    weight = (15.0 * s.abs() + b.abs()).t().contiguous()
+    lost = 2.0 ** -133 * ((X.abs() < 2.0 ** -109) & (X != 0) & (X.abs().amax(1, keepdim=True) >= 2.0 ** -64)).double()
+    n = q.group * (3 if x.dtype == torch.float32 else 1)
+    size = abs(scale) * (sums(X.abs()) @ weight)
+    assert torch.isfinite(size).all() and size.max() < TOP
+    bound = 1.01 * ((2 * n + 2 * groups + 3) * U * size + abs(scale) * (sums(lost) @ weight) + (2 * groups + 3) * 2.0 ** -150 * max(1.0, abs(scale)))
+    bad = ~((got.double() - want).abs() <= bound)
+    assert not bad.any(), (int(bad.sum()), torch.argwhere(bad)[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist(), bound[bad][:4].tolist())
+
+
+@pytest.mark.parametrize("e", [-146, -140, -132, -126, -120, -112, -104, -80, -65, -62, 0, 90, 110, 113, 117])
+@pytest.mark.parametrize("M, N, K", SHAPES[:-6])
+def test_product_of_rows_of_one_size(M, N, K, e):
+    g = torch.Generator(device=DEV).manual_seed(M + e)
+    x = torch.randn(M, K, device=DEV, generator=g) * 2.0 ** max(e, -126) * 2.0 ** min(e + 126, 0)
+    for group in GROUPS:
+        check(x, *table_of(g, N, K, group, 2.0 ** max(-60, min(60, -e // 2))), scale=0.75)
+
+
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("M, N, K", SHAPES)
+def test_product_of_rows_of_every_size_together(M, N, K, group):
+    """Rows from 2^-149 to 2^112 next to each other, one of zeros; and one whose numbers are of every size themselves."""
+    g = torch.Generator(device=DEV).manual_seed(N)
+    x = torch.randn(M, K, device=DEV, generator=g, dtype=torch.float64) * 2.0 ** torch.randint(-145, 112, (M, 1), device=DEV, generator=g).double()
+    if M > 2:
+        x[1] = 0.0
+        x[2] = torch.randn(K, device=DEV, generator=g, dtype=torch.float64) * 2.0 ** torch.randint(-145, 100, (K,), device=DEV, generator=g).double()
+    check(x.float(), *table_of(g, N, K, group, 1.0))
+
+
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("M, N, K", SHAPES)
+def test_numbers_of_24_bits_count_whole_down_to_the_least(M, N, K, group):
+    """One number of 24 bits (or, where it is subnormal, all that there are) in a row, codes 1, 2, 4 or 8 and steps that are powers of two: the
+    product is one number of binary32, and has to be that."""
+    rng = np.random.default_rng(K)
+    e = rng.integers(-149, 100, M)
+    odd = 2 * rng.integers(1 << 22, 1 << 23, M) + 1
+    a = np.zeros((M, K))
+    a[np.arange(M), rng.integers(0, K, M)] = np.ldexp(np.where(e < -140, odd >> 4, odd).astype(np.float64), np.maximum(e - 23, -149)) * rng.choice([-1, 1], M)
+    x = torch.from_numpy(a).float()
+    assert (x.double().numpy() == a).all()
+    blocks = -(-K // 128)
+    codes = torch.from_numpy((1 << rng.integers(0, 4, (N, 64 * blocks))) | (16 << rng.integers(0, 4, (N, 64 * blocks)))).to(torch.uint8)
+    scales = torch.zeros(N, blocks * (128 // group), 2, dtype=torch.bfloat16)
+    scales[:, :, 0] = torch.from_numpy(2.0 ** rng.integers(0, 20, (N, blocks * (128 // group)))).to(torch.bfloat16)
+    q = binding.GroupMatrix(codes.to(DEV), scales.to(DEV), K, group)
+    want = x.to(DEV).double() @ binding.group_dequantize(q).double().t().contiguous()
+    assert torch.equal(binding.group_product(x.to(DEV), q).double(), want)
+
+
+@pytest.mark.parametrize("dtype, e", [(torch.float32, -149), (torch.float32, -139), (torch.float32, -125), (torch.float32, -64), (torch.float32, 60), (torch.float32, 111), (torch.float32, 117),
+                                      (torch.bfloat16, -133), (torch.bfloat16, -126), (torch.bfloat16, 100), (torch.float16, -24), (torch.float16, -14), (torch.float16, 14)])
+@pytest.mark.parametrize("M, N, K", SHAPES)
+def test_product_of_small_integers_times_a_power_of_two_is_exact(M, N, K, dtype, e):
+    """Every sum on the way is an integer below 2^24 of the least unit: the result has to be that one."""
+    rng = np.random.default_rng(M)
+    a = torch.from_numpy(np.ldexp(rng.integers(-3, 4, (M, K)).astype(np.float64), e)).to(dtype)
+    t = -40 if e > 50 else 0
+    for group in GROUPS:
+        codes = torch.randint(0, 256, (N, -(-K // 128) * 64), device=DEV, dtype=torch.uint8, generator=torch.Generator(device=DEV).manual_seed(N))
+        n = -(-K // 128) * (128 // group)
+        scales = torch.from_numpy(np.ldexp(np.stack((2.0 ** rng.integers(0, 3, (N, n)), rng.integers(-4, 5, (N, n))), axis=2), t)).to(torch.bfloat16)
+        q = binding.GroupMatrix(codes, scales.to(DEV), K, group)
+        want = a.to(DEV).double() @ binding.group_dequantize(q).double().t().contiguous()
+        assert torch.equal(binding.group_product(a.to(DEV), q, dtype=torch.float32).double(), want)
+
+
+@pytest.mark.parametrize("M, N, K", [(3, 70, 4000), (13, 50, 1000), (30, 300, 4200), (130, 20_000, 300)])
+def test_rows_that_are_not_finite_do_not_touch_small_and_large_ones(M, N, K):
+    g = torch.Generator(device=DEV).manual_seed(5)
+    q, w, s, b = table_of(g, N, K, 64, 1.0)
+    x = torch.randn(M, K, device=DEV, generator=g) * 2.0 ** -126
+    x[-1] = x[-1] * 2.0 ** 120 * 2.0 ** 115
+    want = binding.group_product(x, q)
+    x[0, K // 2], x[1, 3] = float("inf"), float("nan")
+    got = binding.group_product(x, q)
+    assert torch.equal(got[2:], want[2:]) and not torch.isfinite(got[:2]).any()
+    x[0, K // 2], x[1, 3] = 0.0, 0.0
+    check(x, q, w, s, b)
