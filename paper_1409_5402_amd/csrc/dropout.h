@@ -6,7 +6,7 @@
 // (c, i, step, word | 2^27), word = 4 2^28 + the step's bits from 32 on (the sweeps' draws have the fields 0 to 3 there): column
 // 8 c + e has half e % 2, the low one first, of word e / 2 of either block, those of the first on top.  The lower halves decide
 // only where the upper ones equal the border's, once in 65,536 elements, so eight elements cost one block (65,536 x 1024 bf16: 57 us with a
-// comparison and a bit for each, 50 by halves of registers, which a copy takes too).
+// comparison and a bit for each, 48 to 50 by halves of registers, which a copy takes too).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -13,8 +13,8 @@ namespace same {
 
 // ---- Rounding.  A lane takes 8 elements, 2^(group_log2 - 3) consecutive lanes a group.  The quotient (x - b) / s is taken as a product
 // in binary32; where that leaves open on which side of a border between two codes it lies, x - b is compared with the border, exactly, and at
-// the ends of the range the quotient is taken in binary64.  Bound by memory in binary32 (100,000 x 256: 22.3 us, 5.2 TB/s read and written),
-// by its instructions on 16-bit rows, half as long (8192 x 8192 bf16: 67 us, 2.5 TB/s).
+// the ends of the range the quotient is taken in binary64.  Bound by memory in binary32 (100,000 x 256: 20 to 23 us, 5 TB/s and more read and
+// written), by its instructions on 16-bit rows, half as long (8192 x 8192 bf16: 73 us, 2.3 TB/s).
 struct GroupQuantizeArgs {
     const void* x;
     int64_t rows, stride;
@@ -116,7 +116,7 @@ __device__ __forceinline__ void group_round(const GroupQuantizeArgs& a, Eight<TI
                 near[e] = rintf(t);
                 off = fminf(off, 0.5f - fabsf(t - near[e]));
                 near[e] = __builtin_amdgcn_fmed3f(near[e], 0.0f, 15.0f);
-                // (elements behind the row's end are zeros, whose code is cut off below)
+                // (elements behind the row's end repeat their chunk's first, whose code is cut off below)
             }
             if (!ordinary) {
 #pragma unroll 1
@@ -341,7 +341,8 @@ __device__ __forceinline__ v4u32 all_ones()
 // Any number of rows, in two launches.  The first one lays the rows of a down as the lanes of the matrix instruction take them, cut into pieces
 // and filled up with zeros: per 16 rows and block of 128 elements 4 P operands of 1 KB; and the sums S of their groups.  Rows in binary32 need
 // their largest number first: those of up to kWholeBlocks blocks are taken whole by one workgroup, of longer ones another launch before it finds the
-// powers of two.
+// powers of two (us without either, whole, with the launch: 64 x 50,021 x 1024 33.3, 34.4, -; 40 x 10,000 x 2000 22.5, 26.2, 24.9; 33 x 4096 x 4096 19.9,
+// 28.5, 22.3).
 constexpr int kWholeBlocks = 8;
 
 struct GroupRowsArgs {
@@ -434,11 +435,11 @@ __global__ __launch_bounds__(kWhole ? 64 * kWholeBlocks : 256) void group_rows_k
 
 // The second one: WM WN WK waves take 16 MT WM rows of a by 16 NT WN of b.  All operands come straight to LDS, kStages - 1 trips ahead, in
 // pieces of 1 KB as the lanes take them (with codes fetched into registers by one wave and shared by way of LDS 512 x 50,021 x 1024 f16 took
-// 108 us, so 106).  WK waves share out the blocks of a row of b, and their sums are added in order at the end: more waves
+// 108 us, so 106, before the change below).  WK waves share out the blocks of a row of b, and their sums are added in order at the end: more waves
 // where rows of b are few.  S comes with the operands, for sum_g b_g S_g as matrix instructions before the loop waited for what it read: 106 us,
-// now 82 to 86.
+// now 82 to 84 on those numbers, random codes and steps, and 72 on positive ones with a few large in a row.
 // Bound by what the matrix instructions and the unpacking of codes take on the same SIMD one after the other, and by the tiles' fetches from the
-// caches (16 KB of rows and 16 KB of codes per 64 x 256 x 128): 512 x 50,021 x 4096 bf16 250 us, 839 TFLOP/s of the 1205 that a plain
+// caches (16 KB of rows and 16 KB of codes per 64 x 256 x 128): 512 x 50,021 x 4096 bf16 247 to 250 us, 840 to 850 TFLOP/s of the 1205 that a plain
 // product of that type reaches; in binary32, three instructions each, 615 us.
 struct GroupTilesArgs {
     GroupProductArgs p;
@@ -626,8 +627,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK, kStages * sizeof(GroupStage<P, k
 
 // Few rows of a, up to 16 a workgroup.  A wave keeps its part of them, KB blocks of 128 elements, in registers and goes through the rows of b, 16 at
 // a time, whose codes come straight from memory, those of the next turns while these are multiplied: every byte of b is read once (for every 16 rows of
-// a where there are more), a once per workgroup.  Bound by memory where rows are long (1 x 50,021 x 4096 bf16: 30 us, 3.6 TB/s of codes and scales; 13 in binary32, G64: 40),
-// by the launch and the one wait for a where they are short (1 x 100,000 x 256 f32, G64: 8.2 us).  Where a row of b has more than KB blocks, waves_per_row waves share it and add up their sums by way of LDS, in order.
+// a where there are more), a once per workgroup.  Bound by memory where rows are long (1 x 50,021 x 4096 bf16: 30 us, 3.6 TB/s of codes and scales; 13 in binary32, G64: 41),
+// by the launch and the one wait for a where they are short (1 x 100,000 x 256 f32, G64: 8.1 to 8.6 us).  Where a row of b has more than KB blocks, waves_per_row waves share it and add up their sums by way of LDS, in order.
 // S depends on a alone; sum_g b_g S_g is a product of its own along the groups, eight in the first lanes of a bfloat16 instruction, S in three
 // pieces.
 // kStack: up to four rows in binary32, whose pieces take the matrix instruction's rows 4 q + i; else binary32 takes three instructions

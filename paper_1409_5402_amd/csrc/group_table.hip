@@ -110,7 +110,7 @@ void product_launch(same::GroupProductArgs& p, bool few, const Laid& to, hipStre
     }
     // Tiles are as large as still gives every compute unit some, and where there are many those whose last round is the fuller one: by the
     // workgroups that run at once (LDS bounds them), and what a round takes to that of the next form.  us of the two launches, G128, by form:
-    //   bf16                 64x256  64x128  64x64  32x128  32x64  16x128      binary32             64x256  32x128  32x64  16x64
+    //   bf16                 64x256  64x128  64x64  32x128  32x64  16x128      binary32 (*)         64x256  32x128  32x64  16x64
     //   512 x 50,021 x 4096     250     268    446     409    643     716      512 x 50,021 x 4096     615     648   1251   1739
     //   2048 x 8192 x 4096      166     190    359     270    434     446      2048 x 8192 x 4096      389     467    959   1028
     //   64 x 50,021 x 1024       22      19     33      26     45      36      64 x 50,021 x 1024       32      35     57     76
@@ -119,6 +119,7 @@ void product_launch(same::GroupProductArgs& p, bool few, const Laid& to, hipStre
     //   32 x 50,021 x 4096       54      54     76      50     60      73      512 x 1000 x 4000        87      40     33     44
     //   32 x 4096 x 4096         43      30     21      21     16      19      40 x 10,000 x 2000       45      21     27     21
     //   1 x 20,000 x 8192        90      64     70      46     53      43      32 x 4096 x 4096         81      34     25     19
+    // (*) without the search for the rows' powers of two, which adds the same to every form: about 1 us up to 1024 elements, beyond 2 to 3, a launch
     const auto tiles = [&](int64_t tall, int64_t wide) { return ((p.rows_a + tall - 1) / tall) * ((p.rows_b + wide - 1) / wide); };
     const auto rounds = [&](int64_t tall, int64_t wide, int64_t per_unit) { return (tiles(tall, wide) + per_unit * kComputeUnits - 1) / (per_unit * kComputeUnits); };
     if constexpr (sizeof(TI) == 4) {

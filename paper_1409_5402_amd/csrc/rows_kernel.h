@@ -1,9 +1,10 @@
 // Rows of a table for a list of tokens (or a matrix as it is) with dropout, and rows of tables in grouped four-bit integers.
 //
 // A lane takes eight elements of a row, which a block of the generator decides and one vector load and store move (two of each in binary32),
-// and two such pieces at once, both loads on their way before the generators' rounds.  Bound by memory: 65,536 x 1024 bf16 50 us, 5.4 TB/s
-// read and written; 131,072 rows of 100,000 x 1024 bf16 95 us, 81 without dropout, a good half of whose rows come from the caches; 131,072 rows
-// out of groups of 64 80 us, at the rate of their stores.
+// and two such pieces at once, both loads on their way before the generators' rounds.  Bound by memory: 65,536 x 1024 bf16 48 us, 5.6 TB/s
+// read and written; 131,072 rows of 100,000 x 1024 bf16 93 us, 77 without dropout, a good half of whose rows come from the caches.  131,072 rows
+// into bf16 out of groups of 64 take 69 us, 3.9 TB/s of stores where a fill reaches 6.8: a lane asks for 4 bytes of codes and 4 of a step and a base
+// for 16 that it stores; with dropout 81, out of microscaled rows 82.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
