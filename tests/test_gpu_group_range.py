@@ -176,3 +176,40 @@ def test_rows_that_are_not_finite_do_not_touch_small_and_large_ones(M, N, K):
     assert torch.equal(got[2:], want[2:]) and not torch.isfinite(got[:2]).any()
     x[0, K // 2], x[1, 3] = 0.0, 0.0
     check(x, q, w, s, b)
+
+
+@pytest.mark.parametrize("M, N, K", [(3, 70, 4000), (13, 50, 1000), (1, 30, 5), (30, 300, 4200), (130, 20_000, 300), (18, 33_000, 700)])
+def test_what_stands_between_the_rows_does_not_count_for_their_powers(M, N, K):
+    g = torch.Generator(device=DEV).manual_seed(6)
+    q = table_of(g, N, K, 32, 1.0)[0]
+    x = torch.randn(M, K, device=DEV, generator=g) * 2.0 ** -120
+    want = binding.group_product(x, q)
+    for gap, at, other in [(1, 0, 3e38), (5, 3, float("inf")), (9, 2, float("nan")), (4, 4, 2.0 ** -149)]:
+        buffer = torch.full((at + M * (K + gap) + 16,), other, device=DEV)
+        rows = torch.as_strided(buffer, (M, K), (K + gap, 1), at)
+        rows.copy_(x)
+        assert torch.equal(binding.group_product(rows, q), want)
+
+
+def test_replays_find_each_rows_power_anew():
+    for M, N, K in [(3, 70, 4000), (13, 50, 1000), (30, 300, 4200), (130, 20_000, 300)]:
+        g = torch.Generator(device=DEV).manual_seed(7)
+        q = table_of(g, N, K, 64, 1.0)[0]
+        x = torch.randn(M, K, device=DEV, generator=g)
+        out, source = torch.empty(M, N, device=DEV), x.clone()
+        binding.group_product(source, q, out=out)
+        graph, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            binding.group_product(source, q, out=out)
+        other, twice = torch.empty_like(out), x * 2.0
+        with torch.cuda.graph(second):
+            binding.group_product(twice, q, out=other)
+        for e in (0, -120, 113, -64, 60, -120):
+            source.copy_(x * 2.0 ** e)
+            source[::2] *= 2.0 ** -6
+            twice.copy_(source * 0.5)
+            graph.replay()
+            second.replay()
+            want, half = binding.group_product(source, q), binding.group_product(twice, q)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and torch.equal(other, half)
